@@ -62,7 +62,11 @@ enum fs_error {
                                       boundary (nothing is ever thrown across it)                       */
 };
 
-enum fs_dtype { FS_F32 = 0, FS_F16 = 1, FS_BF16 = 2, FS_I32 = 3 };
+enum fs_dtype { FS_F32 = 0, FS_F16 = 1, FS_BF16 = 2, FS_I32 = 3, FS_E4M3 = 4 };
+/* FS_E4M3: 8-bit floating point for storage (1 sign, 4 exponent, 3 mantissa bits, bias 7; no infinities, largest value 448),
+ * held next to the float32 scales of blocks of values (8-bit checkpoints, below).  Graph inputs, targets of FS_CONVERT and
+ * outputs can have it; transposes cannot.  Rounding to it is to nearest-even; what is larger than 448, infinities too,
+ * becomes 448 with its sign, NaN stays NaN.                                              */
 
 /* Memory-intensive op vocabulary (Section 4: light element-wise, expensive
  * element-wise, reduction; Section 3.1: broadcast; plus transpose and convert).

@@ -53,6 +53,12 @@ def to_f64(a: np.ndarray, dtype: str) -> np.ndarray:
         return np.asarray(a, dtype=np.float32).astype(np.float64)
     if dtype == "i32":
         return np.asarray(a, dtype=np.int32).astype(np.float64)
+    if dtype == "e4m3":   # sign, 4 exponent bits (bias 7), 3 mantissa bits; the all-ones pattern is NaN
+        b = np.asarray(a, dtype=np.uint8).astype(np.int64)
+        e, m = (b >> 3) & 15, b & 7
+        v = np.where(e == 0, np.ldexp(m.astype(np.float64), -9), np.ldexp(8.0 + m, e - 10))
+        v = np.where((b & 0x7F) == 0x7F, np.nan, v)
+        return np.where(b & 0x80, -v, v)
     raise ValueError(dtype)
 
 
@@ -73,6 +79,11 @@ def round_to(a: np.ndarray, dtype: str) -> np.ndarray:
         out[nz] = np.ldexp(q, e - 8)
         out[~nz] = a[~nz]
         return out
+    if dtype == "e4m3":
+        # 4 significant bits, spacing 2**-9 below 2**-6; what is beyond 448 (infinities too) saturates
+        c = np.clip(a, -448.0, 448.0)
+        e = np.maximum(np.frexp(np.where(np.isnan(c), 0.0, c))[1], -5)
+        return np.ldexp(np.rint(np.ldexp(c, 4 - e)), e - 4)
     raise ValueError(dtype)
 
 

@@ -12,7 +12,7 @@ import os
 from typing import Dict, List, Optional, Sequence
 
 FS_MAX_RANK = 4
-DTYPE = {"f32": 0, "f16": 1, "bf16": 2, "i32": 3}
+DTYPE = {"f32": 0, "f16": 1, "bf16": 2, "i32": 3, "e4m3": 4}
 DTYPE_NAME = {v: k for k, v in DTYPE.items()}
 OPCODE = {
     "add": 0, "sub": 1, "mul": 2, "div": 3, "max": 4, "scale": 5, "add_scalar": 6, "square": 7,
@@ -556,27 +556,31 @@ def bind_probe(dst_ptr: int, src_ptr: int, stream_bytes: int, reads: int, writes
 # ---- torch <-> storage helpers (memory plumbing, no arithmetic) --------------------
 def torch_dtype(name: str):
     import torch
-    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16, "i32": torch.int32}[name]
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16, "i32": torch.int32, "e4m3": torch.float8_e4m3fn}[name]
 
 
 def to_device(array, dtype: str, device="cuda"):
-    """numpy storage array (bf16 as uint16 bit patterns) -> torch device tensor of the storage dtype."""
+    """numpy storage array (bf16 as uint16, e4m3 as uint8 bit patterns) -> torch device tensor of the storage dtype."""
     import numpy as np
     import torch
     if dtype == "bf16":
         t = torch.from_numpy(np.ascontiguousarray(array).view(np.int16)).view(torch.bfloat16)
+    elif dtype == "e4m3":
+        t = torch.from_numpy(np.ascontiguousarray(array)).view(torch.float8_e4m3fn)
     else:
         t = torch.from_numpy(np.ascontiguousarray(array))
     return t.to(device)
 
 
 def to_host(tensor, dtype: str):
-    """torch device tensor -> numpy storage array (bf16 as uint16 bit patterns)."""
+    """torch device tensor -> numpy storage array (bf16 as uint16, e4m3 as uint8 bit patterns)."""
     import numpy as np
     import torch
     t = tensor.detach().cpu().contiguous()
     if dtype == "bf16":
         return t.view(torch.int16).numpy().view(np.uint16)
+    if dtype == "e4m3":
+        return t.view(torch.uint8).numpy()
     return t.numpy()
 
 

@@ -37,13 +37,14 @@ fs_status fail_caught(const char* who) {
   }
 }
 
-int dtype_bytes(int32_t dt) { return (dt == FS_F32 || dt == FS_I32) ? 4 : 2; }
+int dtype_bytes(int32_t dt) { return (dt == FS_F32 || dt == FS_I32) ? 4 : dt == FS_E4M3 ? 1 : 2; }
 const char* dtype_name(int32_t dt) {
   switch (dt) {
     case FS_F32: return "f32";
     case FS_F16: return "f16";
     case FS_BF16: return "bf16";
     case FS_I32: return "i32";
+    case FS_E4M3: return "e4m3";
     default: return "?";
   }
 }
@@ -59,8 +60,14 @@ const char* scheme_name(int32_t s) {
   return (s >= 0 && s <= FS_SCHEME_GLOBAL) ? names[s] : "?";
 }
 
-static bool valid_dtype(int32_t dt) { return dt >= FS_F32 && dt <= FS_I32; }
-static bool float_dtype(int32_t dt) { return dt == FS_F32 || dt == FS_F16 || dt == FS_BF16; }
+static bool valid_dtype(int32_t dt) { return dt >= FS_F32 && dt <= FS_E4M3; }
+static bool float_dtype(int32_t dt) { return dt == FS_F32 || dt == FS_F16 || dt == FS_BF16 || dt == FS_E4M3; }
+
+bool holds_8bit(const fs_graph& g) {
+  for (const Tensor& t : g.tensors)
+    if (t.dtype == FS_E4M3 || (t.output_slot >= 0 && t.store_as == FS_E4M3)) return true;
+  return false;
+}
 
 static int operand_count(int32_t opcode) { return opcode <= FS_MAX ? 2 : 1; }
 
@@ -136,6 +143,7 @@ fs_tensor fs_graph_op(fs_graph* g, int32_t opcode, int32_t n_in, const fs_tensor
     const int32_t dt = g->tensors[in[i]].dtype;
     if (!float_dtype(dt) && !is_transpose)
       return fail(FS_ERR_DTYPE, "fs_graph_op(%s): operand %d has dtype %s; only transpose moves integer tensors", opcode_name(opcode), i, dtype_name(dt));
+    if (dt == FS_E4M3 && is_transpose) return fail(FS_ERR_DTYPE, "fs_graph_op(transpose): 8-bit tensors are not transposed; convert first");
   }
 
   if (opcode <= FS_MAX) {

@@ -68,6 +68,8 @@ struct fs_graph {
 
 namespace fs {
 
+bool holds_8bit(const fs_graph& g);   // some tensor of the graph is FS_E4M3
+
 // ---- plan ------------------------------------------------------------------
 
 // One kernel launch of a plan.  `args` is a POD blob the launcher understands;

@@ -437,6 +437,8 @@ int fs::streamed_loads(const Launch& l) {
     case K_TCHAIN_WAVE: case K_TCHAIN_LDS: return a.u.tchain.stream;
     case K_ROW_WAVE: case K_ROW_BLOCK: return a.u.row.stream;
     case K_ROW_GENERATED: return a.u.prog.stream;
+    case K_CHECKPOINT_WAVE: case K_CHECKPOINT_BLOCK: case K_CHECKPOINT_GRAD: case K_CHECKPOINT_GRAD_SUMS:
+      return a.u.checkpoint.vec > 1 ? a.u.checkpoint.stream : -1;
     default: return -1;
   }
 }

@@ -1134,6 +1134,7 @@ bool make_candidate(const fs_graph& g, const Compiler& c, int vec, const Shape& 
 }  // namespace
 
 bool build_row_program(const fs_graph& g, std::vector<Candidate>* out) {
+  if (holds_8bit(g)) return false;   // neither form reads or writes 8-bit values
   Compiler c(g);
   if (!c.run()) return false;
   const int64_t bytes_min = graph_bytes_min(g);
@@ -1175,6 +1176,7 @@ static bool sums_need_no_reduction(const RowProgP& p) {
 // 6.3 / 3.8; [256,3072] 6.1 / 3.7, 7.0 / 4.0, 6.1 / 3.7.  The arithmetic is done twice as well: patterns of more than these three have are
 // left out.
 bool sums_beside_rows(const fs_graph& g, SumsBesideRows* out) {
+  if (holds_8bit(g)) return false;
   Compiler c(g);
   if (g.cut_out || !c.run() || c.n_colsum == 0 || c.n_rout + c.n_colsum > kProgMaxOperands || !sums_need_no_reduction(c.p)) return false;
   if (c.p.stream || c.p.n_full > 3 || c.n_colsum > 2 || c.vec_instr > 20 || c.trans > 4) return false;

@@ -27,14 +27,17 @@ FastDiv make_fastdiv(uint32_t d) {
 std::string build_stitched(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack) {
   PackForm scratch_form;
   if (!pack) pack = &scratch_form;
-  struct Family { const char* name; bool (*build)(const fs_graph&, std::vector<Candidate>*, PackForm*); };
+  struct Family { const char* name; bool (*build)(const fs_graph&, std::vector<Candidate>*, PackForm*); bool knows_8bit; };
   static const Family families[] = {
-      {"softmax", build_softmax}, {"layernorm", build_layernorm}, {"bias_gelu", build_gelu},
-      {"transpose_chain", build_tchain}, {"softmax_backward", build_softmax_backward}, {"rmsnorm", build_rmsnorm},
-      {"layernorm_backward", build_layernorm_backward}, {"transpose", build_transpose},
+      {"softmax", build_softmax, false}, {"layernorm", build_layernorm, false}, {"bias_gelu", build_gelu, false},
+      {"transpose_chain", build_tchain, false}, {"softmax_backward", build_softmax_backward, false}, {"rmsnorm", build_rmsnorm, false},
+      {"layernorm_backward", build_layernorm_backward, false}, {"transpose", build_transpose, false},
+      {"checkpoint", build_checkpoint, true}, {"checkpoint_backward", build_checkpoint_backward, true},
   };
+  const bool has_8bit = holds_8bit(g);
   std::string recognised;
   for (const Family& f : families) {
+    if (has_8bit && !f.knows_8bit) continue;
     out->clear();
     *pack = PackForm();
     if (f.build(g, out, pack)) {

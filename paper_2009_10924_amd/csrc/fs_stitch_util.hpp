@@ -101,6 +101,8 @@ bool build_tchain(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack
 bool build_transpose(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
 bool build_softmax_backward(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
 bool build_rmsnorm(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
+bool build_checkpoint(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
+bool build_checkpoint_backward(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
 // The launch that folds [n_rows, width] float32 column partials (second step of a global hand-off).
 // K_COLFOLD over partial rows of `width` floats (`stride` floats apart, 0 = width): columns below `split` go to the
 // launch's first output, the rest to its second.

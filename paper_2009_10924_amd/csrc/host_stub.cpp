@@ -16,7 +16,8 @@ namespace {
 const char* const kNames[K_COUNT] = {"unary", "binary", "reduce_row", "reduce_mid", "transpose_rows", "transpose_tile", "copy",
                                      "softmax_wave", "softmax_block", "layernorm_wave", "layernorm_block", "bias_gelu",
                                      "bias_gelu_dbias", "colfold", "tchain_wave", "tchain_lds", "row_wave", "row_block",
-                                     "row_program", "layernorm_bwd", "row_generated"};
+                                     "row_program", "layernorm_bwd", "row_generated", "checkpoint_wave", "checkpoint_block",
+                                     "checkpoint_long", "checkpoint_grad", "checkpoint_grad_sums"};
 long g_launches = 0;
 
 // what any launch must satisfy whatever the kernel: returns a hipError-like code (1 = invalid value)

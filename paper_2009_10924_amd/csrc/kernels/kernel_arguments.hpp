@@ -207,6 +207,21 @@ __attribute__((always_inline)) inline bool list_arguments(int32_t kernel, const 
       l->add(p[0], p[1], p[2], r.rows, row_word(r.cols, lanes), p[4], r.f[0], r.f[1]);
       return true;
     }
+    case K_CHECKPOINT_WAVE: case K_CHECKPOINT_BLOCK: case K_CHECKPOINT_LONG: {
+      const CheckpointP& c = a.u.checkpoint;
+      l->add(p[0], p[1], p[2], p[3], p[4], c.rows, c.cols, c.lanes_log2, c.inv_max, c.tiny, c.div_period.d, c.div_period.m, c.div_period.s);
+      return true;
+    }
+    case K_CHECKPOINT_GRAD: {
+      const CheckpointP& c = a.u.checkpoint;
+      l->add(p[0], p[1], p[2], p[3], c.rows * c.cols, c.div_cols.d, c.div_cols.m, c.div_cols.s);
+      return true;
+    }
+    case K_CHECKPOINT_GRAD_SUMS: {
+      const CheckpointP& c = a.u.checkpoint;
+      l->add(p[0], p[1], p[2], p[3], p[4], c.rows, c.blocks * c.cols, c.n_row_blocks, c.blocks, c.cols, colsum_pitch(c.blocks * c.cols));
+      return true;
+    }
     default: return false;
   }
 }

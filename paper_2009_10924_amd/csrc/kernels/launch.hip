@@ -10,7 +10,8 @@ namespace {
 const char* const kNames[K_COUNT] = {
     "unary", "binary", "reduce_row", "reduce_mid", "transpose_rows", "transpose_tile", "copy", "softmax_wave", "softmax_block",
     "layernorm_wave", "layernorm_block", "bias_gelu", "bias_gelu_dbias", "colfold", "tchain_wave", "tchain_lds", "row_wave",
-    "row_block", "row_program", "layernorm_bwd", "row_generated",
+    "row_block", "row_program", "layernorm_bwd", "row_generated", "checkpoint_wave", "checkpoint_block", "checkpoint_long", "checkpoint_grad",
+    "checkpoint_grad_sums",
 };
 
 const void* symbol_for(int32_t kernel, const KernelArgs& a) {
@@ -30,6 +31,8 @@ const void* symbol_for(int32_t kernel, const KernelArgs& a) {
       return rowops_kernel_symbol(kernel, a);
     case K_ROW_PROGRAM:
       return rowprog_kernel_symbol(kernel, a);
+    case K_CHECKPOINT_WAVE: case K_CHECKPOINT_BLOCK: case K_CHECKPOINT_LONG: case K_CHECKPOINT_GRAD: case K_CHECKPOINT_GRAD_SUMS:
+      return checkpoint_kernel_symbol(kernel, a);
     default:
       return nullptr;
   }

@@ -16,7 +16,7 @@ constexpr int kSlotFull = 0, kSlotCol = 8, kSlotRscal = 16, kSlotOut = 24, kSlot
 constexpr int kGenArgPtrs = 41;   // pointers of a generated kernel: the operand slots + the workspace
 
 // storage dtypes, numbered like the public fs_dtype
-enum DType : int32_t { DT_F32 = 0, DT_F16 = 1, DT_BF16 = 2, DT_I32 = 3 };
+enum DType : int32_t { DT_F32 = 0, DT_F16 = 1, DT_BF16 = 2, DT_I32 = 3, DT_E4M3 = 4 };
 
 enum KernelId : int32_t {
   // per-op baseline
@@ -45,6 +45,11 @@ enum KernelId : int32_t {
   K_ROW_GENERATED,     // a kernel generated and compiled for one row pattern at plan time; pointer slots as K_ROW_PROGRAM,
                        // p40 the workspace for column partial sums (or null).
                        // Not in the compiled-in table: launched through its own handle (gen_launch)
+  K_CHECKPOINT_WAVE,   // p0 x, p1 bias (or null), p2 y (or null), p3 q, p4 scales : a lane group per block of values
+  K_CHECKPOINT_BLOCK,  // a workgroup per block
+  K_CHECKPOINT_LONG,   // a workgroup per block, which it reads twice
+  K_CHECKPOINT_GRAD,   // p0 q, p1 scales, p2 dy (or null), p3 dx or the values themselves
+  K_CHECKPOINT_GRAD_SUMS,   // p0 q, p1 scales, p2 dy, p3 dx, p4 partials [n_row_blocks, pitch] f32 (folded by K_COLFOLD)
   K_COUNT
 };
 
@@ -156,6 +161,20 @@ struct LnBwdP {
   int32_t lanes_per_row, lanes_log2, vecs_per_lane;
   int32_t waves, rows_per_group;    // workgroup = waves x 64 lanes; rows each lane group loads up front
   int32_t fast;                     // 1: the row fills the lanes exactly, the tiles fill the workgroups' rounds exactly
+  int32_t stream;
+};
+enum Activation : int32_t { ACT_NONE = 0, ACT_GELU = 1, ACT_SILU = 2 };
+struct CheckpointP {
+  int32_t dt, act;                  // x / y / dy / dx share dt; q is DT_E4M3, the scales float32
+  uint32_t rows, cols;              // blocks of values and their length (K_CHECKPOINT_GRAD_SUMS: rows of `blocks` such blocks)
+  uint32_t blocks;                  // blocks in a row
+  FastDiv div_period;               // store: blocks after which the bias starts over
+  FastDiv div_cols;                 // use: block of an element
+  float inv_max, tiny;              // scale = max * inv_max + tiny
+  int32_t vec;                      // elements per access: a whole vector, or 1 for blocks shorter than one
+  int32_t lanes_per_row, lanes_log2, vecs_per_lane;
+  int32_t waves, unroll;            // K_CHECKPOINT_GRAD_SUMS: workgroup = waves x 64 lanes, a row tile = waves * unroll rows
+  uint32_t n_row_blocks;
   int32_t stream;
 };
 enum RowPattern : int32_t { ROW_SOFTMAX_BWD = 0, ROW_RMSNORM = 1 };
@@ -300,6 +319,7 @@ struct KernelArgs {
     TChainP tchain;
     RowP row;
     LnBwdP lnbwd;
+    CheckpointP checkpoint;
     RowProgP prog;
   } u;
   KernelArgs() { u.binary = BinaryP{}; }

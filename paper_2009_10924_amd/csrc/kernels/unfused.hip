@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include "device_utils.hpp"
+#include "e4m3.hpp"
 #include "kernel_table.hpp"
 
 namespace fsk {
@@ -17,10 +18,12 @@ __device__ __forceinline__ void load_rt(const void* base, int dt, uint32_t off, 
   if constexpr (V == 1) {
     if (dt == DT_F32) v[0] = load1(reinterpret_cast<const float*>(base) + off);
     else if (dt == DT_F16) v[0] = load1(reinterpret_cast<const f16_t*>(base) + off);
+    else if (dt == DT_E4M3) v[0] = load1(reinterpret_cast<const e4m3_t*>(base) + off);
     else v[0] = load1(reinterpret_cast<const bf16_t*>(base) + off);
   } else if constexpr (V == 4) {
     if (dt == DT_F32) load_vec4(reinterpret_cast<const float*>(base) + off, v);
     else if (dt == DT_F16) load_vec4(reinterpret_cast<const f16_t*>(base) + off, v);
+    else if (dt == DT_E4M3) load_vec4(reinterpret_cast<const e4m3_t*>(base) + off, v);
     else load_vec4(reinterpret_cast<const bf16_t*>(base) + off, v);
   } else {
     static_assert(V == 8, "vector width");
@@ -32,6 +35,8 @@ __device__ __forceinline__ void load_rt(const void* base, int dt, uint32_t off, 
       for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
     } else if (dt == DT_F16) {
       load_vec(reinterpret_cast<const f16_t*>(base) + off, v);
+    } else if (dt == DT_E4M3) {
+      load_vec(reinterpret_cast<const e4m3_t*>(base) + off, v);
     } else {
       load_vec(reinterpret_cast<const bf16_t*>(base) + off, v);
     }
@@ -43,10 +48,12 @@ __device__ __forceinline__ void store_rt(void* base, int dt, uint32_t off, const
   if constexpr (V == 1) {
     if (dt == DT_F32) store1(reinterpret_cast<float*>(base) + off, v[0]);
     else if (dt == DT_F16) store1(reinterpret_cast<f16_t*>(base) + off, v[0]);
+    else if (dt == DT_E4M3) store1(reinterpret_cast<e4m3_t*>(base) + off, v[0]);
     else store1(reinterpret_cast<bf16_t*>(base) + off, v[0]);
   } else if constexpr (V == 4) {
     if (dt == DT_F32) store_vec4(reinterpret_cast<float*>(base) + off, v);
     else if (dt == DT_F16) store_vec4(reinterpret_cast<f16_t*>(base) + off, v);
+    else if (dt == DT_E4M3) store_vec4(reinterpret_cast<e4m3_t*>(base) + off, v);
     else store_vec4(reinterpret_cast<bf16_t*>(base) + off, v);
   } else {
     if (dt == DT_F32) {
@@ -57,6 +64,8 @@ __device__ __forceinline__ void store_rt(void* base, int dt, uint32_t off, const
       store_vec(reinterpret_cast<float*>(base) + off + 4, b);
     } else if (dt == DT_F16) {
       store_vec(reinterpret_cast<f16_t*>(base) + off, v);
+    } else if (dt == DT_E4M3) {
+      store_vec(reinterpret_cast<e4m3_t*>(base) + off, v);
     } else {
       store_vec(reinterpret_cast<bf16_t*>(base) + off, v);
     }

@@ -1,0 +1,61 @@
+// Vectors of VEC elements (a whole 128-bit access of the type, or a single element where rows are shorter than one) at any
+// element of a tensor: rows of any length start anywhere, and the memory pipeline takes such accesses as they are.  Loads hand
+// out raw bits, so that many can be under way before the first is widened.
+#pragma once
+#include "e4m3.hpp"
+
+namespace fsk {
+
+template <typename T, int VEC> struct VecIo {
+  static_assert(VEC == Elem<T>::VEC, "a whole vector, or one element");
+  typedef u32x4 Raw;
+  typedef typename AtAlignment<u32x4, sizeof(T)>::type Place;
+  template <bool STREAM> __device__ __forceinline__ static Raw load(const T* p) {
+    const Place* q = reinterpret_cast<const Place*>(p);
+    return STREAM ? __builtin_nontemporal_load(q) : *q;
+  }
+  __device__ __forceinline__ static void widen(Raw r, float (&v)[VEC]) { unpack(r, v, (const T*)nullptr); }
+  __device__ __forceinline__ static void store(T* p, const float (&v)[VEC]) {
+    u32x4 w;
+    if constexpr (sizeof(T) == 4) w = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
+    else w = u32x4{pack2(v[0], v[1], (const T*)nullptr), pack2(v[2], v[3], (const T*)nullptr), pack2(v[4], v[5], (const T*)nullptr),
+                   pack2(v[6], v[7], (const T*)nullptr)};
+    __builtin_nontemporal_store(w, reinterpret_cast<Place*>(p));
+  }
+};
+template <typename T> struct VecIo<T, 1> {
+  typedef float Raw;
+  template <bool STREAM> __device__ __forceinline__ static Raw load(const T* p) { return load1(p); }
+  __device__ __forceinline__ static void widen(Raw r, float (&v)[1]) { v[0] = r; }
+  __device__ __forceinline__ static void store(T* p, const float (&v)[1]) { store1(p, v[0]); }
+};
+template <> struct VecIo<e4m3_t, 8> {
+  typedef u32x2 Raw;
+  typedef AtAlignment<u32x2, 1>::type Place;
+  template <bool STREAM> __device__ __forceinline__ static Raw load(const e4m3_t* p) {
+    const Place* q = reinterpret_cast<const Place*>(p);
+    return STREAM ? __builtin_nontemporal_load(q) : *q;
+  }
+  __device__ __forceinline__ static void widen(Raw r, float (&v)[8]) {
+    unpack_e4m3(r.x, v[0], v[1], v[2], v[3]);
+    unpack_e4m3(r.y, v[4], v[5], v[6], v[7]);
+  }
+  __device__ __forceinline__ static void store(e4m3_t* p, const float (&v)[8]) {
+    const u32x2 w = {pack_e4m3(v[0], v[1], v[2], v[3]), pack_e4m3(v[4], v[5], v[6], v[7])};
+    __builtin_nontemporal_store(w, reinterpret_cast<Place*>(p));
+  }
+};
+template <> struct VecIo<e4m3_t, 4> {
+  typedef uint32_t Raw;
+  typedef AtAlignment<uint32_t, 1>::type Place;
+  template <bool STREAM> __device__ __forceinline__ static Raw load(const e4m3_t* p) {
+    const Place* q = reinterpret_cast<const Place*>(p);
+    return STREAM ? __builtin_nontemporal_load(q) : *q;
+  }
+  __device__ __forceinline__ static void widen(Raw r, float (&v)[4]) { unpack_e4m3(r, v[0], v[1], v[2], v[3]); }
+  __device__ __forceinline__ static void store(e4m3_t* p, const float (&v)[4]) {
+    __builtin_nontemporal_store(pack_e4m3(v[0], v[1], v[2], v[3]), reinterpret_cast<Place*>(p));
+  }
+};
+
+}  // namespace fsk

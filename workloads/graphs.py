@@ -20,8 +20,8 @@ from __future__ import annotations
 from dataclasses import dataclass, field
 from typing import Dict, List, Sequence, Tuple
 
-DTYPES = ("f32", "f16", "bf16", "i32")
-DTYPE_BYTES = {"f32": 4, "f16": 2, "bf16": 2, "i32": 4}
+DTYPES = ("f32", "f16", "bf16", "i32", "e4m3")
+DTYPE_BYTES = {"f32": 4, "f16": 2, "bf16": 2, "i32": 4, "e4m3": 1}
 
 # opcode -> number of tensor operands
 OPCODES = {
@@ -268,6 +268,129 @@ def layernorm_backward_graph(rows: int, cols: int, dtype: str = "f32") -> GraphS
         ops=ops,
         outputs=[("dx", dtype), ("dgamma", "f32"), ("dbeta", "f32")],
     )
+
+
+# ---- group normalisation (channels last) and 8-bit activation checkpoints ----------------------------------------------
+E4M3_MAX = 448.0
+CHECKPOINT_TINY = 1e-30   # added to a block's scale: a block of zeros is divided by it
+
+
+def _act_ops(act: str, z: str, out: str) -> List[OpSpec]:
+    """y = act(z): SiLU (2 ops) or tanh-GELU (1 op)."""
+    if act == "silu":
+        return [_op(out + "_sig", "sigmoid", z), _op(out, "mul", z, out + "_sig")]
+    assert act == "gelu", act
+    return [_op(out, "gelu_tanh", z)]
+
+
+def _act_grad_ops(act: str, z: str, out: str) -> List[OpSpec]:
+    """d act / dz: s (1 + z (1 - s)) with s = sigmoid(z) (6 ops), or the derivative of the tanh-GELU (1 op)."""
+    if act == "silu":
+        return [_op(out + "_sig", "sigmoid", z), _op(out + "_n", "scale", out + "_sig", value=-1.0),
+                _op(out + "_c", "add_scalar", out + "_n", value=1.0), _op(out + "_zc", "mul", z, out + "_c"),
+                _op(out + "_o", "add_scalar", out + "_zc", value=1.0), _op(out, "mul", out + "_sig", out + "_o")]
+    assert act == "gelu", act
+    return [_op(out, "gelu_tanh_grad", z)]
+
+
+def _store_8bit_ops(src: str, axes: Sequence[int]) -> List[OpSpec]:
+    """s = max |src| over the block's axes / 448 + tiny, q = e4m3(src / s)."""
+    ops, last = [_op("q_a", "abs", src)], "q_a"
+    for k, axis in enumerate(axes):
+        ops.append(_op(f"q_m{k}", "reduce_max", last, axis=axis))
+        last = f"q_m{k}"
+    return ops + [_op("q_s0", "scale", last, value=1.0 / E4M3_MAX), _op("s", "add_scalar", "q_s0", value=CHECKPOINT_TINY),
+                  _op("q_d", "div", src, "s"), _op("q", "convert", "q_d", dtype="e4m3")]
+
+
+def group_norm_graph(batch: int, positions: int, groups: int, dim: int, dtype: str = "bf16", act: str = "silu", keep: str = "none",
+                     eps: float = 1e-5) -> GraphSpec:
+    """Group normalisation of [batch, positions, groups, dim] (channels last: channel = group * dim + d) and an activation:
+    mean and population variance over a group's positions and channels, gain and shift per channel.  keep: "stats" hands out
+    mean and reciprocal deviation, "checkpoint" the normalised values in 8 bits with a scale per batch entry and group, and
+    the reciprocal deviation."""
+    ops = [
+        _op("mu_d", "reduce_mean", "x", axis=3), _op("mu", "reduce_mean", "mu_d", axis=1),
+        _op("c", "sub", "x", "mu"), _op("c2", "square", "c"),
+        _op("v_d", "reduce_mean", "c2", axis=3), _op("v", "reduce_mean", "v_d", axis=1),
+        _op("ve", "add_scalar", "v", value=float(eps)), _op("r", "rsqrt", "ve"),
+        _op("n", "mul", "c", "r"), _op("ng", "mul", "n", "gamma"), _op("z", "add", "ng", "beta"),
+    ]
+    out = "z"
+    if act != "none":
+        ops += _act_ops(act, "z", "y")
+        out = "y"
+    outputs = [(out, dtype)]
+    if keep == "checkpoint":
+        ops += _store_8bit_ops("n", (3, 1))
+        outputs += [("q", "e4m3"), ("s", "f32"), ("r", "f32")]
+    elif keep == "stats":
+        outputs += [("mu", "f32"), ("r", "f32")]
+    return GraphSpec(name=f"group_norm_{dtype}_{act}_{keep}_{batch}x{positions}x{groups}x{dim}",
+                     inputs=[TensorSpec("x", dtype, (batch, positions, groups, dim)), TensorSpec("gamma", dtype, (groups, dim)),
+                             TensorSpec("beta", dtype, (groups, dim))],
+                     ops=ops, outputs=outputs)
+
+
+def group_norm_backward_graph(batch: int, positions: int, groups: int, dim: int, dtype: str = "bf16", act: str = "silu",
+                              keep: str = "stats") -> GraphSpec:
+    """Its backward pass, from the input and the statistics (keep = "stats") or from the 8-bit checkpoint: dx, and the sums
+    dgamma and dbeta over batch and positions."""
+    full, per_group, chan = (batch, positions, groups, dim), (batch, 1, groups, 1), (groups, dim)
+    if keep == "checkpoint":
+        inputs = [TensorSpec("q", "e4m3", full), TensorSpec("s", "f32", per_group)]
+        ops = [_op("n", "mul", "q", "s")]
+    else:
+        inputs = [TensorSpec("x", dtype, full), TensorSpec("mu", "f32", per_group)]
+        ops = [_op("c", "sub", "x", "mu"), _op("n", "mul", "c", "r")]
+    inputs += [TensorSpec("dy", dtype, full), TensorSpec("r", "f32", per_group), TensorSpec("gamma", dtype, chan)]
+    dz = "dy"
+    if act != "none":
+        inputs.append(TensorSpec("beta", dtype, chan))
+        ops += [_op("ng", "mul", "n", "gamma"), _op("z", "add", "ng", "beta"), *_act_grad_ops(act, "z", "da"), _op("dz", "mul", "dy", "da")]
+        dz = "dz"
+    ops += [
+        _op("g", "mul", dz, "gamma"), _op("m1_d", "reduce_mean", "g", axis=3), _op("m1", "reduce_mean", "m1_d", axis=1),
+        _op("gn", "mul", "g", "n"), _op("m2_d", "reduce_mean", "gn", axis=3), _op("m2", "reduce_mean", "m2_d", axis=1),
+        _op("t1", "sub", "g", "m1"), _op("t2", "mul", "n", "m2"), _op("t3", "sub", "t1", "t2"), _op("dx", "mul", "t3", "r"),
+        _op("dzn", "mul", dz, "n"), _op("dgamma_s", "reduce_sum", "dzn", axis=1), _op("dgamma", "reduce_sum", "dgamma_s", axis=0),
+        _op("dbeta_s", "reduce_sum", dz, axis=1), _op("dbeta", "reduce_sum", "dbeta_s", axis=0),
+    ]
+    return GraphSpec(name=f"group_norm_backward_{dtype}_{act}_{keep}_{batch}x{positions}x{groups}x{dim}", inputs=inputs, ops=ops,
+                     outputs=[("dx", dtype), ("dgamma", "f32"), ("dbeta", "f32")])
+
+
+def checkpoint_graph(rows: int, blocks: int, block: int, dtype: str = "bf16", act: str = "gelu", bias: bool = True) -> GraphSpec:
+    """An activation put away in 8 bits: z = x (+ bias) in e4m3 with a float32 scale per block of `block` values of a row of
+    `blocks` blocks, next to act(z) where there is an activation."""
+    inputs, ops, z = [TensorSpec("x", dtype, (rows, blocks, block))], [], "x"
+    if bias:
+        inputs.append(TensorSpec("bias", dtype, (blocks, block)))
+        ops.append(_op("z", "add", "x", "bias"))
+        z = "z"
+    outputs = [("q", "e4m3"), ("s", "f32")]
+    if act != "none":
+        ops += _act_ops(act, z, "y")
+        outputs = [("y", dtype)] + outputs
+    return GraphSpec(name=f"checkpoint_{dtype}_{act}_{'bias' if bias else 'plain'}_{rows}x{blocks}x{block}", inputs=inputs,
+                     ops=ops + _store_8bit_ops(z, (2,)), outputs=outputs)
+
+
+def checkpoint_backward_graph(rows: int, blocks: int, block: int, dtype: str = "bf16", act: str = "gelu", dbias: bool = True) -> GraphSpec:
+    """What backward makes of an 8-bit checkpoint: the values themselves (act = "none"), or dx = dy * act'(z) and the bias
+    gradient, dx summed over all rows."""
+    full = (rows, blocks, block)
+    inputs = [TensorSpec("q", "e4m3", full), TensorSpec("s", "f32", (rows, blocks, 1))]
+    ops, outputs = [_op("z", "mul", "q", "s")], [("z", dtype)]
+    if act != "none":
+        inputs.append(TensorSpec("dy", dtype, full))
+        ops += [*_act_grad_ops(act, "z", "da"), _op("dx", "mul", "dy", "da")]
+        outputs = [("dx", dtype)]
+        if dbias:
+            ops.append(_op("dbias", "reduce_sum", "dx", axis=0))
+            outputs.append(("dbias", "f32"))
+    return GraphSpec(name=f"checkpoint_backward_{dtype}_{act}_{'dbias' if dbias else 'plain'}_{rows}x{blocks}x{block}", inputs=inputs, ops=ops,
+                     outputs=outputs)
 
 
 # The five configurations the build is measured on, at their full sizes, and a

@@ -7,7 +7,7 @@ any op of a subgraph.
 
 Storage representation handed to both the oracle and the GPU binding:
   f32 -> numpy float32, f16 -> numpy float16, bf16 -> numpy uint16 bit patterns,
-  i32 -> numpy int32.
+  i32 -> numpy int32, e4m3 -> numpy uint8 bit patterns.
 """
 from __future__ import annotations
 
@@ -18,7 +18,8 @@ import numpy as np
 from .graphs import GraphSpec
 
 CONFIG_INDEX = {"pattern": 11, "rmsnorm": 10, "softmax_backward": 8, "layernorm_backward": 9, "softmax": 1, "add_bias_layernorm": 2, "attention_scores": 3,
-                "bias_gelu_dbias": 4, "transpose_chain": 5, "transpose": 6, "bias_gelu": 7}
+                "bias_gelu_dbias": 4, "transpose_chain": 5, "transpose": 6, "bias_gelu": 7,
+                "group_norm": 12, "group_norm_backward": 13, "checkpoint": 14, "checkpoint_backward": 15}
 
 
 def f64_to_bf16_bits(a: np.ndarray) -> np.ndarray:
@@ -28,6 +29,18 @@ def f64_to_bf16_bits(a: np.ndarray) -> np.ndarray:
     return rounded.astype(np.uint16)
 
 
+def f64_to_e4m3_bits(a: np.ndarray) -> np.ndarray:
+    """Round float64 -> e4m3 (nearest-even, saturating at 448), return uint8 bit patterns."""
+    a = np.ascontiguousarray(a, dtype=np.float64)
+    m = np.minimum(np.abs(a), 448.0)
+    with np.errstate(invalid="ignore"):
+        e = np.maximum(np.frexp(m)[1], -5)                    # m < 2**e; below 2**-6 the spacing stays 2**-9
+        steps = np.rint(np.ldexp(m, 4 - e)).astype(np.int64)  # in units of 2**(e-4); 16 carries into the next exponent
+    bits = np.where(steps >= 8, ((e + 6) << 3) + (steps - 8), steps)   # a step count below 8 occurs only at the lowest exponent
+    bits = np.where(np.isnan(a), 0x7F, bits)
+    return (bits | np.where(np.signbit(a), 0x80, 0)).astype(np.uint8)
+
+
 def quantise(a: np.ndarray, dtype: str) -> np.ndarray:
     if dtype == "f32":
         return np.ascontiguousarray(a, dtype=np.float64).astype(np.float32)
@@ -35,6 +48,8 @@ def quantise(a: np.ndarray, dtype: str) -> np.ndarray:
         return np.ascontiguousarray(a, dtype=np.float64).astype(np.float16)
     if dtype == "bf16":
         return f64_to_bf16_bits(a)
+    if dtype == "e4m3":
+        return f64_to_e4m3_bits(a)
     if dtype == "i32":
         return np.ascontiguousarray(a).astype(np.int32)
     raise ValueError(dtype)
@@ -70,6 +85,8 @@ def make_inputs(graph: GraphSpec, seed: int = 0) -> Dict[str, np.ndarray]:
       softmax_backward   y ~ Dirichlet(1,..,1) per row (positive, rows sum to 1); dy ~ N(0,1)
       rmsnorm            x ~ N(0,1); gamma ~ 1+N(0,0.02)
       layernorm_backward h, dy ~ N(0,1); gamma ~ 1+N(0,0.02); mu ~ N(0,0.05); rstd ~ U(0.8,1.2)
+      group_norm(_backward), checkpoint(_backward)   x ~ N(0.5,1); dy ~ N(0,1); gamma ~ 1+N(0,0.1); beta, bias, mu ~ N(0,0.1);
+                         r ~ U(0.8,1.2); q ~ N(0,112), saturating; s ~ U(0.5,1.5)/112
       pattern (any other pattern or multi-pattern graph) by tensor name (a segment prefix s<k>_ is ignored):
                          g* ~ 1+N(0,0.02); r* ~ U(0.8,1.2); mu* ~ N(0,0.05); bias*, beta* ~ N(0,0.02);
                          mask* 0 / -10000 from per-batch valid length; everything else ~ N(0,1)
@@ -112,6 +129,15 @@ def make_inputs(graph: GraphSpec, seed: int = 0) -> Dict[str, np.ndarray]:
                 a = 0.05 * g.standard_normal(t.dims)
             else:
                 a = g.uniform(0.8, 1.2, t.dims)
+        elif kind in ("group_norm", "group_norm_backward", "checkpoint", "checkpoint_backward"):
+            if n == "r":
+                a = g.uniform(0.8, 1.2, t.dims)
+            elif n == "s":
+                a = g.uniform(0.5, 1.5, t.dims) / 112.0
+            elif n in ("gamma", "beta", "bias", "mu"):
+                a = (1.0 if n == "gamma" else 0.0) + 0.1 * g.standard_normal(t.dims)
+            else:
+                a = {"q": 112.0}.get(n, 1.0) * g.standard_normal(t.dims) + (0.5 if n == "x" else 0.0)
         elif kind == "pattern":
             base = n.split("_", 1)[1] if n[0] == "s" and "_" in n and n[1:n.index("_")].isdigit() else n   # segment prefix s<k>_
             if base.startswith("mask"):
