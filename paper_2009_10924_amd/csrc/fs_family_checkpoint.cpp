@@ -69,12 +69,8 @@ bool is_trailing(const Tensor& v, const Tensor& full) {
 }
 
 namespace {
-bool is_float(int32_t dt) { return dt == FS_F32 || dt == FS_F16 || dt == FS_BF16; }
 // blocks of `cols` values: how many values a lane accesses at once
 int access_of(int32_t dt, uint32_t cols) { return cols >= (uint32_t)vec_of(dt) ? vec_of(dt) : 1; }
-const char* act_name(int32_t act) { return act == ACT_GELU ? "gelu" : act == ACT_SILU ? "silu" : "none"; }
-double act_valu(int32_t act) { return act == ACT_GELU ? 8.0 : act == ACT_SILU ? 4.0 : 0.0; }
-double act_trans(int32_t act) { return act == ACT_NONE ? 0.0 : 2.0; }
 }  // namespace
 
 // ------------------------------------------------------------------ store
@@ -110,7 +106,7 @@ bool build_checkpoint(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
   p.tiny = (float)st.scalars[81];
   p.stream = streams_inputs(g) ? 1 : 0;
   p.vec = access_of(p.dt, p.cols);
-  if (!is_float(p.dt) || !same_dims(x, g.tensors[tz])) return true;
+  if (!is_float_dtype(p.dt) || !same_dims(x, g.tensors[tz])) return true;
   if (t_y >= 0 && g.tensors[t_y].store_as != p.dt) return true;
   uint32_t period = 1;
   if (tb >= 0) {
@@ -288,7 +284,7 @@ bool build_checkpoint_backward(const fs_graph& g, std::vector<Candidate>* out, P
   p.stream = streams_inputs(g) ? 1 : 0;
   p.vec = access_of(p.dt, p.cols);
   // one scale per block of the last axis
-  if (!is_float(p.dt) || s.dtype != FS_F32 || s.rank != q.rank || s.dims[s.rank - 1] != 1 || s.numel() != (int64_t)p.rows) return true;
+  if (!is_float_dtype(p.dt) || s.dtype != FS_F32 || s.rank != q.rank || s.dims[s.rank - 1] != 1 || s.numel() != (int64_t)p.rows) return true;
   if (tdy >= 0 && (!same_dims(g.tensors[tdy], q) || g.tensors[tdy].dtype != p.dt)) return true;
   const int esz = dtype_bytes(p.dt);
   const double n = (double)p.rows * p.cols;

@@ -1,0 +1,505 @@
+// Pattern families: group normalisation with an activation (channels last), forward and backward.
+#include "fs_stitch_util.hpp"
+
+namespace fs {
+
+namespace {
+
+constexpr int64_t kAlign = 256;
+int64_t aligned(int64_t bytes) { return (bytes + kAlign - 1) / kAlign * kAlign; }
+
+// mean (or maximum) over a group's positions and channels: axes 1 and 3 of [batch, positions, groups, dim], in either order
+bool match_over_group(const fs_graph& g, const char* op, const std::string& inner, int32_t t, MatchState* st) {
+  for (const char* axes : {"[-3]|[-1]", "[-1]|[-3]"}) {
+    const std::string a(axes, 4), b(axes + 5, 4);
+    if (Pattern(std::string(op) + a + "(" + op + b + "(" + inner + "))").match(g, t, st)) return true;
+  }
+  return false;
+}
+
+bool per_group(const Tensor& t, const Tensor& x) {
+  return t.rank == 4 && t.dims[0] == x.dims[0] && t.dims[1] == 1 && t.dims[2] == x.dims[2] && t.dims[3] == 1 && t.dtype == FS_F32;
+}
+bool per_channel(const Tensor& t, const Tensor& x) { return t.numel() == x.dims[2] * x.dims[3] && is_trailing(t, x) && t.dtype == x.dtype; }
+
+bool shape_of(const Tensor& x, GroupNormP* p) {
+  p->batch = (uint32_t)x.dims[0];
+  p->positions = (uint32_t)x.dims[1];
+  p->groups = (uint32_t)x.dims[2];
+  p->dim = (uint32_t)x.dims[3];
+  p->channels = p->groups * p->dim;
+  p->div_dim = make_fastdiv(p->dim);
+  p->inv_count = (float)(1.0 / ((double)p->positions * p->dim));
+  return p->div_dim.d != 0;
+}
+
+// A workgroup of `threads` on sets of `set_groups` groups; false: a position of a set has more vectors than threads, or a
+// constant that the kernels need does not exist.
+bool lay_out(GroupNormP* p, int threads, uint32_t set_groups) {
+  const uint32_t width = set_groups * p->dim;
+  p->threads = threads;
+  p->set_groups = set_groups;
+  p->sets = p->groups / set_groups;
+  p->vec = width >= (uint32_t)vec_of(p->dt) ? vec_of(p->dt) : 1;
+  p->whole = p->dim % p->vec == 0 ? 1 : 0;
+  p->set_vecs = (width + p->vec - 1) / p->vec;
+  if (p->set_vecs > (uint32_t)threads) return false;
+  p->rows_at_once = (uint32_t)threads / p->set_vecs;
+  p->set_vecs_m = ((1u << 20) + p->set_vecs - 1) / p->set_vecs;
+  p->div_per = make_fastdiv(p->whole ? p->dim / p->vec : p->dim);
+  p->div_sets = make_fastdiv(p->sets);
+  p->div_chunks = make_fastdiv(1);
+  p->chunks = 1;
+  p->chunk_rows = p->positions;
+  return p->div_per.d != 0 && p->div_sets.d != 0;
+}
+int pow2_at_most_log2(uint32_t v) {
+  int l = 0;
+  while ((2u << l) <= v) ++l;
+  return l;
+}
+// lanes that fold `each` of n sums of `items` values: all threads busy, at most a wavefront, no more lanes than items
+int fold_lanes_log2(uint32_t threads, uint32_t n, uint32_t items) {
+  return std::min({pow2_at_most_log2(std::max<uint32_t>(1, threads / std::max<uint32_t>(1, n))), 6, log2_of(pow2_at_least(items))});
+}
+// Chunks of positions for launches of 256 threads: about `want` workgroups in all, each with whole rounds of four positions
+// per thread where there are that many.
+bool cut(GroupNormP* p, uint32_t want) {
+  const uint32_t round = 4 * p->rows_at_once;
+  const uint32_t most = std::max<uint32_t>(1, want / (p->batch * p->sets));
+  uint32_t rows = (p->positions + most - 1) / most;
+  rows = std::min(p->positions, (rows + round - 1) / round * round);
+  p->chunk_rows = rows;
+  p->chunks = (p->positions + rows - 1) / rows;
+  p->div_chunks = make_fastdiv(p->chunks);
+  return p->div_chunks.d != 0 && (uint64_t)p->batch * p->chunks * p->sets < (1ull << 31);
+}
+// sets of 1 group, of more by twos, of all
+std::vector<uint32_t> set_sizes(uint32_t groups) {
+  std::vector<uint32_t> s;
+  for (uint32_t k = 1; k < groups; k *= 2)
+    if (groups % k == 0) s.push_back(k);
+  s.push_back(groups);
+  return s;
+}
+// the largest set of groups whose positions 256 threads cover; 0: none
+uint32_t widest_set(const GroupNormP& p) {
+  for (uint32_t s = p.groups; s >= 1; --s) {
+    GroupNormP q = p;
+    if (p.groups % s == 0 && lay_out(&q, 256, s)) return s;
+  }
+  return 0;
+}
+
+struct Traffic {
+  double read_bytes = 0, written_bytes = 0, n = 0, valu = 0, trans = 0;
+};
+// What a set's rows cost beyond their bytes: pieces shorter than a line are read by several workgroups.
+void slab_cost(const GroupNormP& p, const Traffic& t, int esz, int K, int raw_bytes, int lds, KernelCost* kc) {
+  kc->hbm_bytes = t.read_bytes + t.written_bytes;
+  kc->elems = t.n;
+  kc->valu_per_elem = t.valu;
+  kc->trans_per_elem = t.trans;
+  kc->waves_per_block = p.threads / 64;
+  kc->waves = (double)p.batch * p.sets * kc->waves_per_block;
+  kc->bytes_in_flight_per_lane = (double)raw_bytes * K;
+  kc->vgpr_estimate = 48 + K * (raw_bytes / 4 + 2);
+  kc->xlane_steps = 16;
+  kc->barriers = 4;
+  kc->lds_bytes_per_block = lds;
+  kc->lane_utilisation = (double)p.positions * p.set_vecs / ((double)K * p.threads);
+  const double run = (double)p.set_groups * p.dim * esz;
+  if (p.sets > 1 && run < 256) kc->stream_penalty = 0.25 * (256.0 / run - 1.0);
+}
+void passes_cost(const GroupNormP& p, const Traffic& t, int raw_bytes, int n_launches, KernelCost* kc) {
+  const double again = t.read_bytes <= 0.75 * device().last_level_cache_bytes ? device().last_level_reread : 1.0;
+  kc->hbm_bytes = t.read_bytes * (1.0 + again) + t.written_bytes;
+  kc->elems = t.n * 1.6;
+  kc->valu_per_elem = t.valu;
+  kc->trans_per_elem = t.trans;
+  kc->waves_per_block = 4;
+  kc->waves = (double)p.batch * p.sets * p.chunks * 4;
+  kc->rows_per_wave_loop = std::max(1.0, (double)p.chunk_rows / (4.0 * p.rows_at_once));
+  kc->bytes_in_flight_per_lane = 4.0 * raw_bytes;
+  kc->vgpr_estimate = 96;
+  kc->barriers = 0;
+  kc->dep_phases = 0.3;
+  kc->first_load = true;
+  kc->serial_tail_s = (n_launches - 1) * 3.0e-6;
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------ forward
+bool build_group_norm(const fs_graph& g, std::vector<Candidate>* out, PackForm*) {
+  if (g.outputs.empty() || g.outputs.size() > 5 || g.inputs.size() != 3 || g.tensors[g.inputs[0]].rank > 4) return false;
+  MatchState st;
+  int32_t t_q = -1, t_s = -1, t_y = -1, act = ACT_NONE;
+  bool has_8bit = false;
+  for (int32_t t : g.outputs) has_8bit = has_8bit || g.tensors[t].store_as == FS_E4M3;
+  if (has_8bit && !match_8bit(g, "rmax[-3](rmax[-1](abs($V)))", &st, &t_q, &t_s) && !match_8bit(g, "rmax[-1](rmax[-3](abs($V)))", &st, &t_q, &t_s))
+    return false;
+  for (int32_t t : g.outputs)
+    if (t != t_q && (t_y < 0 || g.tensors[t].numel() > g.tensors[t_y].numel())) t_y = t;
+  if (t_y < 0 || g.tensors[t_y].rank != 4) return false;
+  MatchState with_act = st;
+  if (match_activation(g, t_y, &with_act, &act)) st = with_act;
+  else st.tensors["Z"] = t_y;
+  const char* affine = "add(mul(mul(sub($X,$MU),rsqrt(addc[#0]($VAR))),$G),$B)";
+  if (!Pattern(affine).match(g, st.tensors["Z"], &st)) return false;
+  // (the same ops once more, to know the normalised values' tensor)
+  if (!Pattern("add(mul($N,$G),$B)").match(g, st.tensors["Z"], &st) || !Pattern("mul($C,rsqrt(addc[#0]($VAR)))").match(g, st.tensors["N"], &st)) return false;
+  if (has_8bit && st.tensors["V"] != st.tensors["N"]) return false;
+  if (!match_over_group(g, "rmean", "square($C)", st.tensors["VAR"], &st) || !match_over_group(g, "rmean", "$X", st.tensors["MU"], &st)) return false;
+  if (!covers_all(g, st)) return false;
+  const int32_t tx = st.tensors["X"], tg = st.tensors["G"], tb = st.tensors["B"];
+  for (int32_t t : {tx, tg, tb})
+    if (!is_input(g, t)) return false;
+  int32_t t_mu = -1, t_r = -1;
+  for (int32_t t : g.outputs) {
+    if (t == t_y || t == t_q || t == t_s) continue;
+    if (g.tensors[t].store_as != FS_F32) return true;
+    const int32_t opcode = g.ops[g.tensors[t].producer].opcode;
+    if (t == st.tensors["MU"]) t_mu = t;
+    else if (opcode == FS_RSQRT) t_r = t;
+    else return true;
+  }
+  const Tensor& x = g.tensors[tx];
+  GroupNormP base{};
+  base.dt = x.dtype;
+  base.act = act;
+  base.checkpoint = has_8bit ? 1 : 0;
+  if (x.rank != 4 || !is_float_dtype(x.dtype) || !same_dims(x, g.tensors[t_y]) || g.tensors[t_y].store_as != x.dtype ||
+      !per_channel(g.tensors[tg], x) || !per_channel(g.tensors[tb], x) || !shape_of(x, &base))
+    return true;
+  base.eps = (float)st.scalars[0];
+  if (has_8bit) {
+    base.inv_max = (float)st.scalars[80];
+    base.tiny = (float)st.scalars[81];
+  }
+  const int esz = dtype_bytes(base.dt);
+  Traffic t;
+  t.n = (double)x.numel();
+  t.read_bytes = t.n * esz;
+  t.written_bytes = t.n * (esz + (has_8bit ? 1 : 0));
+  t.valu = 9.0 + act_valu(act) + (has_8bit ? 10.0 : 0.0) + (esz == 2 ? 1.5 : 0.0);
+  t.trans = act_trans(act);
+
+  // ---- one launch
+  struct Slab { int threads, K; };
+  for (uint32_t gs : set_sizes(base.groups)) {
+    for (Slab sh : {Slab{256, 1}, Slab{256, 2}, Slab{256, 4}, Slab{256, 8}, Slab{512, 4}, Slab{512, 8}, Slab{512, 16}, Slab{512, 32}}) {
+      GroupNormP p = base;
+      if (!lay_out(&p, sh.threads, gs)) continue;
+      const uint64_t held = (uint64_t)sh.K * p.rows_at_once;
+      if (held < p.positions || (sh.K > 1 && held >= 2ull * p.positions + p.rows_at_once)) continue;
+      if (held * p.channels * esz >= (1ull << 32)) continue;   // the kernel's distances within a batch entry
+      const uint32_t items = p.rows_at_once * (p.whole ? p.set_vecs : gs * p.dim);
+      p.vecs_per_lane = sh.K;
+      p.fold_log2 = fold_lanes_log2(sh.threads, gs, p.rows_at_once * (p.whole ? p.dim / p.vec : p.dim));
+      const int64_t lds = 4ll * ((has_8bit ? 2 : 1) * (int64_t)items + 3 * gs);
+      if (lds > 64 * 1024 || (uint64_t)p.batch * p.sets >= (1ull << 31)) continue;
+      Candidate c = make_candidate(g, "group_norm", FS_SCHEME_LDS, K_GN_SLAB);
+      Launch& l = c.launches.front();
+      l.args.u.gn = p;
+      l.ptr[0] = in_ref(g, tx);
+      l.ptr[1] = in_ref(g, tg);
+      l.ptr[2] = in_ref(g, tb);
+      l.ptr[3] = out_ref(g.tensors[t_y].output_slot);
+      if (t_mu >= 0) l.ptr[4] = out_ref(g.tensors[t_mu].output_slot);
+      if (t_r >= 0) l.ptr[5] = out_ref(g.tensors[t_r].output_slot);
+      if (t_q >= 0) { l.ptr[6] = out_ref(g.tensors[t_q].output_slot); l.ptr[7] = out_ref(g.tensors[t_s].output_slot); }
+      l.shape.block[0] = (uint32_t)sh.threads;
+      l.shape.grid[0] = p.batch * p.sets;
+      l.shape.lds_bytes = (uint32_t)lds;
+      c.info.lanes_per_row = (int32_t)p.set_vecs;
+      c.info.vecs_per_lane = sh.K;
+      c.info.rows_per_block = (int32_t)p.rows_at_once;
+      c.info.lds_bytes = (int32_t)lds;
+      KernelCost kc;
+      slab_cost(p, t, esz, sh.K, p.vec * esz, (int)lds, &kc);
+      char var[56];
+      snprintf(var, sizeof var, "<%s,%s,T%d,K%d,G%u>", dtype_name(p.dt), act_name(act), sh.threads, sh.K, gs);
+      finish_candidate(&c, var, kc);
+      out->push_back(c);
+    }
+  }
+
+  // ---- three launches
+  const uint32_t gs = widest_set(base);
+  if (gs == 0) return true;
+  for (uint32_t want : {1024u, 2048u}) {
+    GroupNormP p = base;
+    if (!lay_out(&p, 256, gs) || !cut(&p, want)) continue;
+    const uint32_t items = p.rows_at_once * (p.whole ? p.set_vecs : gs * p.dim);
+    p.fold_log2 = fold_lanes_log2(256, gs, p.rows_at_once * (p.whole ? p.dim / p.vec : p.dim));
+    const int64_t lds = 4ll * ((has_8bit ? 4 : 2) * (int64_t)items + p.rows_at_once);
+    const int64_t chunk_bytes = aligned(16ll * p.batch * p.chunks * p.groups);
+    Candidate c = make_candidate(g, "group_norm", FS_SCHEME_GLOBAL, K_GN_STATS);
+    {
+      Launch& l = c.launches.front();
+      l.args.u.gn = p;
+      l.ptr[0] = in_ref(g, tx);
+      l.ptr[1] = ws_ref(0);
+      l.shape.block[0] = 256;
+      l.shape.grid[0] = p.batch * p.chunks * p.sets;
+      l.shape.lds_bytes = (uint32_t)lds;
+    }
+    {
+      c.launches.emplace_back();
+      Launch& l = c.launches.back();
+      l.kernel = K_GN_JOIN;
+      l.args.u.gn = p;
+      l.args.u.gn.fold_log2 = std::min(6, log2_of(pow2_at_least(p.chunks)));
+      l.ptr[0] = ws_ref(0);
+      l.ptr[1] = ws_ref(chunk_bytes);
+      if (t_mu >= 0) l.ptr[2] = out_ref(g.tensors[t_mu].output_slot);
+      if (t_r >= 0) l.ptr[3] = out_ref(g.tensors[t_r].output_slot);
+      if (t_s >= 0) l.ptr[4] = out_ref(g.tensors[t_s].output_slot);
+      const uint32_t at_once = 256u >> l.args.u.gn.fold_log2;
+      l.shape.block[0] = 256;
+      l.shape.grid[0] = (p.batch * p.groups + at_once - 1) / at_once;
+    }
+    {
+      c.launches.emplace_back();
+      Launch& l = c.launches.back();
+      l.kernel = K_GN_APPLY;
+      l.args.u.gn = p;
+      l.ptr[0] = in_ref(g, tx);
+      l.ptr[1] = in_ref(g, tg);
+      l.ptr[2] = in_ref(g, tb);
+      l.ptr[3] = ws_ref(chunk_bytes);
+      l.ptr[4] = out_ref(g.tensors[t_y].output_slot);
+      if (t_q >= 0) l.ptr[5] = out_ref(g.tensors[t_q].output_slot);
+      l.shape.block[0] = 256;
+      l.shape.grid[0] = p.batch * p.chunks * p.sets;
+    }
+    c.info.n_kernels = 3;
+    c.info.workspace_bytes = chunk_bytes + aligned(16ll * p.batch * p.groups);
+    c.info.bytes_moved_model = c.info.bytes_min + (int64_t)t.read_bytes;
+    c.info.lanes_per_row = (int32_t)p.set_vecs;
+    c.info.vecs_per_lane = 4;
+    c.info.rows_per_block = (int32_t)p.chunk_rows;
+    c.info.lds_bytes = (int32_t)lds;
+    KernelCost kc;
+    passes_cost(p, t, p.vec * esz, 3, &kc);
+    char var[56];
+    snprintf(var, sizeof var, "<%s,%s,G%u,C%u,apply>", dtype_name(p.dt), act_name(act), gs, p.chunks);
+    finish_candidate(&c, var, kc);
+    out->push_back(c);
+  }
+  return true;
+}
+
+// ------------------------------------------------------------------ backward
+bool build_group_norm_backward(const fs_graph& g, std::vector<Candidate>* out, PackForm*) {
+  if (g.outputs.size() != 3) return false;
+  // two sums over batch and positions, and dx
+  int32_t t_dx = -1, t_sum[2] = {-1, -1}, of[2] = {-1, -1};
+  std::set<int32_t> sum_ops;
+  int n_sums = 0;
+  for (int32_t t : g.outputs) {
+    if (g.tensors[t].rank != 4) return false;
+    const Op& op = g.ops[g.tensors[t].producer];
+    if (op.opcode != FS_REDUCE_SUM) {
+      if (t_dx >= 0) return false;
+      t_dx = t;
+      continue;
+    }
+    const Tensor& inner = g.tensors[op.in[0]];
+    if (n_sums == 2 || inner.producer < 0 || inner.output_slot >= 0) return false;
+    const Op& first = g.ops[inner.producer];
+    if (first.opcode != FS_REDUCE_SUM || first.axis + op.axis != 1) return false;   // axes 0 and 1
+    sum_ops.insert(g.tensors[t].producer);
+    sum_ops.insert(inner.producer);
+    t_sum[n_sums] = t;
+    of[n_sums++] = first.in[0];
+  }
+  if (n_sums != 2 || t_dx < 0) return false;
+  MatchState st;
+  int32_t t_dbeta = -1, t_dgamma = -1;
+  for (int k = 0; k < 2 && t_dbeta < 0; ++k) {   // dbeta sums DZ, dgamma DZ times the normalised values
+    MatchState trial;
+    trial.tensors["DZ"] = of[k];
+    if (!Pattern("mul($DZ,$N)").match(g, of[1 - k], &trial)) continue;
+    if (!Pattern("mul(sub(sub($GG,$M1),mul($N,$M2)),$R)").match(g, t_dx, &trial)) continue;
+    if (!Pattern("mul($DZ,$G)").match(g, trial.tensors["GG"], &trial)) continue;
+    if (!match_over_group(g, "rmean", "$GG", trial.tensors["M1"], &trial) || !match_over_group(g, "rmean", "mul($GG,$N)", trial.tensors["M2"], &trial)) continue;
+    st = trial;
+    t_dbeta = t_sum[k];
+    t_dgamma = t_sum[1 - k];
+  }
+  if (t_dbeta < 0) return false;
+  GroupNormP base{};
+  base.act = ACT_NONE;
+  const int32_t tdz = st.tensors["DZ"], tn = st.tensors["N"];
+  int32_t tdy = tdz, tb = -1;
+  if (!is_input(g, tdz)) {
+    if (!match_activation_gradient(g, tdz, &st, &base.act)) return false;
+    tdy = st.tensors["DY"];
+    if (!Pattern("add(mul($N,$G),$B)").match(g, st.tensors["Z"], &st)) return false;
+    tb = st.tensors["B"];
+    if (!is_input(g, tb)) return false;
+  }
+  int32_t tx, tcentre;
+  if (Pattern("mul(sub($X,$MU),$R)").match(g, tn, &st)) {
+    tx = st.tensors["X"];
+    tcentre = st.tensors["MU"];
+  } else {
+    if (!Pattern("mul($Q,$S)").match(g, tn, &st)) return false;
+    tx = st.tensors["Q"];
+    tcentre = st.tensors["S"];
+    if (!is_input(g, tx) || !is_input(g, tcentre)) return false;
+    if (g.tensors[tx].dtype != FS_E4M3) std::swap(tx, tcentre);
+    if (g.tensors[tx].dtype != FS_E4M3) return false;
+    base.checkpoint = 1;
+  }
+  for (int32_t op : sum_ops) st.covered.insert(op);
+  if (!covers_all(g, st)) return false;
+  const int32_t tr = st.tensors["R"], tg = st.tensors["G"];
+  for (int32_t t : {tx, tcentre, tr, tg, tdy})
+    if (!is_input(g, t)) return false;
+  const Tensor& dy = g.tensors[tdy];
+  base.dt = dy.dtype;
+  const Tensor& x = g.tensors[tx];
+  if (dy.rank != 4 || !is_float_dtype(dy.dtype) || !same_dims(x, dy) || (!base.checkpoint && x.dtype != dy.dtype) || !same_dims(g.tensors[t_dx], dy) ||
+      g.tensors[t_dx].store_as != dy.dtype || g.tensors[t_dbeta].store_as != FS_F32 || g.tensors[t_dgamma].store_as != FS_F32 ||
+      !per_group(g.tensors[tcentre], dy) || !per_group(g.tensors[tr], dy) || !per_channel(g.tensors[tg], dy) || (tb >= 0 && !per_channel(g.tensors[tb], dy)) ||
+      !shape_of(dy, &base))
+    return true;
+  const int esz = dtype_bytes(base.dt), xsz = base.checkpoint ? 1 : esz;
+  const uint32_t pitch = colsum_pitch(base.channels);
+  Traffic t;
+  t.n = (double)dy.numel();
+  t.read_bytes = t.n * (esz + xsz);
+  t.written_bytes = t.n * esz;
+  t.valu = 18.0 + 2.5 * act_valu(base.act) + (esz == 2 ? 2.0 : 0.0);
+  t.trans = 2.0 * act_trans(base.act);
+  auto fill_inputs = [&](Launch& l) {
+    l.ptr[0] = in_ref(g, tx);
+    l.ptr[1] = in_ref(g, tcentre);
+    l.ptr[2] = in_ref(g, tr);
+    l.ptr[3] = in_ref(g, tg);
+    if (tb >= 0) l.ptr[4] = in_ref(g, tb);
+    l.ptr[5] = in_ref(g, tdy);
+  };
+  // the batch entries' sums added up: dbeta from the first half of each row, dgamma from the second
+  auto add_fold = [&](Candidate* c, int64_t at) {
+    c->launches.emplace_back();
+    Launch& f = c->launches.back();
+    make_fold_launch(&f, base.batch, 2 * pitch, pitch, base.channels);
+    f.ptr[0] = ws_ref(at);
+    f.ptr[1] = out_ref(g.tensors[t_dbeta].output_slot);
+    f.ptr[2] = out_ref(g.tensors[t_dgamma].output_slot);
+  };
+  const int64_t sum_bytes = aligned(8ll * base.batch * pitch);
+
+  // ---- one launch and the fold
+  struct Slab { int threads, K; };
+  for (uint32_t gs : set_sizes(base.groups)) {
+    for (Slab sh : {Slab{256, 1}, Slab{256, 2}, Slab{256, 4}, Slab{512, 4}, Slab{512, 8}, Slab{512, 16}}) {
+      GroupNormP p = base;
+      if (!lay_out(&p, sh.threads, gs)) continue;
+      const uint64_t held = (uint64_t)sh.K * p.rows_at_once;
+      if (held < p.positions || (sh.K > 1 && held >= 2ull * p.positions + p.rows_at_once)) continue;
+      if (held * p.channels * esz >= (1ull << 32)) continue;
+      const uint32_t width = gs * p.dim;
+      p.vecs_per_lane = sh.K;
+      p.fold_log2 = fold_lanes_log2(sh.threads, width, p.rows_at_once);
+      const int64_t lds = 4ll * ((int64_t)p.rows_at_once * width + 2 * width + 2 * gs);
+      if (lds > 64 * 1024 || (uint64_t)p.batch * p.sets >= (1ull << 31)) continue;
+      Candidate c = make_candidate(g, "group_norm_backward", FS_SCHEME_LDS, K_GN_BWD_SLAB);
+      Launch& l = c.launches.front();
+      l.args.u.gn = p;
+      fill_inputs(l);
+      l.ptr[6] = out_ref(g.tensors[t_dx].output_slot);
+      l.ptr[7] = ws_ref(0);
+      l.shape.block[0] = (uint32_t)sh.threads;
+      l.shape.grid[0] = p.batch * p.sets;
+      l.shape.lds_bytes = (uint32_t)lds;
+      KernelCost kc;
+      slab_cost(p, t, esz, sh.K, p.vec * (esz + xsz), (int)lds, &kc);
+      kc.serial_tail_s = 2.0e-6;
+      char var[56];
+      snprintf(var, sizeof var, "<%s,%s,T%d,K%d,G%u,fold>", dtype_name(p.dt), act_name(p.act), sh.threads, sh.K, gs);
+      finish_candidate(&c, var, kc);
+      add_fold(&c, 0);
+      c.info.n_kernels = 2;
+      c.info.workspace_bytes = sum_bytes;
+      c.info.bytes_moved_model = c.info.bytes_min + 2 * sum_bytes;
+      c.info.lanes_per_row = (int32_t)p.set_vecs;
+      c.info.vecs_per_lane = sh.K;
+      c.info.rows_per_block = (int32_t)p.rows_at_once;
+      c.info.lds_bytes = (int32_t)lds;
+      out->push_back(c);
+    }
+  }
+
+  // ---- three launches and the fold
+  const uint32_t gs = widest_set(base);
+  if (gs == 0) return true;
+  for (uint32_t want : {1024u, 2048u}) {
+    GroupNormP p = base;
+    if (!lay_out(&p, 256, gs) || !cut(&p, want)) continue;
+    const uint32_t width = gs * p.dim;
+    p.fold_log2 = fold_lanes_log2(256, width, p.rows_at_once);
+    const int64_t lds = 4ll * ((int64_t)p.rows_at_once * width + width);
+    const int64_t chunk_bytes = aligned(8ll * p.batch * p.chunks * p.channels);
+    Candidate c = make_candidate(g, "group_norm_backward", FS_SCHEME_GLOBAL, K_GN_BWD_SUMS);
+    {
+      Launch& l = c.launches.front();
+      l.args.u.gn = p;
+      fill_inputs(l);
+      l.ptr[6] = ws_ref(0);
+      l.shape.block[0] = 256;
+      l.shape.grid[0] = p.batch * p.chunks * p.sets;
+      l.shape.lds_bytes = (uint32_t)lds;
+    }
+    {
+      c.launches.emplace_back();
+      Launch& l = c.launches.back();
+      l.kernel = K_GN_BWD_JOIN;
+      GroupNormP& q = l.args.u.gn;
+      q = p;
+      const uint32_t at_once = p.chunks <= 32 ? 64 : 16;   // channels side by side, the rest of the threads along the chunks
+      q.fold_log2 = log2_of(256 / at_once);
+      q.join_cols = p.dim * std::max<uint32_t>(1, at_once / p.dim);
+      l.ptr[0] = ws_ref(0);
+      l.ptr[1] = in_ref(g, tg);
+      l.ptr[2] = ws_ref(chunk_bytes);
+      l.ptr[3] = ws_ref(chunk_bytes + sum_bytes);
+      l.shape.block[0] = 256;
+      l.shape.grid[0] = p.batch * ((p.channels + q.join_cols - 1) / q.join_cols);
+      l.shape.lds_bytes = 8 * q.join_cols;
+      if (l.shape.lds_bytes > 60 * 1024) continue;
+    }
+    {
+      c.launches.emplace_back();
+      Launch& l = c.launches.back();
+      l.kernel = K_GN_BWD_APPLY;
+      l.args.u.gn = p;
+      fill_inputs(l);
+      l.ptr[6] = out_ref(g.tensors[t_dx].output_slot);
+      l.ptr[7] = ws_ref(chunk_bytes + sum_bytes);
+      l.shape.block[0] = 256;
+      l.shape.grid[0] = p.batch * p.chunks * p.sets;
+    }
+    add_fold(&c, chunk_bytes);
+    c.info.n_kernels = 4;
+    c.info.workspace_bytes = chunk_bytes + sum_bytes + aligned(8ll * p.batch * p.groups);
+    c.info.bytes_moved_model = c.info.bytes_min + (int64_t)t.read_bytes + 2 * chunk_bytes;
+    c.info.lanes_per_row = (int32_t)p.set_vecs;
+    c.info.vecs_per_lane = 4;
+    c.info.rows_per_block = (int32_t)p.chunk_rows;
+    c.info.lds_bytes = (int32_t)lds;
+    KernelCost kc;
+    passes_cost(p, t, p.vec * (esz + xsz), 4, &kc);
+    char var[56];
+    snprintf(var, sizeof var, "<%s,%s,G%u,C%u,apply,fold>", dtype_name(p.dt), act_name(p.act), gs, p.chunks);
+    finish_candidate(&c, var, kc);
+    out->push_back(c);
+  }
+  return true;
+}
+
+}  // namespace fs

@@ -32,6 +32,7 @@ std::string build_stitched(const fs_graph& g, std::vector<Candidate>* out, PackF
       {"softmax", build_softmax, false}, {"layernorm", build_layernorm, false}, {"bias_gelu", build_gelu, false},
       {"transpose_chain", build_tchain, false}, {"softmax_backward", build_softmax_backward, false}, {"rmsnorm", build_rmsnorm, false},
       {"layernorm_backward", build_layernorm_backward, false}, {"transpose", build_transpose, false},
+      {"group_norm", build_group_norm, true}, {"group_norm_backward", build_group_norm_backward, true},
       {"checkpoint", build_checkpoint, true}, {"checkpoint_backward", build_checkpoint_backward, true},
   };
   const bool has_8bit = holds_8bit(g);

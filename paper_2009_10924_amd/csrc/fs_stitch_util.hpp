@@ -101,8 +101,21 @@ bool build_tchain(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack
 bool build_transpose(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
 bool build_softmax_backward(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
 bool build_rmsnorm(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
+bool build_group_norm(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
+bool build_group_norm_backward(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
 bool build_checkpoint(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
 bool build_checkpoint_backward(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
+// What the checkpoint and group normalisation families match in common (fs_family_checkpoint.cpp): an activation of $Z; $DY times
+// the slope of one at $Z; the 8-bit output that is $V over its scale, and that scale, `maximum` being the pattern of the largest
+// |$V|.  On success the bindings are merged into *st.
+bool match_activation(const fs_graph& g, int32_t t, MatchState* st, int32_t* act);
+bool match_activation_gradient(const fs_graph& g, int32_t t, MatchState* st, int32_t* act);
+bool match_8bit(const fs_graph& g, const char* maximum, MatchState* st, int32_t* t_q, int32_t* t_s);
+bool is_trailing(const Tensor& v, const Tensor& full);
+inline bool is_float_dtype(int32_t dt) { return dt == FS_F32 || dt == FS_F16 || dt == FS_BF16; }
+inline const char* act_name(int32_t act) { return act == ACT_GELU ? "gelu" : act == ACT_SILU ? "silu" : "none"; }
+inline double act_valu(int32_t act) { return act == ACT_GELU ? 8.0 : act == ACT_SILU ? 4.0 : 0.0; }   // per element
+inline double act_trans(int32_t act) { return act == ACT_NONE ? 0.0 : 2.0; }
 // The launch that folds [n_rows, width] float32 column partials (second step of a global hand-off).
 // K_COLFOLD over partial rows of `width` floats (`stride` floats apart, 0 = width): columns below `split` go to the
 // launch's first output, the rest to its second.

@@ -1,0 +1,432 @@
+// Group normalisation with an activation:  z = (x - mean) rstd gamma + beta,  y = act(z), mean and variance over the positions
+// and channels of a group; beside it the 8-bit checkpoint of (x - mean) rstd.
+//
+// A group's values are read once where a workgroup can hold them (k_gn_slab).  Otherwise a first launch gathers mean and
+// sum of squared deviations per chunk of positions, a second joins the chunks, a third reads x again.  No variance is a
+// difference of large sums: inside registers it is the mean of squared deviations from the known mean, and partial results
+// join as M2 = M2a + M2b + (mean_b - mean_a)^2 na nb / (na + nb).
+#include <hip/hip_runtime.h>
+
+#include "group_norm.hpp"
+#include "kernel_table.hpp"
+
+namespace fsk {
+using namespace fs;
+
+// ---- one launch: the set's values stay in registers ----------------------------------------------------------------------
+template <typename T, int VEC, int K, bool WHOLE, int ACT, int NT>
+__global__ void __launch_bounds__(NT) k_gn_slab(const T* x, const T* gamma, const T* beta, T* y, float* mean_out, float* rstd_out, e4m3_t* q,
+                                                float* scale_out, const GnShape p) {
+  extern __shared__ __align__(16) float lds[];
+  constexpr int G = WHOLE ? 1 : VEC;   // groups that a vector can touch
+  const uint32_t width = p.set_groups * p.dim;
+  const uint32_t n_items = p.rows_at_once * (WHOLE ? p.set_vecs : width);
+  float* const items = lds;
+  float* const most = lds + n_items;                       // with a checkpoint only
+  float* const stat = lds + (q ? 2u : 1u) * n_items;       // [3][set_groups]
+  const uint32_t b = gn_block(p.batch * p.sets), n = fast_div(b, p.div_sets), set = b - n * p.sets;
+  const GnLane l = gn_lane<VEC>(p);
+  const size_t base = (size_t)n * p.positions * p.channels + set * width;
+
+  const uint32_t place = l.row * p.channels + l.col, step = p.rows_at_once * p.channels, last = (p.positions - 1u) * p.channels + l.col;
+
+  typename VecIo<T, VEC>::Raw raw[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) raw[k] = VecIo<T, VEC>::template load<false>(near_element(x + base, min(place + (uint32_t)k * step, last)));
+  const auto raw_gamma = VecIo<T, VEC>::template load<false>(gamma + set * width + l.col);
+  const auto raw_beta = VecIo<T, VEC>::template load<false>(beta + set * width + l.col);
+
+  auto valid = [&](int k) { return l.live && place + (uint32_t)k * step <= last; };
+  float a[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) a[e] = 0.0f;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    float v[VEC];
+    again(raw[k]);
+    VecIo<T, VEC>::widen(raw[k], v);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) a[e] += valid(k) ? v[e] : 0.0f;
+    done(a);
+  }
+  gn_deposit<WHOLE, VEC>(items, p, l, a);
+  __syncthreads();
+  gn_groups<WHOLE, VEC>(p, [&](uint32_t g, uint32_t lane, bool writes, uint32_t first, uint32_t per, uint32_t pitch) {
+    const float s = gn_fold<OpSum>(items, p, lane, first, per, pitch);
+    if (writes) stat[g] = s * p.inv_count;
+  });
+  __syncthreads();
+  uint32_t group[G];
+  float mean[G];
+#pragma unroll
+  for (int i = 0; i < G; ++i) {
+    group[i] = fast_div(l.col + i, p.div_dim);
+    mean[i] = stat[group[i]];
+  }
+  float far[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) a[e] = far[e] = 0.0f;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    float v[VEC];
+    again(raw[k]);
+    VecIo<T, VEC>::widen(raw[k], v);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const float c = valid(k) ? v[e] - mean[WHOLE ? 0 : e] : 0.0f;
+      a[e] = __builtin_fmaf(c, c, a[e]);
+      far[e] = fmaxf(far[e], __builtin_fabsf(c));
+    }
+    done(a);
+    done(far);
+  }
+  gn_deposit<WHOLE, VEC>(items, p, l, a);
+  if (q) gn_deposit_max<WHOLE, VEC>(most, p, l, far);
+  __syncthreads();
+  gn_groups<WHOLE, VEC>(p, [&](uint32_t g, uint32_t lane, bool writes, uint32_t first, uint32_t per, uint32_t pitch) {
+    const float r = fast_rsqrt(gn_fold<OpSum>(items, p, lane, first, per, pitch) * p.inv_count + p.eps);
+    const float s = q ? scale_of(gn_fold<OpMax>(most, p, lane, first, per, pitch) * r, p.inv_max, p.tiny) : 0.0f;
+    if (writes) {
+      stat[p.set_groups + g] = r;
+      stat[2u * p.set_groups + g] = s;
+      const uint32_t at = n * p.groups + set * p.set_groups + g;
+      if (mean_out) mean_out[at] = stat[g];
+      if (rstd_out) rstd_out[at] = r;
+      if (q) scale_out[at] = s;
+    }
+  });
+  __syncthreads();
+  float rstd[G], ga[VEC], be[VEC];
+#pragma unroll
+  for (int i = 0; i < G; ++i) rstd[i] = stat[p.set_groups + group[i]];
+  VecIo<T, VEC>::widen(raw_gamma, ga);
+  VecIo<T, VEC>::widen(raw_beta, be);
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    again(raw[k]);
+    if (!valid(k)) continue;
+    float v[VEC];
+    VecIo<T, VEC>::widen(raw[k], v);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      v[e] = activate<ACT>(__builtin_fmaf((v[e] - mean[WHOLE ? 0 : e]) * rstd[WHOLE ? 0 : e], ga[e], be[e]));
+    VecIo<T, VEC>::store(near_element(y + base, place + (uint32_t)k * step), v);
+  }
+  if (!q) return;
+  float inv[G], s[G];
+#pragma unroll
+  for (int i = 0; i < G; ++i) {
+    const Divisor d(stat[2u * p.set_groups + group[i]]);
+    s[i] = d.back;
+    inv[i] = d.inv;
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    again(raw[k]);
+    if (!valid(k)) continue;
+    float v[VEC];
+    VecIo<T, VEC>::widen(raw[k], v);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const int i = WHOLE ? 0 : e;
+      const float z = (v[e] - mean[i]) * rstd[i], d = z * inv[i];
+      v[e] = __builtin_fmaf(__builtin_fmaf(-d, s[i], z), inv[i], d);
+    }
+    VecIo<e4m3_t, VEC>::store(near_element(q + base, place + (uint32_t)k * step), v);
+  }
+}
+
+// ---- first launch of three: statistics of a chunk of positions -------------------------------------------------------------
+// out[batch][chunk][group] = mean, sum of squared deviations from it, lowest and highest value (the last two for the scale of
+// a checkpoint).  Four positions are gathered at a time while the next four are on their way.
+template <typename T, int VEC, bool WHOLE, bool RANGE>
+__global__ void __launch_bounds__(256) k_gn_stats(const T* x, float* out, const GnShape p) {
+  extern __shared__ __align__(16) float lds[];
+  constexpr int U = 4;
+  const uint32_t width = p.set_groups * p.dim;
+  const uint32_t n_items = p.rows_at_once * (WHOLE ? p.set_vecs : width);
+  float* const means = lds;
+  float* const squares = lds + n_items;
+  float* const weight = lds + (RANGE ? 4u : 2u) * n_items;   // [rows_at_once]
+  const uint32_t bc = fast_div(blockIdx.x, p.div_sets), set = blockIdx.x - bc * p.sets;
+  const uint32_t n = fast_div(bc, p.div_chunks), chunk = bc - n * p.chunks;
+  const uint32_t r0 = chunk * p.chunk_rows, r1 = min(r0 + p.chunk_rows, p.positions);
+  const GnLane l = gn_lane<VEC>(p);
+  const T* const from = x + (size_t)n * p.positions * p.channels + set * width + l.col;
+  auto load = [&](uint32_t row) { return VecIo<T, VEC>::template load<false>(from + min(row, r1 - 1u) * p.channels); };
+
+  float mean[VEC], m2[VEC], lo[VEC], hi[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) mean[e] = m2[e] = 0.0f, lo[e] = __builtin_inff(), hi[e] = -__builtin_inff();
+  float count = 0.0f;
+  auto join = [&](const float (&m)[VEC], const float (&d)[VEC], float n_new) {
+    const float w = n_new / (count + n_new), u = count * w;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const float apart = m[e] - mean[e];
+      mean[e] = __builtin_fmaf(apart, w, mean[e]);
+      m2[e] += __builtin_fmaf(apart * apart, u, d[e]);
+    }
+    count += n_new;
+  };
+  uint32_t row = r0 + l.row;
+  const uint32_t step = p.rows_at_once;
+  if (l.live) {
+    typename VecIo<T, VEC>::Raw next[U], now[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = load(row + u * step);
+    for (uint32_t all = r0 + U * step; all <= r1; all += U * step) {   // (every live thread has the positions below `all`)
+#pragma unroll
+      for (int u = 0; u < U; ++u) now[u] = next[u];
+      row += U * step;
+#pragma unroll
+      for (int u = 0; u < U; ++u) next[u] = load(row + u * step);
+      float v[U][VEC], m[VEC], d[VEC];
+#pragma unroll
+      for (int u = 0; u < U; ++u) VecIo<T, VEC>::widen(now[u], v[u]);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        m[e] = ((v[0][e] + v[1][e]) + (v[2][e] + v[3][e])) * 0.25f;
+        d[e] = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const float c = v[u][e] - m[e];
+          d[e] = __builtin_fmaf(c, c, d[e]);
+          if constexpr (RANGE) lo[e] = fminf(lo[e], v[u][e]), hi[e] = fmaxf(hi[e], v[u][e]);
+        }
+      }
+      join(m, d, (float)U);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (row + u * step < r1) {
+        float v[VEC], none[VEC];
+        VecIo<T, VEC>::widen(next[u], v);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          none[e] = 0.0f;
+          if constexpr (RANGE) lo[e] = fminf(lo[e], v[e]), hi[e] = fmaxf(hi[e], v[e]);
+        }
+        join(v, none, 1.0f);
+      }
+    }
+  }
+  // the thread's channels of one group as one item: equal counts, so their mean is the mean of the means
+  if constexpr (WHOLE) {
+    float m = 0.0f, d = 0.0f;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) m += mean[e];
+    m *= 1.0f / VEC;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const float apart = mean[e] - m;
+      d += __builtin_fmaf(apart * apart, count, m2[e]);
+      if constexpr (RANGE) lo[0] = fminf(lo[0], lo[e]), hi[0] = fmaxf(hi[0], hi[e]);
+    }
+    if (l.live) {
+      const uint32_t at = l.row * p.set_vecs + l.vec;
+      means[at] = m;
+      squares[at] = d;
+      if constexpr (RANGE) lds[2u * n_items + at] = lo[0], lds[3u * n_items + at] = hi[0];
+    }
+  } else if (l.live) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const uint32_t at = l.row * width + l.col + e;
+      means[at] = mean[e];
+      squares[at] = m2[e];
+      if constexpr (RANGE) lds[2u * n_items + at] = lo[e], lds[3u * n_items + at] = hi[e];
+    }
+  }
+  if (l.live && l.vec == 0) weight[l.row] = WHOLE ? count * VEC : count;
+  __syncthreads();
+  const float inv = 1.0f / ((float)(r1 - r0) * (float)p.dim);
+  gn_groups<WHOLE, VEC>(p, [&](uint32_t g, uint32_t lane, bool writes, uint32_t first, uint32_t per, uint32_t pitch) {
+    const uint32_t n_it = p.rows_at_once * per, lanes = 1u << p.fold_log2;
+    float m = 0.0f, d = 0.0f, low = __builtin_inff(), high = -__builtin_inff();
+    for (uint32_t i = lane; i < n_it; i += lanes) {
+      const uint32_t rr = fast_div(i, p.div_per), at = rr * pitch + first + (i - rr * per);
+      m = __builtin_fmaf(weight[rr], means[at], m);
+      if constexpr (RANGE) low = fminf(low, lds[2u * n_items + at]), high = fmaxf(high, lds[3u * n_items + at]);
+    }
+    m = group_allreduce<OpSum>(m, (int)lanes) * inv;
+    for (uint32_t i = lane; i < n_it; i += lanes) {
+      const uint32_t rr = fast_div(i, p.div_per), at = rr * pitch + first + (i - rr * per);
+      const float apart = means[at] - m;
+      d += __builtin_fmaf(apart * apart, weight[rr], squares[at]);
+    }
+    d = group_allreduce<OpSum>(d, (int)lanes);
+    if constexpr (RANGE) {
+      high = group_allreduce<OpMax>(high, (int)lanes);
+      low = -group_allreduce<OpMax>(-low, (int)lanes);
+    }
+    if (writes)
+      *reinterpret_cast<f32x4*>(out + ((size_t)bc * p.groups + set * p.set_groups + g) * 4u) = f32x4{m, d, low, high};
+  });
+}
+
+// ---- second launch: the chunks of a batch entry and group, joined ------------------------------------------------------------
+// joined[batch][group] = mean, rstd, scale.  1 << fold_log2 lanes each.
+__global__ void __launch_bounds__(256) k_gn_join(const float* chunks, float* joined, float* mean_out, float* rstd_out, float* scale_out,
+                                                 const GnShape p) {
+  const uint32_t lanes = 1u << p.fold_log2, lane = threadIdx.x & (lanes - 1u);
+  const uint32_t own = blockIdx.x * (256u >> p.fold_log2) + (threadIdx.x >> p.fold_log2);
+  const uint32_t at = min(own, p.batch * p.groups - 1u), n = at / p.groups, g = at - n * p.groups;
+  const f32x4* const from = reinterpret_cast<const f32x4*>(chunks) + (size_t)n * p.chunks * p.groups + g;
+  const float full = (float)p.chunk_rows * (float)p.dim;
+  const float last = (float)(p.positions - (p.chunks - 1u) * p.chunk_rows) * (float)p.dim;
+  float m = 0.0f, d = 0.0f, low = __builtin_inff(), high = -__builtin_inff();
+#pragma unroll 4
+  for (uint32_t c = lane; c < p.chunks; c += lanes) {
+    const f32x4 v = from[(size_t)c * p.groups];
+    m = __builtin_fmaf(c + 1u < p.chunks ? full : last, v.x, m);
+    low = fminf(low, v.z);
+    high = fmaxf(high, v.w);
+  }
+  m = group_allreduce<OpSum>(m, (int)lanes) * p.inv_count;
+#pragma unroll 4
+  for (uint32_t c = lane; c < p.chunks; c += lanes) {
+    const f32x4 v = from[(size_t)c * p.groups];
+    const float apart = v.x - m;
+    d += __builtin_fmaf(apart * apart, c + 1u < p.chunks ? full : last, v.y);
+  }
+  d = group_allreduce<OpSum>(d, (int)lanes);
+  high = group_allreduce<OpMax>(high, (int)lanes);
+  low = -group_allreduce<OpMax>(-low, (int)lanes);
+  const float r = fast_rsqrt(d * p.inv_count + p.eps);
+  const float s = scale_of(fmaxf(high - m, m - low) * r, p.inv_max, p.tiny);
+  if (lane != 0 || own >= p.batch * p.groups) return;
+  *reinterpret_cast<f32x4*>(joined + (size_t)at * 4u) = f32x4{m, r, s, 0.0f};
+  if (mean_out) mean_out[at] = m;
+  if (rstd_out) rstd_out[at] = r;
+  if (scale_out) scale_out[at] = s;
+}
+
+// ---- third launch ------------------------------------------------------------------------------------------------------
+template <typename T, int VEC, bool WHOLE, int ACT, bool STORE8>
+__global__ void __launch_bounds__(256) k_gn_apply(const T* x, const T* gamma, const T* beta, const float* joined, T* y, e4m3_t* q, const GnShape p) {
+  constexpr int U = 4, G = WHOLE ? 1 : VEC;
+  const uint32_t width = p.set_groups * p.dim;
+  const uint32_t bc = fast_div(blockIdx.x, p.div_sets), set = blockIdx.x - bc * p.sets;
+  const uint32_t n = fast_div(bc, p.div_chunks), chunk = bc - n * p.chunks;
+  const uint32_t r0 = chunk * p.chunk_rows, r1 = min(r0 + p.chunk_rows, p.positions);
+  const GnLane l = gn_lane<VEC>(p);
+  if (!l.live) return;
+  const size_t base = (size_t)n * p.positions * p.channels + set * width + l.col;
+  auto load = [&](uint32_t row) { return VecIo<T, VEC>::template load<true>(x + base + min(row, r1 - 1u) * p.channels); };
+  const uint32_t step = p.rows_at_once;
+  uint32_t row = r0 + l.row;
+  typename VecIo<T, VEC>::Raw next[U], now[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) next[u] = load(row + u * step);
+  float mean[G], rstd[G], s[G], inv[G], ga[VEC], be[VEC];
+#pragma unroll
+  for (int i = 0; i < G; ++i) {
+    const f32x4 j = *reinterpret_cast<const f32x4*>(joined + (size_t)(n * p.groups + set * p.set_groups + fast_div(l.col + i, p.div_dim)) * 4u);
+    mean[i] = j.x;
+    rstd[i] = j.y;
+    if constexpr (STORE8) {
+      const Divisor d(j.z);
+      s[i] = d.back;
+      inv[i] = d.inv;
+    }
+  }
+  VecIo<T, VEC>::widen(VecIo<T, VEC>::template load<false>(gamma + set * width + l.col), ga);
+  VecIo<T, VEC>::widen(VecIo<T, VEC>::template load<false>(beta + set * width + l.col), be);
+  auto put = [&](typename VecIo<T, VEC>::Raw raw, uint32_t at) {
+    float v[VEC], z[VEC];
+    VecIo<T, VEC>::widen(raw, v);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const int i = WHOLE ? 0 : e;
+      v[e] = (v[e] - mean[i]) * rstd[i];
+      z[e] = activate<ACT>(__builtin_fmaf(v[e], ga[e], be[e]));
+    }
+    VecIo<T, VEC>::store(y + base + at * p.channels, z);
+    if constexpr (STORE8) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const int i = WHOLE ? 0 : e;
+        const float d = v[e] * inv[i];
+        z[e] = __builtin_fmaf(__builtin_fmaf(-d, s[i], v[e]), inv[i], d);
+      }
+      VecIo<e4m3_t, VEC>::store(q + base + at * p.channels, z);
+    }
+  };
+  for (uint32_t all = r0 + U * step; all <= r1; all += U * step) {   // (every thread has the positions below `all`)
+    const uint32_t at = row;
+#pragma unroll
+    for (int u = 0; u < U; ++u) now[u] = next[u];
+    row += U * step;
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = load(row + u * step);
+#pragma unroll
+    for (int u = 0; u < U; ++u) put(now[u], at + u * step);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (row + u * step < r1) put(next[u], row + u * step);
+}
+
+}  // namespace fsk
+
+namespace fs {
+using namespace fsk;
+
+namespace {
+template <typename T, int VEC, bool WHOLE, int ACT>
+const void* slab_sym(const GroupNormP& p) {
+  if (p.threads == 256) {
+    switch (p.vecs_per_lane) {
+      case 1: return (const void*)k_gn_slab<T, VEC, 1, WHOLE, ACT, 256>;
+      case 2: return (const void*)k_gn_slab<T, VEC, 2, WHOLE, ACT, 256>;
+      case 4: return (const void*)k_gn_slab<T, VEC, 4, WHOLE, ACT, 256>;
+      case 8: return (const void*)k_gn_slab<T, VEC, 8, WHOLE, ACT, 256>;
+    }
+  } else if (p.threads == 512) {
+    switch (p.vecs_per_lane) {
+      case 4: return (const void*)k_gn_slab<T, VEC, 4, WHOLE, ACT, 512>;
+      case 8: return (const void*)k_gn_slab<T, VEC, 8, WHOLE, ACT, 512>;
+      case 16: return (const void*)k_gn_slab<T, VEC, 16, WHOLE, ACT, 512>;
+      case 32: return (const void*)k_gn_slab<T, VEC, 32, WHOLE, ACT, 512>;
+    }
+  }
+  return nullptr;
+}
+template <typename T, int VEC, bool WHOLE>
+const void* act_sym(int32_t kernel, const GroupNormP& p) {
+  if (kernel == K_GN_STATS) return p.checkpoint ? (const void*)k_gn_stats<T, VEC, WHOLE, true> : (const void*)k_gn_stats<T, VEC, WHOLE, false>;
+  if (kernel == K_GN_SLAB) {
+    switch (p.act) {
+      case ACT_NONE: return slab_sym<T, VEC, WHOLE, ACT_NONE>(p);
+      case ACT_GELU: return slab_sym<T, VEC, WHOLE, ACT_GELU>(p);
+      case ACT_SILU: return slab_sym<T, VEC, WHOLE, ACT_SILU>(p);
+      default: return nullptr;
+    }
+  }
+  switch (p.act) {
+    case ACT_NONE: return p.checkpoint ? (const void*)k_gn_apply<T, VEC, WHOLE, ACT_NONE, true> : (const void*)k_gn_apply<T, VEC, WHOLE, ACT_NONE, false>;
+    case ACT_GELU: return p.checkpoint ? (const void*)k_gn_apply<T, VEC, WHOLE, ACT_GELU, true> : (const void*)k_gn_apply<T, VEC, WHOLE, ACT_GELU, false>;
+    case ACT_SILU: return p.checkpoint ? (const void*)k_gn_apply<T, VEC, WHOLE, ACT_SILU, true> : (const void*)k_gn_apply<T, VEC, WHOLE, ACT_SILU, false>;
+    default: return nullptr;
+  }
+}
+template <typename T>
+const void* type_sym(int32_t kernel, const GroupNormP& p) {
+  if (p.vec == 1) return act_sym<T, 1, true>(kernel, p);
+  return p.whole ? act_sym<T, Elem<T>::VEC, true>(kernel, p) : act_sym<T, Elem<T>::VEC, false>(kernel, p);
+}
+}  // namespace
+
+const void* group_norm_kernel_symbol(int32_t kernel, const KernelArgs& a) {
+  const GroupNormP& p = a.u.gn;
+  if (kernel == K_GN_JOIN) return (const void*)k_gn_join;
+  switch (p.dt) {
+    case DT_F32: return type_sym<float>(kernel, p);
+    case DT_F16: return type_sym<f16_t>(kernel, p);
+    case DT_BF16: return type_sym<bf16_t>(kernel, p);
+    default: return nullptr;
+  }
+}
+
+}  // namespace fs

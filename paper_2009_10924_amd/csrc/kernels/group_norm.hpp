@@ -1,0 +1,89 @@
+// What the group normalisation kernels share: which channels and positions a thread of a workgroup has, and the sums of its
+// group's values.
+//
+// x is [batch, positions, channels], channel = group * dim + d.  A workgroup works on a set of `set_groups` groups (`width`
+// neighbouring channels) of one batch entry.  Thread t has the vector t % set_vecs of the set's channels, at positions
+// t / set_vecs, + rows_at_once, + 2 rows_at_once, ...: its channels stay the same, so what is per channel is loaded once, and
+// neighbouring threads read neighbouring memory.  The last vector of a set starts early where the width is no multiple of VEC;
+// the channels it then shares with its neighbour have the same values in both and are deposited twice in the same place.
+#pragma once
+#include "activation.hpp"
+#include "kernel_arguments.hpp"
+#include "vec_access.hpp"
+
+namespace fsk {
+using fs::GnShape;
+
+struct GnLane {
+  uint32_t row, vec, col;   // first position, vector within the set, its first channel within the set
+  bool live;                // threads beyond rows_at_once * set_vecs have nothing
+};
+template <int VEC>
+__device__ __forceinline__ GnLane gn_lane(const GnShape& p) {
+  GnLane l;
+  l.row = (threadIdx.x * p.set_vecs_m) >> 20;   // exact for 1024 threads: the factor is off by less than 2^-20 * set_vecs
+  l.vec = threadIdx.x - l.row * p.set_vecs;
+  l.col = min(l.vec * VEC, p.set_groups * p.dim - VEC);
+  l.live = l.row < p.rows_at_once;
+  return l;
+}
+
+// Workgroups go to the dies in turn; neighbouring sets, which share lines of memory, belong on one die and behind its cache.
+__device__ __forceinline__ uint32_t gn_block(uint32_t blocks) {
+  const uint32_t b = blockIdx.x;
+  return (blocks & 7u) == 0 ? (b & 7u) * (blocks >> 3) + (b >> 3) : b;
+}
+
+// Items of a thread in LDS: WHOLE (its channels are of one group) one per vector, otherwise one per channel.
+template <bool WHOLE, int VEC>
+__device__ __forceinline__ void gn_deposit(float* items, const GnShape& p, const GnLane& l, const float (&v)[VEC]) {
+  if (!l.live) return;
+  if constexpr (WHOLE) {
+    float s = v[0];
+#pragma unroll
+    for (int e = 1; e < VEC; ++e) s += v[e];
+    items[l.row * p.set_vecs + l.vec] = s;
+  } else {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) items[l.row * (p.set_groups * p.dim) + l.col + e] = v[e];
+  }
+}
+template <bool WHOLE, int VEC>
+__device__ __forceinline__ void gn_deposit_max(float* items, const GnShape& p, const GnLane& l, const float (&v)[VEC]) {
+  if constexpr (WHOLE) {
+    float s = v[0];
+#pragma unroll
+    for (int e = 1; e < VEC; ++e) s = fmaxf(s, v[e]);
+    if (l.live) items[l.row * p.set_vecs + l.vec] = s;
+  } else {
+    gn_deposit<false, VEC>(items, p, l, v);
+  }
+}
+
+// 1 << fold_log2 lanes per group run through its items, group by group where there are more groups than such lane sets:
+// f(group, lane among them, first item, items a position has of the group, distance from position to position), called by
+// whole wavefronts (with the last group again where lanes are left over).
+template <bool WHOLE, int VEC, typename F>
+__device__ __forceinline__ void gn_groups(const GnShape& p, F&& f) {
+  const uint32_t lanes = 1u << p.fold_log2, sets = blockDim.x >> p.fold_log2;
+  const uint32_t per = WHOLE ? p.dim / VEC : p.dim, pitch = WHOLE ? p.set_vecs : p.set_groups * p.dim;
+  for (uint32_t g0 = 0; g0 < p.set_groups; g0 += sets) {
+    const uint32_t g = g0 + (threadIdx.x >> p.fold_log2), lane = threadIdx.x & (lanes - 1u);
+    const uint32_t gc = min(g, p.set_groups - 1u);
+    f(gc, lane, lane == 0 && g < p.set_groups, gc * per, per, pitch);
+  }
+}
+// sum (or maximum) of a group's items
+template <typename OP>
+__device__ __forceinline__ float gn_fold(const float* items, const GnShape& p, uint32_t lane, uint32_t first, uint32_t per, uint32_t pitch) {
+  float a = 0.0f;
+  const uint32_t n = p.rows_at_once * per, lanes = 1u << p.fold_log2;
+#pragma unroll 4
+  for (uint32_t i = lane; i < n; i += lanes) {
+    const uint32_t row = fast_div(i, p.div_per);
+    a = OP::apply(a, items[row * pitch + first + (i - row * per)]);
+  }
+  return group_allreduce<OP>(a, (int)lanes);
+}
+
+}  // namespace fsk

@@ -10,6 +10,8 @@ const void* layernorm_kernel_symbol(int32_t kernel, const KernelArgs& a);
 const void* gelu_kernel_symbol(int32_t kernel, const KernelArgs& a);
 const void* tchain_kernel_symbol(int32_t kernel, const KernelArgs& a);
 const void* rowops_kernel_symbol(int32_t kernel, const KernelArgs& a);
+const void* group_norm_kernel_symbol(int32_t kernel, const KernelArgs& a);
+const void* group_norm_backward_kernel_symbol(int32_t kernel, const KernelArgs& a);
 const void* checkpoint_kernel_symbol(int32_t kernel, const KernelArgs& a);
 const void* rowprog_kernel_symbol(int32_t kernel, const KernelArgs& a);
 }  // namespace fs

@@ -11,7 +11,7 @@ const char* const kNames[K_COUNT] = {
     "unary", "binary", "reduce_row", "reduce_mid", "transpose_rows", "transpose_tile", "copy", "softmax_wave", "softmax_block",
     "layernorm_wave", "layernorm_block", "bias_gelu", "bias_gelu_dbias", "colfold", "tchain_wave", "tchain_lds", "row_wave",
     "row_block", "row_program", "layernorm_bwd", "row_generated", "checkpoint_wave", "checkpoint_block", "checkpoint_long", "checkpoint_grad",
-    "checkpoint_grad_sums",
+    "checkpoint_grad_sums", "gn_slab", "gn_stats", "gn_join", "gn_apply", "gn_bwd_slab", "gn_bwd_sums", "gn_bwd_join", "gn_bwd_apply",
 };
 
 const void* symbol_for(int32_t kernel, const KernelArgs& a) {
@@ -33,6 +33,10 @@ const void* symbol_for(int32_t kernel, const KernelArgs& a) {
       return rowprog_kernel_symbol(kernel, a);
     case K_CHECKPOINT_WAVE: case K_CHECKPOINT_BLOCK: case K_CHECKPOINT_LONG: case K_CHECKPOINT_GRAD: case K_CHECKPOINT_GRAD_SUMS:
       return checkpoint_kernel_symbol(kernel, a);
+    case K_GN_SLAB: case K_GN_STATS: case K_GN_JOIN: case K_GN_APPLY:
+      return group_norm_kernel_symbol(kernel, a);
+    case K_GN_BWD_SLAB: case K_GN_BWD_SUMS: case K_GN_BWD_JOIN: case K_GN_BWD_APPLY:
+      return group_norm_backward_kernel_symbol(kernel, a);
     default:
       return nullptr;
   }

@@ -50,6 +50,16 @@ enum KernelId : int32_t {
   K_CHECKPOINT_LONG,   // a workgroup per block, which it reads twice
   K_CHECKPOINT_GRAD,   // p0 q, p1 scales, p2 dy (or null), p3 dx or the values themselves
   K_CHECKPOINT_GRAD_SUMS,   // p0 q, p1 scales, p2 dy, p3 dx, p4 partials [n_row_blocks, pitch] f32 (folded by K_COLFOLD)
+  // group normalisation: a workgroup per batch entry and set of groups holds their values (SLAB), or the statistics are
+  // gathered chunk by chunk of positions, joined, and the values read again
+  K_GN_SLAB,           // p0 x, p1 gamma, p2 beta, p3 y, p4 mean, p5 rstd, p6 q, p7 scales (p4 to p7: or null)
+  K_GN_STATS,          // p0 x, p1 chunk statistics
+  K_GN_JOIN,           // p0 chunk statistics, p1 joined statistics, p2 mean, p3 rstd, p4 scales (or null)
+  K_GN_APPLY,          // p0 x, p1 gamma, p2 beta, p3 joined statistics, p4 y, p5 q (or null)
+  K_GN_BWD_SLAB,       // p0 x or q, p1 mean or scales, p2 rstd, p3 gamma, p4 beta, p5 dy, p6 dx, p7 sums [batch, 2, pitch]
+  K_GN_BWD_SUMS,       // p0 x or q, p1 mean or scales, p2 rstd, p3 gamma, p4 beta, p5 dy, p6 chunk sums [batch, chunks, 2, C]
+  K_GN_BWD_JOIN,       // p0 chunk sums, p1 gamma, p2 sums [batch, 2, pitch], p3 group means [batch, G, 2]
+  K_GN_BWD_APPLY,      // p0 x or q, p1 mean or scales, p2 rstd, p3 gamma, p4 beta, p5 dy, p6 dx, p7 group means
   K_COUNT
 };
 
@@ -175,6 +185,24 @@ struct CheckpointP {
   int32_t lanes_per_row, lanes_log2, vecs_per_lane;
   int32_t waves, unroll;            // K_CHECKPOINT_GRAD_SUMS: workgroup = waves x 64 lanes, a row tile = waves * unroll rows
   uint32_t n_row_blocks;
+  int32_t stream;
+};
+struct GroupNormP {
+  int32_t dt, act;                  // x / y / dy / dx / gamma / beta share dt; statistics and sums are float32
+  int32_t checkpoint;               // forward: q and its scales are written; backward: they are read instead of x and the mean
+  uint32_t batch, positions, groups, dim, channels;   // channels = groups * dim
+  uint32_t set_groups, sets;        // groups that a workgroup works on, sets of them
+  int32_t vec;                      // elements per access: a whole vector, or 1 where a set has fewer channels
+  int32_t whole;                    // 1: a vector lies within one group
+  uint32_t set_vecs, rows_at_once;  // vectors of a position in a set; positions that a workgroup's threads cover
+  uint32_t set_vecs_m;              // ceil(2^20 / set_vecs)
+  FastDiv div_dim, div_per;         // by dim; by the items a position leaves in LDS for one group
+  FastDiv div_sets, div_chunks;
+  int32_t fold_log2;                // log2 of the lanes that fold one group's items
+  uint32_t chunk_rows, chunks;      // positions per chunk
+  int32_t threads, vecs_per_lane;
+  uint32_t join_cols;               // K_GN_BWD_JOIN: channels of a workgroup, whole groups
+  float eps, inv_count, inv_max, tiny;   // inv_count = 1 / (positions * dim)
   int32_t stream;
 };
 enum RowPattern : int32_t { ROW_SOFTMAX_BWD = 0, ROW_RMSNORM = 1 };
@@ -320,6 +348,7 @@ struct KernelArgs {
     RowP row;
     LnBwdP lnbwd;
     CheckpointP checkpoint;
+    GroupNormP gn;
     RowProgP prog;
   } u;
   KernelArgs() { u.binary = BinaryP{}; }

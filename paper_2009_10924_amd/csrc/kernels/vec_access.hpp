@@ -58,4 +58,22 @@ template <> struct VecIo<e4m3_t, 4> {
   }
 };
 
+// Element `i` behind a pointer that the whole workgroup shares, at a distance of less than 2^32 bytes: a scalar base and one
+// vector register instead of a 64-bit address per access.
+template <typename T> __device__ __forceinline__ const T* near_element(const T* base, uint32_t i) {
+  return reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + (uint32_t)(i * (uint32_t)sizeof(T)));
+}
+template <typename T> __device__ __forceinline__ T* near_element(T* base, uint32_t i) {
+  return reinterpret_cast<T*>(reinterpret_cast<char*>(base) + (uint32_t)(i * (uint32_t)sizeof(T)));
+}
+
+// Passes over values that a thread keeps as raw bits (a workgroup's registers hold them all).  Left alone, the compiler keeps the
+// widened values of one pass for the next, and works on all steps of a pass at once: several times the registers.
+// again(): the bits may have changed, what was made of them is made anew.  done(): the step's results are wanted here.
+template <typename R> __device__ __forceinline__ void again(R& raw) { asm volatile("" : "+v"(raw)); }
+template <int N> __device__ __forceinline__ void done(float (&v)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) asm volatile("" : "+v"(v[e]));
+}
+
 }  // namespace fsk
