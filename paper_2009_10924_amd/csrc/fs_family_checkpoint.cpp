@@ -37,8 +37,8 @@ bool match_activation_gradient(const fs_graph& g, int32_t t, MatchState* st, int
 }
 
 // The output that is $V's quotient by its scale, in 8 bits, and the scale: maxima of |$V| (`maximum` over "abs($V)"), times a
-// constant, plus a constant.  Constants for which the kernels' quotients are those of a division: scales between 1e-37 and
-// 2^125, whose reciprocals are normal numbers.
+// constant, plus a constant.  Constants for which quotients by a reciprocal are those of a division (scales between 1e-37 and
+// 2^125, whose reciprocals are normal numbers) and stay within the format's range (at least 1 / 448 of the maximum).
 bool match_8bit(const fs_graph& g, const char* maximum, MatchState* st, int32_t* t_q, int32_t* t_s) {
   for (int32_t t : g.outputs) {
     if (g.tensors[t].store_as != FS_E4M3) continue;
@@ -48,7 +48,7 @@ bool match_8bit(const fs_graph& g, const char* maximum, MatchState* st, int32_t*
     if (!Pattern("addc[#81](scale[#80](" + std::string(maximum) + "))").match(g, s, &trial)) return false;
     if (g.tensors[s].output_slot < 0 || g.tensors[s].store_as != FS_F32) return false;
     const double inv_max = trial.scalars[80], tiny = trial.scalars[81];
-    if (!(inv_max > 0.0 && inv_max <= 0.125 && tiny >= 1e-37 && tiny <= 1e30)) return false;
+    if (!(inv_max >= (1.0 - 1e-6) / 448.0 && inv_max <= 0.125 && tiny >= 1e-37 && tiny <= 1e30)) return false;
     *st = trial;
     *t_q = t;
     *t_s = s;

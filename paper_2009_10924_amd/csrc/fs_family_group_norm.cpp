@@ -67,7 +67,7 @@ int fold_lanes_log2(uint32_t threads, uint32_t n, uint32_t items) {
 bool cut(GroupNormP* p, uint32_t want) {
   const uint32_t round = 4 * p->rows_at_once;
   const uint32_t most = std::max<uint32_t>(1, want / (p->batch * p->sets));
-  uint32_t rows = (p->positions + most - 1) / most;
+  uint32_t rows = std::min((p->positions + most - 1) / most, kGnMostRows * p->rows_at_once);
   rows = std::min(p->positions, (rows + round - 1) / round * round);
   p->chunk_rows = rows;
   p->chunks = (p->positions + rows - 1) / rows;
@@ -89,6 +89,12 @@ uint32_t widest_set(const GroupNormP& p) {
     if (p.groups % s == 0 && lay_out(&q, 256, s)) return s;
   }
   return 0;
+}
+
+// Whether the last launch's workgroups join their groups' chunks themselves: a launch less, where one batch of `loads` loads per
+// lane brings all of them (a second one costs more than a launch).
+bool joins(const GroupNormP& p, uint32_t set_groups, uint32_t loads) {
+  return (uint64_t)p.chunks * std::max<uint32_t>(set_groups, 4) <= 256ull * loads;
 }
 
 struct Traffic {
@@ -225,19 +231,22 @@ bool build_group_norm(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
     }
   }
 
-  // ---- three launches
+  // ---- two or three launches
   const uint32_t gs = widest_set(base);
   if (gs == 0) return true;
-  for (uint32_t want : {1024u, 2048u}) {
+  uint32_t last_chunks = 0;
+  for (uint32_t want : {256u, 512u, 1024u, 2048u}) {
     GroupNormP p = base;
-    if (!lay_out(&p, 256, gs) || !cut(&p, want)) continue;
+    if (!lay_out(&p, 256, gs) || !cut(&p, want) || p.chunks == last_chunks) continue;
+    last_chunks = p.chunks;
     const uint32_t items = p.rows_at_once * (p.whole ? p.set_vecs : gs * p.dim);
-    p.fold_log2 = fold_lanes_log2(256, gs, p.rows_at_once * (p.whole ? p.dim / p.vec : p.dim));
     const int64_t lds = 4ll * ((has_8bit ? 4 : 2) * (int64_t)items + p.rows_at_once);
-    const int64_t chunk_bytes = aligned(16ll * p.batch * p.chunks * p.groups);
+    const int64_t chunk_bytes = aligned((has_8bit ? 16ll : 8ll) * p.batch * p.chunks * p.groups);
+    const bool join = joins(p, gs, has_8bit ? 8 : 16);
     Candidate c = make_candidate(g, "group_norm", FS_SCHEME_GLOBAL, K_GN_STATS);
     {
       Launch& l = c.launches.front();
+      p.fold_log2 = fold_lanes_log2(256, gs, p.rows_at_once * (p.whole ? p.dim / p.vec : p.dim));
       l.args.u.gn = p;
       l.ptr[0] = in_ref(g, tx);
       l.ptr[1] = ws_ref(0);
@@ -245,7 +254,12 @@ bool build_group_norm(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
       l.shape.grid[0] = p.batch * p.chunks * p.sets;
       l.shape.lds_bytes = (uint32_t)lds;
     }
-    {
+    auto statistics = [&](Launch& l, int first) {
+      if (t_mu >= 0) l.ptr[first] = out_ref(g.tensors[t_mu].output_slot);
+      if (t_r >= 0) l.ptr[first + 1] = out_ref(g.tensors[t_r].output_slot);
+      if (t_s >= 0) l.ptr[first + 2] = out_ref(g.tensors[t_s].output_slot);
+    };
+    if (!join) {
       c.launches.emplace_back();
       Launch& l = c.launches.back();
       l.kernel = K_GN_JOIN;
@@ -253,9 +267,7 @@ bool build_group_norm(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
       l.args.u.gn.fold_log2 = std::min(6, log2_of(pow2_at_least(p.chunks)));
       l.ptr[0] = ws_ref(0);
       l.ptr[1] = ws_ref(chunk_bytes);
-      if (t_mu >= 0) l.ptr[2] = out_ref(g.tensors[t_mu].output_slot);
-      if (t_r >= 0) l.ptr[3] = out_ref(g.tensors[t_r].output_slot);
-      if (t_s >= 0) l.ptr[4] = out_ref(g.tensors[t_s].output_slot);
+      statistics(l, 2);
       const uint32_t at_once = 256u >> l.args.u.gn.fold_log2;
       l.shape.block[0] = 256;
       l.shape.grid[0] = (p.batch * p.groups + at_once - 1) / at_once;
@@ -265,26 +277,30 @@ bool build_group_norm(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
       Launch& l = c.launches.back();
       l.kernel = K_GN_APPLY;
       l.args.u.gn = p;
+      l.args.u.gn.join = join ? 1 : 0;
+      l.args.u.gn.fold_log2 = fold_lanes_log2(256, gs, p.chunks);
       l.ptr[0] = in_ref(g, tx);
       l.ptr[1] = in_ref(g, tg);
       l.ptr[2] = in_ref(g, tb);
-      l.ptr[3] = ws_ref(chunk_bytes);
+      l.ptr[3] = ws_ref(join ? 0 : chunk_bytes);
       l.ptr[4] = out_ref(g.tensors[t_y].output_slot);
       if (t_q >= 0) l.ptr[5] = out_ref(g.tensors[t_q].output_slot);
+      if (join) statistics(l, 6);
       l.shape.block[0] = 256;
       l.shape.grid[0] = p.batch * p.chunks * p.sets;
+      l.shape.lds_bytes = join ? 16 * gs : 0;
     }
-    c.info.n_kernels = 3;
-    c.info.workspace_bytes = chunk_bytes + aligned(16ll * p.batch * p.groups);
+    c.info.n_kernels = (int32_t)c.launches.size();
+    c.info.workspace_bytes = chunk_bytes + (join ? 0 : aligned(16ll * p.batch * p.groups));
     c.info.bytes_moved_model = c.info.bytes_min + (int64_t)t.read_bytes;
     c.info.lanes_per_row = (int32_t)p.set_vecs;
     c.info.vecs_per_lane = 4;
     c.info.rows_per_block = (int32_t)p.chunk_rows;
     c.info.lds_bytes = (int32_t)lds;
     KernelCost kc;
-    passes_cost(p, t, p.vec * esz, 3, &kc);
+    passes_cost(p, t, p.vec * esz, (int)c.launches.size(), &kc);
     char var[56];
-    snprintf(var, sizeof var, "<%s,%s,G%u,C%u,apply>", dtype_name(p.dt), act_name(act), gs, p.chunks);
+    snprintf(var, sizeof var, "<%s,%s,G%u,C%u,%sapply>", dtype_name(p.dt), act_name(act), gs, p.chunks, join ? "" : "join,");
     finish_candidate(&c, var, kc);
     out->push_back(c);
   }
@@ -406,27 +422,31 @@ bool build_group_norm_backward(const fs_graph& g, std::vector<Candidate>* out, P
       const uint32_t width = gs * p.dim;
       p.vecs_per_lane = sh.K;
       p.fold_log2 = fold_lanes_log2(sh.threads, width, p.rows_at_once);
-      const int64_t lds = 4ll * ((int64_t)p.rows_at_once * width + 2 * width + 2 * gs);
+      p.means_log2 = fold_lanes_log2(sh.threads, gs, p.dim);
+      const int64_t lds = 4ll * ((int64_t)p.rows_at_once * width + 3 * width + 2 * gs);
       if (lds > 64 * 1024 || (uint64_t)p.batch * p.sets >= (1ull << 31)) continue;
       Candidate c = make_candidate(g, "group_norm_backward", FS_SCHEME_LDS, K_GN_BWD_SLAB);
       Launch& l = c.launches.front();
       l.args.u.gn = p;
       fill_inputs(l);
       l.ptr[6] = out_ref(g.tensors[t_dx].output_slot);
-      l.ptr[7] = ws_ref(0);
+      l.ptr[7] = p.batch == 1 ? out_ref(g.tensors[t_dbeta].output_slot) : ws_ref(0);
+      l.ptr[8] = p.batch == 1 ? out_ref(g.tensors[t_dgamma].output_slot) : ws_ref(4ll * pitch);
       l.shape.block[0] = (uint32_t)sh.threads;
       l.shape.grid[0] = p.batch * p.sets;
       l.shape.lds_bytes = (uint32_t)lds;
       KernelCost kc;
       slab_cost(p, t, esz, sh.K, p.vec * (esz + xsz), (int)lds, &kc);
-      kc.serial_tail_s = 2.0e-6;
+      kc.serial_tail_s = p.batch == 1 ? 0.0 : 2.0e-6;
       char var[56];
-      snprintf(var, sizeof var, "<%s,%s,T%d,K%d,G%u,fold>", dtype_name(p.dt), act_name(p.act), sh.threads, sh.K, gs);
+      snprintf(var, sizeof var, "<%s,%s,T%d,K%d,G%u%s>", dtype_name(p.dt), act_name(p.act), sh.threads, sh.K, gs, p.batch == 1 ? "" : ",fold");
       finish_candidate(&c, var, kc);
-      add_fold(&c, 0);
-      c.info.n_kernels = 2;
-      c.info.workspace_bytes = sum_bytes;
-      c.info.bytes_moved_model = c.info.bytes_min + 2 * sum_bytes;
+      if (p.batch > 1) {
+        add_fold(&c, 0);
+        c.info.n_kernels = 2;
+        c.info.workspace_bytes = sum_bytes;
+        c.info.bytes_moved_model = c.info.bytes_min + 2 * sum_bytes;
+      }
       c.info.lanes_per_row = (int32_t)p.set_vecs;
       c.info.vecs_per_lane = sh.K;
       c.info.rows_per_block = (int32_t)p.rows_at_once;
@@ -435,67 +455,74 @@ bool build_group_norm_backward(const fs_graph& g, std::vector<Candidate>* out, P
     }
   }
 
-  // ---- three launches and the fold
+  // ---- two or three launches
   const uint32_t gs = widest_set(base);
   if (gs == 0) return true;
-  for (uint32_t want : {1024u, 2048u}) {
+  uint32_t last_chunks = 0;
+  for (uint32_t want : {256u, 512u, 1024u, 2048u}) {
     GroupNormP p = base;
-    if (!lay_out(&p, 256, gs) || !cut(&p, want)) continue;
-    const uint32_t width = gs * p.dim;
-    p.fold_log2 = fold_lanes_log2(256, width, p.rows_at_once);
-    const int64_t lds = 4ll * ((int64_t)p.rows_at_once * width + width);
-    const int64_t chunk_bytes = aligned(8ll * p.batch * p.chunks * p.channels);
+    if (!lay_out(&p, 256, gs) || !cut(&p, want) || p.chunks == last_chunks) continue;
+    last_chunks = p.chunks;
+    const uint32_t width = gs * p.dim, rows = p.batch * p.chunks;
+    const int64_t lds = 4ll * ((int64_t)p.rows_at_once * width + 3 * width);
+    const int64_t chunk_bytes = aligned(8ll * rows * pitch), mean_bytes = aligned(8ll * rows * p.groups);
+    const bool join = joins(p, gs, 16);
     Candidate c = make_candidate(g, "group_norm_backward", FS_SCHEME_GLOBAL, K_GN_BWD_SUMS);
     {
       Launch& l = c.launches.front();
+      p.fold_log2 = fold_lanes_log2(256, width, p.rows_at_once);
+      p.means_log2 = fold_lanes_log2(256, gs, p.dim);
       l.args.u.gn = p;
       fill_inputs(l);
       l.ptr[6] = ws_ref(0);
+      l.ptr[7] = ws_ref(chunk_bytes);
       l.shape.block[0] = 256;
-      l.shape.grid[0] = p.batch * p.chunks * p.sets;
+      l.shape.grid[0] = rows * p.sets;
       l.shape.lds_bytes = (uint32_t)lds;
     }
-    {
+    if (!join) {
       c.launches.emplace_back();
       Launch& l = c.launches.back();
       l.kernel = K_GN_BWD_JOIN;
-      GroupNormP& q = l.args.u.gn;
-      q = p;
-      const uint32_t at_once = p.chunks <= 32 ? 64 : 16;   // channels side by side, the rest of the threads along the chunks
-      q.fold_log2 = log2_of(256 / at_once);
-      q.join_cols = p.dim * std::max<uint32_t>(1, at_once / p.dim);
-      l.ptr[0] = ws_ref(0);
-      l.ptr[1] = in_ref(g, tg);
-      l.ptr[2] = ws_ref(chunk_bytes);
-      l.ptr[3] = ws_ref(chunk_bytes + sum_bytes);
+      l.args.u.gn = p;
+      l.args.u.gn.fold_log2 = std::min(6, log2_of(pow2_at_least(p.chunks)));
+      l.ptr[0] = ws_ref(chunk_bytes);
+      l.ptr[1] = ws_ref(chunk_bytes + mean_bytes);
+      const uint32_t at_once = 256u >> l.args.u.gn.fold_log2;
       l.shape.block[0] = 256;
-      l.shape.grid[0] = p.batch * ((p.channels + q.join_cols - 1) / q.join_cols);
-      l.shape.lds_bytes = 8 * q.join_cols;
-      if (l.shape.lds_bytes > 60 * 1024) continue;
+      l.shape.grid[0] = (p.batch * p.groups + at_once - 1) / at_once;
     }
     {
       c.launches.emplace_back();
       Launch& l = c.launches.back();
       l.kernel = K_GN_BWD_APPLY;
-      l.args.u.gn = p;
+      GroupNormP& q = l.args.u.gn;
+      q = p;
+      q.join = join ? 1 : 0;
+      q.fold_log2 = fold_lanes_log2(256, gs, p.chunks);
+      const uint32_t quads = rows > 128 ? 4 : 16;   // quads of columns per workgroup of the fold
+      q.fold_blocks = ((2 * pitch / 4 + quads - 1) / quads + 7) / 8 * 8;
       fill_inputs(l);
       l.ptr[6] = out_ref(g.tensors[t_dx].output_slot);
-      l.ptr[7] = ws_ref(chunk_bytes + sum_bytes);
+      l.ptr[7] = ws_ref(join ? chunk_bytes : chunk_bytes + mean_bytes);
+      l.ptr[8] = ws_ref(0);
+      l.ptr[9] = out_ref(g.tensors[t_dbeta].output_slot);
+      l.ptr[10] = out_ref(g.tensors[t_dgamma].output_slot);
       l.shape.block[0] = 256;
-      l.shape.grid[0] = p.batch * p.chunks * p.sets;
+      l.shape.grid[0] = q.fold_blocks + rows * p.sets;
+      l.shape.lds_bytes = std::max<uint32_t>(4096, join ? 8 * gs : 0);
     }
-    add_fold(&c, chunk_bytes);
-    c.info.n_kernels = 4;
-    c.info.workspace_bytes = chunk_bytes + sum_bytes + aligned(8ll * p.batch * p.groups);
+    c.info.n_kernels = (int32_t)c.launches.size();
+    c.info.workspace_bytes = chunk_bytes + mean_bytes + (join ? 0 : aligned(8ll * p.batch * p.groups));
     c.info.bytes_moved_model = c.info.bytes_min + (int64_t)t.read_bytes + 2 * chunk_bytes;
     c.info.lanes_per_row = (int32_t)p.set_vecs;
     c.info.vecs_per_lane = 4;
     c.info.rows_per_block = (int32_t)p.chunk_rows;
     c.info.lds_bytes = (int32_t)lds;
     KernelCost kc;
-    passes_cost(p, t, p.vec * (esz + xsz), 4, &kc);
+    passes_cost(p, t, p.vec * (esz + xsz), (int)c.launches.size(), &kc);
     char var[56];
-    snprintf(var, sizeof var, "<%s,%s,G%u,C%u,apply,fold>", dtype_name(p.dt), act_name(p.act), gs, p.chunks);
+    snprintf(var, sizeof var, "<%s,%s,G%u,C%u,%sapply>", dtype_name(p.dt), act_name(p.act), gs, p.chunks, join ? "" : "join,");
     finish_candidate(&c, var, kc);
     out->push_back(c);
   }

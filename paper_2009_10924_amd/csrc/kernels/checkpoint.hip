@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(1024) k_checkpoint_long(const T* x, const T* b
     } else {
       for (uint32_t i = c; i < cols; ++i) {
         const float v = load1(x + base + i) + (bias ? load1(bias + at + i) : 0.0f);
-        store1(q + base + i, s.divide(v));
+        store1_in_range(q + base + i, s.divide(v));
         if constexpr (ACT != ACT_NONE) store1(y + base + i, activate<ACT>(v));
       }
     }

@@ -19,6 +19,13 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
   w = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_clamp(c), e4m3_clamp(d), w, true);
   return (uint32_t)w;
 }
+// the same for values of at most 448 but for their rounding (which the format's next border, 464, is far from), or NaN
+__device__ __forceinline__ uint32_t pack_e4m3_in_range(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+  return (uint32_t)w;
+}
+__device__ __forceinline__ void store1_in_range(e4m3_t* p, float v) { p->bits = (unsigned char)(__builtin_amdgcn_cvt_pk_fp8_f32(v, 0.0f, 0, false) & 0xFF); }
 __device__ __forceinline__ void unpack_e4m3(uint32_t w, float& a, float& b, float& c, float& d) {
   const f32x2 lo = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false));
   const f32x2 hi = __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true));

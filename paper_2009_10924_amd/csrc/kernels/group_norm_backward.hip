@@ -3,10 +3,11 @@
 //     A = sum over positions of dz,   B = sum over positions of dz xh
 // everything else follows: dbeta = sum_n A, dgamma = sum_n B, and for a group's n values
 //     m1 = sum_d gamma A / n,   m2 = sum_d gamma B / n,   dx = (gamma dz - m1 - xh m2) rstd.
-// A workgroup that holds a set's values (k_gn_bwd_slab) reads them once; otherwise a first launch gathers A and B per chunk of
-// positions, a second adds the chunks and makes the group means, a third reads the values again.  K_COLFOLD adds up the batch.
+// A workgroup that holds a set's values (k_gn_bwd_slab) reads them once, and K_COLFOLD adds up the batch; otherwise a first launch
+// gathers A and B per chunk of positions and a second one, which adds up the chunks, reads the values again.
 #include <hip/hip_runtime.h>
 
+#include "fold.hpp"
 #include "group_norm.hpp"
 #include "kernel_table.hpp"
 
@@ -17,35 +18,59 @@ using namespace fs;
 template <typename T, bool FROM8> struct GnValue { typedef T type; };
 template <typename T> struct GnValue<T, true> { typedef e4m3_t type; };
 
-// What a thread knows of its channels: xh = (v - shift) * scale.
+// What a thread knows of its channels.  Its values are worked on about their mean, v - shift (an 8-bit value as it is), and the
+// factor that makes xh of them is multiplied into what is per channel: z = (v - shift) (scale gamma) + beta,  sum dz xh = scale
+// sum dz (v - shift).
 template <typename T, int VEC, bool FROM8>
 struct GnChannels {
-  float shift[VEC], scale[VEC], ga[VEC], be[VEC];
+  float shift[VEC], scale[VEC], slope[VEC], be[VEC], ga[VEC];
   // `centre`: means, or the checkpoint's scales
   __device__ __forceinline__ void load(const GnShape& p, const GnLane& l, uint32_t n, uint32_t set, const float* centre, const float* rstd,
                                        const T* gamma, const T* beta) {
     const uint32_t c = set * p.set_groups * p.dim + l.col, g0 = n * p.groups;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      const uint32_t g = g0 + fast_div(c + e, p.div_dim);
-      shift[e] = FROM8 ? 0.0f : centre[g];
-      scale[e] = FROM8 ? centre[g] : rstd[g];
-    }
     VecIo<T, VEC>::widen(VecIo<T, VEC>::template load<false>(gamma + c), ga);
     if (beta) VecIo<T, VEC>::widen(VecIo<T, VEC>::template load<false>(beta + c), be);
+    // one group: one pair of values (as many loads as channels otherwise, which in the small shapes is what a thread mostly does)
+    const uint32_t first = g0 + fast_div(c, p.div_dim);
+    const float t0 = centre[first], r0 = FROM8 ? t0 : rstd[first];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) shift[e] = FROM8 ? 0.0f : t0, scale[e] = r0;
+    if (!p.whole) {
+#pragma unroll
+      for (int e = 1; e < VEC; ++e) {
+        const uint32_t g = g0 + fast_div(c + e, p.div_dim);
+        shift[e] = FROM8 ? 0.0f : centre[g];
+        scale[e] = FROM8 ? centre[g] : rstd[g];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) slope[e] = scale[e] * ga[e];
   }
-  __device__ __forceinline__ float normal(float v, int e) const { return FROM8 ? v * scale[e] : (v - shift[e]) * scale[e]; }
+  __device__ __forceinline__ float about_mean(float v, int e) const { return FROM8 ? v : v - shift[e]; }
   template <int ACT>
-  __device__ __forceinline__ float dz(float xh, float dy, int e) const {
+  __device__ __forceinline__ float dz(float v, float dy, int e) const {   // v: about its mean
     if constexpr (ACT == ACT_NONE) return dy;
-    else return dy * activation_slope<ACT>(__builtin_fmaf(xh, ga[e], be[e]));
+    else return dy * activation_slope<ACT>(__builtin_fmaf(v, slope[e], be[e]));
+  }
+};
+// dx = (gamma dz - m1 - xh m2) rstd = dz (gamma rstd) + ((v - shift) (-m2 scale rstd) - m1 rstd)
+template <int VEC>
+struct GnGradient {
+  float by_dz[VEC], by_v[VEC], off[VEC];
+  __device__ __forceinline__ float dx(float v, float dz, int e) const { return __builtin_fmaf(dz, by_dz[e], __builtin_fmaf(v, by_v[e], off[e])); }
+  template <typename C>
+  __device__ __forceinline__ void set(int e, const C& ch, float rstd, float m1, float m2) {
+    by_dz[e] = ch.ga[e] * rstd;
+    by_v[e] = -m2 * rstd * ch.scale[e];
+    off[e] = -m1 * rstd;
   }
 };
 
-// Sums over the workgroup's positions of what every thread has gathered per channel: channel c of the set to out[c], by
-// 1 << fold_log2 lanes each.  `items`: rows_at_once * width floats of LDS.
+// Sums over the workgroup's positions of what every thread has gathered per channel: channel c of the set to out[c], and times
+// gamma to weighted[c], by 1 << fold_log2 lanes each.  `items`: rows_at_once * width floats of LDS.
 template <int VEC>
-__device__ __forceinline__ void gn_channel_sums(float* items, const GnShape& p, const GnLane& l, const float (&v)[VEC], float* sums, float* out) {
+__device__ __forceinline__ void gn_channel_sums(float* items, const GnShape& p, const GnLane& l, const float (&v)[VEC], const float* gain, float* weighted,
+                                                float* out) {
   const uint32_t width = p.set_groups * p.dim, lanes = 1u << p.fold_log2, lane = threadIdx.x & (lanes - 1u);
   gn_deposit<false, VEC>(items, p, l, v);
   __syncthreads();
@@ -56,22 +81,49 @@ __device__ __forceinline__ void gn_channel_sums(float* items, const GnShape& p, 
     for (uint32_t r = lane; r < p.rows_at_once; r += lanes) a += items[r * width + cc];
     a = group_allreduce<OpSum>(a, (int)lanes);
     if (lane == 0 && c < width) {
-      sums[c] = a;
+      weighted[c] = a * gain[c];
       out[c] = a;
     }
   }
   __syncthreads();
 }
+// gamma of the set's channels in LDS (the first position's threads have them all)
+template <int VEC>
+__device__ __forceinline__ void gn_keep_gain(float* gain, const GnLane& l, const float (&ga)[VEC]) {
+  if (l.row != 0) return;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) gain[l.col + e] = ga[e];
+}
+// A group's means m1 and m2 from its channels' weighted sums in LDS, 1 << means_log2 lanes per group: f(group, m1, m2) on the
+// first of them.  (A wavefront per group, with gamma from memory, took 5 us of the 16 of f16 [2, 16384, 512].)
+template <typename F>
+__device__ __forceinline__ void gn_group_means(const GnShape& p, const float* wa, const float* wb, F&& f) {
+  const uint32_t lanes = 1u << p.means_log2, lane = threadIdx.x & (lanes - 1u);
+  for (uint32_t g0 = 0; g0 < p.set_groups; g0 += blockDim.x >> p.means_log2) {
+    const uint32_t g = g0 + (threadIdx.x >> p.means_log2), gc = min(g, p.set_groups - 1u);
+    float m1 = 0.0f, m2 = 0.0f;
+#pragma unroll 4
+    for (uint32_t d = lane; d < p.dim; d += lanes) {
+      m1 += wa[gc * p.dim + d];
+      m2 += wb[gc * p.dim + d];
+    }
+    m1 = group_allreduce<OpSum>(m1, (int)lanes);
+    m2 = group_allreduce<OpSum>(m2, (int)lanes);
+    if (lane == 0 && g < p.set_groups) f(g, m1 * p.inv_count, m2 * p.inv_count);
+  }
+}
 
-// ---- one launch (and the fold over the batch) --------------------------------------------------------------------------------
+// ---- one launch (and, for more than one batch entry, the fold) -----------------------------------------------------------------
+// out_a, out_b: A and B of batch entry n, `2 * sum_pitch` floats behind those of n - 1 (with one entry they are dbeta and dgamma).
 template <typename T, int VEC, int K, int ACT, bool FROM8, int NT>
 __global__ void __launch_bounds__(NT) k_gn_bwd_slab(const typename GnValue<T, FROM8>::type* x, const float* centre, const float* rstd, const T* gamma,
-                                                    const T* beta, const T* dy, T* dx, float* sums, const GnShape p) {
+                                                    const T* beta, const T* dy, T* dx, float* out_a, float* out_b, const GnShape p) {
   typedef typename GnValue<T, FROM8>::type X;
   extern __shared__ __align__(16) float lds[];
   const uint32_t width = p.set_groups * p.dim;
   float* const items = lds;
-  float* const sum_a = lds + p.rows_at_once * width;
+  float* const gain = lds + p.rows_at_once * width;
+  float* const sum_a = gain + width;
   float* const sum_b = sum_a + width;
   float* const means = sum_b + width;   // [set_groups][2]
   const uint32_t b = gn_block(p.batch * p.sets), n = fast_div(b, p.div_sets), set = b - n * p.sets;
@@ -87,6 +139,7 @@ __global__ void __launch_bounds__(NT) k_gn_bwd_slab(const typename GnValue<T, FR
   }
   GnChannels<T, VEC, FROM8> ch;
   ch.load(p, l, n, set, centre, rstd, gamma, beta);
+  gn_keep_gain<VEC>(gain, l, ch.ga);
   auto valid = [&](int k) { return l.live && place + (uint32_t)k * step <= last; };
   float a[VEC], bb[VEC];
 #pragma unroll
@@ -100,42 +153,29 @@ __global__ void __launch_bounds__(NT) k_gn_bwd_slab(const typename GnValue<T, FR
     VecIo<T, VEC>::widen(rd[k], d);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-      const float xh = ch.normal(v[e], e);
-      const float dz = ch.template dz<ACT>(xh, d[e], e);
-      a[e] += valid(k) ? dz : 0.0f;
-      bb[e] += valid(k) ? dz * xh : 0.0f;
+      v[e] = ch.about_mean(v[e], e);
+      const float dz = valid(k) ? ch.template dz<ACT>(v[e], d[e], e) : 0.0f;
+      a[e] += dz;
+      bb[e] = __builtin_fmaf(dz, valid(k) ? v[e] : 0.0f, bb[e]);
     }
     done(a);
     done(bb);
   }
-  const uint32_t pitch = p.sum_pitch;
-  float* const out = sums + (size_t)n * 2u * pitch + set * width;
-  gn_channel_sums<VEC>(items, p, l, a, sum_a, out);
-  gn_channel_sums<VEC>(items, p, l, bb, sum_b, out + pitch);
-  // a wavefront per group
-  for (uint32_t g0 = 0; g0 < p.set_groups; g0 += NT / 64) {
-    const uint32_t g = g0 + (threadIdx.x >> 6), gc = min(g, p.set_groups - 1u);
-    float m1 = 0.0f, m2 = 0.0f;
-    for (uint32_t d = threadIdx.x & 63u; d < p.dim; d += 64u) {
-      const float w = load1(gamma + set * width + gc * p.dim + d);
-      m1 = __builtin_fmaf(w, sum_a[gc * p.dim + d], m1);
-      m2 = __builtin_fmaf(w, sum_b[gc * p.dim + d], m2);
-    }
-    m1 = group_allreduce<OpSum>(m1, 64);
-    m2 = group_allreduce<OpSum>(m2, 64);
-    if ((threadIdx.x & 63u) == 0 && g < p.set_groups) {
-      means[2u * g] = m1 * p.inv_count;
-      means[2u * g + 1u] = m2 * p.inv_count;
-    }
-  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) bb[e] *= ch.scale[e];
+  const size_t out = (size_t)n * 2u * p.sum_pitch + set * width;
+  gn_channel_sums<VEC>(items, p, l, a, gain, sum_a, out_a + out);
+  gn_channel_sums<VEC>(items, p, l, bb, gain, sum_b, out_b + out);
+  gn_group_means(p, sum_a, sum_b, [&](uint32_t g, float m1, float m2) {
+    means[2u * g] = m1;
+    means[2u * g + 1u] = m2;
+  });
   __syncthreads();
-  float m1[VEC], m2[VEC], r[VEC];
+  GnGradient<VEC> gr;
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
     const uint32_t g = fast_div(l.col + e, p.div_dim);
-    m1[e] = means[2u * g];
-    m2[e] = means[2u * g + 1u];
-    r[e] = FROM8 ? rstd[n * p.groups + set * p.set_groups + g] : ch.scale[e];
+    gr.set(e, ch, FROM8 ? rstd[n * p.groups + set * p.set_groups + g] : ch.scale[e], means[2u * g], means[2u * g + 1u]);
   }
 #pragma unroll
   for (int k = 0; k < K; ++k) {
@@ -147,18 +187,18 @@ __global__ void __launch_bounds__(NT) k_gn_bwd_slab(const typename GnValue<T, FR
     VecIo<T, VEC>::widen(rd[k], d);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-      const float xh = ch.normal(v[e], e);
-      const float dz = ch.template dz<ACT>(xh, d[e], e);
-      d[e] = (__builtin_fmaf(dz, ch.ga[e], -m1[e]) - xh * m2[e]) * r[e];
+      v[e] = ch.about_mean(v[e], e);
+      d[e] = gr.dx(v[e], ch.template dz<ACT>(v[e], d[e], e), e);
     }
-    VecIo<T, VEC>::store(near_element(dx + base, place + (uint32_t)k * step), d);
+    VecIo<T, VEC>::template store<false>(near_element(dx + base, place + (uint32_t)k * step), d);
   }
 }
 
-// ---- first launch of three: A and B of a chunk of positions ------------------------------------------------------------------
+// ---- first launch of two: A and B of a chunk of positions, and what they add to the group means --------------------------------
+// sums[batch][chunk][2][sum_pitch], means[batch][chunk][group][2]
 template <typename T, int VEC, int ACT, bool FROM8>
 __global__ void __launch_bounds__(256) k_gn_bwd_sums(const typename GnValue<T, FROM8>::type* x, const float* centre, const float* rstd, const T* gamma,
-                                                     const T* beta, const T* dy, float* out, const GnShape p) {
+                                                     const T* beta, const T* dy, float* sums, float* means, const GnShape p) {
   typedef typename GnValue<T, FROM8>::type X;
   extern __shared__ __align__(16) float lds[];
   constexpr int U = 4;
@@ -187,16 +227,17 @@ __global__ void __launch_bounds__(256) k_gn_bwd_sums(const typename GnValue<T, F
     issue();
     GnChannels<T, VEC, FROM8> ch;
     ch.load(p, l, n, set, centre, rstd, gamma, beta);
+    gn_keep_gain<VEC>(lds + p.rows_at_once * width, l, ch.ga);
     auto add = [&](typename VecIo<X, VEC>::Raw rx, typename VecIo<T, VEC>::Raw rd) {
       float v[VEC], d[VEC];
       VecIo<X, VEC>::widen(rx, v);
       VecIo<T, VEC>::widen(rd, d);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const float xh = ch.normal(v[e], e);
-        const float dz = ch.template dz<ACT>(xh, d[e], e);
+        v[e] = ch.about_mean(v[e], e);
+        const float dz = ch.template dz<ACT>(v[e], d[e], e);
         a[e] += dz;
-        b[e] = __builtin_fmaf(dz, xh, b[e]);
+        b[e] = __builtin_fmaf(dz, v[e], b[e]);
       }
       done(a);
       done(b);
@@ -212,77 +253,69 @@ __global__ void __launch_bounds__(256) k_gn_bwd_sums(const typename GnValue<T, F
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (row + u * step < r1) add(nx[u], nd[u]);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) b[e] *= ch.scale[e];
   }
-  float* const to = out + (size_t)bc * 2u * p.channels + set * width;
-  float* const spare = lds + p.rows_at_once * width;   // (the sums in LDS are not read here)
-  gn_channel_sums<VEC>(lds, p, l, a, spare, to);
-  gn_channel_sums<VEC>(lds, p, l, b, spare, to + p.channels);
+  float* const to = sums + (size_t)bc * 2u * p.sum_pitch + set * width;
+  float* const gain = lds + p.rows_at_once * width;
+  float* const sum_a = gain + width;
+  float* const sum_b = sum_a + width;
+  gn_channel_sums<VEC>(lds, p, l, a, gain, sum_a, to);
+  gn_channel_sums<VEC>(lds, p, l, b, gain, sum_b, to + p.sum_pitch);
+  float* const group_to = means + 2u * ((size_t)bc * p.groups + set * p.set_groups);
+  gn_group_means(p, sum_a, sum_b,
+                 [&](uint32_t g, float m1, float m2) { *reinterpret_cast<f32x2*>(group_to + 2u * g) = f32x2{m1, m2}; });
 }
 
-// ---- second launch: the chunks' sums added, the group means made ---------------------------------------------------------------
-// Workgroup (n, tile): join_cols channels (whole groups), 1 << fold_log2 lanes per channel.
-template <typename T>
-__global__ void __launch_bounds__(256) k_gn_bwd_join(const float* chunks, const T* gamma, float* sums, float* means, const GnShape p) {
-  extern __shared__ __align__(16) float lds[];   // [2][join_cols], weighted by gamma
-  const uint32_t tiles = (p.channels + p.join_cols - 1u) / p.join_cols;
-  const uint32_t n = blockIdx.x / tiles, c0 = (blockIdx.x - n * tiles) * p.join_cols, c1 = min(c0 + p.join_cols, p.channels);
-  const uint32_t lanes = 1u << p.fold_log2, at_once = 256u >> p.fold_log2;   // neighbouring threads: neighbouring channels
-  const uint32_t lane = threadIdx.x / at_once, own = threadIdx.x - lane * at_once;
-  __shared__ float part[2][256];
-  const float* const from = chunks + (size_t)n * p.chunks * 2u * p.channels;
-  const uint32_t pitch = p.sum_pitch;
-  for (uint32_t cb = c0; cb < c1; cb += at_once) {
-    const uint32_t c = min(cb + own, c1 - 1u);
-    float a = 0.0f, b = 0.0f;
-#pragma unroll 8
-    for (uint32_t k = lane; k < p.chunks; k += lanes) {
-      a += from[(size_t)k * 2u * p.channels + c];
-      b += from[((size_t)k * 2u + 1u) * p.channels + c];
+// ---- a launch between them, where every workgroup of the second one would add up too many chunks ---------------------------------
+// joined[batch][group][2], 1 << fold_log2 lanes each
+__device__ __forceinline__ f32x2 gn_bwd_join(const float* means, uint32_t n, uint32_t group, uint32_t lane, uint32_t lanes, const GnShape& p) {
+  const f32x2* const from = reinterpret_cast<const f32x2*>(means) + (size_t)n * p.chunks * p.groups + group;
+  constexpr int B = 16;   // loads that are under way together: their latency is what this costs
+  float m1 = 0.0f, m2 = 0.0f;
+  for (uint32_t c0 = lane; c0 - lane < p.chunks; c0 += B * lanes) {
+    f32x2 v[B];
+#pragma unroll
+    for (int i = 0; i < B; ++i) v[i] = from[(size_t)min(c0 + i * lanes, p.chunks - 1u) * p.groups];
+#pragma unroll
+    for (int i = 0; i < B; ++i) {
+      m1 += c0 + i * lanes < p.chunks ? v[i].x : 0.0f;
+      m2 += c0 + i * lanes < p.chunks ? v[i].y : 0.0f;
     }
-    part[0][threadIdx.x] = a;
-    part[1][threadIdx.x] = b;
-    __syncthreads();
-    if (lane == 0 && cb + own < c1) {
-      for (uint32_t k = 1; k < lanes; ++k) {
-        a += part[0][k * at_once + own];
-        b += part[1][k * at_once + own];
-      }
-      float* const out = sums + (size_t)n * 2u * pitch + c;
-      out[0] = a;
-      out[pitch] = b;
-      const float w = load1(gamma + c);
-      lds[c - c0] = w * a;
-      lds[p.join_cols + c - c0] = w * b;
-    }
-    __syncthreads();
   }
-  const uint32_t groups = (c1 - c0) / p.dim;
-  for (uint32_t g0 = 0; g0 < groups; g0 += 4u) {   // a wavefront per group
-    const uint32_t g = g0 + (threadIdx.x >> 6), gc = min(g, groups - 1u);
-    float m1 = 0.0f, m2 = 0.0f;
-    for (uint32_t d = threadIdx.x & 63u; d < p.dim; d += 64u) {
-      m1 += lds[gc * p.dim + d];
-      m2 += lds[p.join_cols + gc * p.dim + d];
-    }
-    m1 = group_allreduce<OpSum>(m1, 64);
-    m2 = group_allreduce<OpSum>(m2, 64);
-    if ((threadIdx.x & 63u) == 0 && g < groups)
-      *reinterpret_cast<f32x2*>(means + 2u * ((size_t)n * p.groups + c0 / p.dim + g)) = f32x2{m1 * p.inv_count, m2 * p.inv_count};
-  }
+  return f32x2{group_allreduce<OpSum>(m1, (int)lanes), group_allreduce<OpSum>(m2, (int)lanes)};
+}
+__global__ void __launch_bounds__(256) k_gn_bwd_join(const float* means, float* joined, const GnShape p) {
+  const uint32_t lanes = 1u << p.fold_log2, lane = threadIdx.x & (lanes - 1u);
+  const uint32_t own = blockIdx.x * (256u >> p.fold_log2) + (threadIdx.x >> p.fold_log2);
+  const uint32_t at = min(own, p.batch * p.groups - 1u), n = at / p.groups;
+  const f32x2 m = gn_bwd_join(means, n, at - n * p.groups, lane, lanes, p);
+  if (lane == 0 && own < p.batch * p.groups) *reinterpret_cast<f32x2*>(joined + 2u * (size_t)at) = m;
 }
 
-// ---- third launch ------------------------------------------------------------------------------------------------------
-template <typename T, int VEC, int ACT, bool FROM8>
+// ---- second launch -----------------------------------------------------------------------------------------------------
+// The first fold_blocks workgroups add up the chunks' A and B to dbeta and dgamma, beside the others.  JOIN: `means` are the
+// chunks', which every workgroup adds up for its groups.
+template <typename T, int VEC, int ACT, bool FROM8, bool JOIN>
 __global__ void __launch_bounds__(256) k_gn_bwd_apply(const typename GnValue<T, FROM8>::type* x, const float* centre, const float* rstd, const T* gamma,
-                                                      const T* beta, const T* dy, T* dx, const float* means, const GnShape p) {
+                                                      const T* beta, const T* dy, T* dx, const float* means, const float* sums, float* dbeta,
+                                                      float* dgamma, const GnShape p) {
   typedef typename GnValue<T, FROM8>::type X;
+  extern __shared__ __align__(16) float lds[];   // JOIN: [set_groups][2]; the fold's workgroups: 256 quads
+  if (blockIdx.x < p.fold_blocks) {
+    const uint32_t rows = p.batch * p.chunks, width = 2u * p.sum_pitch;
+    f32x4* const quads = reinterpret_cast<f32x4*>(lds);
+    if (rows > 128u) fold_tile<4, 64>(sums, dbeta, dgamma, rows, width, width, p.sum_pitch, p.channels, blockIdx.x, quads, kFoldF32);
+    else fold_tile<16, 16>(sums, dbeta, dgamma, rows, width, width, p.sum_pitch, p.channels, blockIdx.x, quads, kFoldF32);
+    return;
+  }
   constexpr int U = 4;
   const uint32_t width = p.set_groups * p.dim;
-  const uint32_t bc = fast_div(blockIdx.x, p.div_sets), set = blockIdx.x - bc * p.sets;
+  const uint32_t block = blockIdx.x - p.fold_blocks;   // (fold_blocks is a multiple of 8: on the die that read it for k_gn_bwd_sums)
+  const uint32_t bc = fast_div(block, p.div_sets), set = block - bc * p.sets;
   const uint32_t n = fast_div(bc, p.div_chunks), chunk = bc - n * p.chunks;
   const uint32_t r0 = chunk * p.chunk_rows, r1 = min(r0 + p.chunk_rows, p.positions);
   const GnLane l = gn_lane<VEC>(p);
-  if (!l.live) return;
   const size_t base = (size_t)n * p.positions * p.channels + set * width + l.col;
   const uint32_t step = p.rows_at_once;
   uint32_t row = r0 + l.row;
@@ -299,14 +332,22 @@ __global__ void __launch_bounds__(256) k_gn_bwd_apply(const typename GnValue<T, 
   issue();
   GnChannels<T, VEC, FROM8> ch;
   ch.load(p, l, n, set, centre, rstd, gamma, beta);
-  float m1[VEC], m2[VEC], r[VEC];
+  if constexpr (JOIN) {
+    const uint32_t lanes = 1u << p.fold_log2, sets = 256u >> p.fold_log2, lane = threadIdx.x & (lanes - 1u);
+    for (uint32_t g0 = 0; g0 < p.set_groups; g0 += sets) {
+      const uint32_t g = g0 + (threadIdx.x >> p.fold_log2);
+      const f32x2 m = gn_bwd_join(means, n, set * p.set_groups + min(g, p.set_groups - 1u), lane, lanes, p);
+      if (lane == 0 && g < p.set_groups) *reinterpret_cast<f32x2*>(lds + 2u * g) = m;
+    }
+    __syncthreads();
+  }
+  if (!l.live) return;
+  GnGradient<VEC> gr;
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
-    const uint32_t g = n * p.groups + set * p.set_groups + fast_div(l.col + e, p.div_dim);
-    const f32x2 m = *reinterpret_cast<const f32x2*>(means + 2u * (size_t)g);
-    m1[e] = m.x;
-    m2[e] = m.y;
-    r[e] = FROM8 ? rstd[g] : ch.scale[e];
+    const uint32_t g = fast_div(l.col + e, p.div_dim), at = n * p.groups + set * p.set_groups + g;
+    const f32x2 m = *reinterpret_cast<const f32x2*>(JOIN ? lds + 2u * g : means + 2u * (size_t)at);
+    gr.set(e, ch, FROM8 ? rstd[at] : ch.scale[e], m.x, m.y);
   }
   auto put = [&](typename VecIo<X, VEC>::Raw rx, typename VecIo<T, VEC>::Raw rd, uint32_t at) {
     float v[VEC], d[VEC];
@@ -314,9 +355,8 @@ __global__ void __launch_bounds__(256) k_gn_bwd_apply(const typename GnValue<T, 
     VecIo<T, VEC>::widen(rd, d);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-      const float xh = ch.normal(v[e], e);
-      const float dz = ch.template dz<ACT>(xh, d[e], e);
-      d[e] = (__builtin_fmaf(dz, ch.ga[e], -m1[e]) - xh * m2[e]) * r[e];
+      v[e] = ch.about_mean(v[e], e);
+      d[e] = gr.dx(v[e], ch.template dz<ACT>(v[e], d[e], e), e);
     }
     VecIo<T, VEC>::store(dx + base + at * p.channels, d);
   };
@@ -327,7 +367,11 @@ __global__ void __launch_bounds__(256) k_gn_bwd_apply(const typename GnValue<T, 
     row += U * step;
     issue();
 #pragma unroll
-    for (int u = 0; u < U; ++u) put(x0[u], d0[u], at + u * step);
+    for (int u = 0; u < U; ++u) {
+      again(x0[u]);
+      again(d0[u]);
+      put(x0[u], d0[u], at + u * step);
+    }
   }
 #pragma unroll
   for (int u = 0; u < U; ++u)
@@ -343,7 +387,8 @@ namespace {
 template <typename T, int VEC, int ACT, bool FROM8>
 const void* bwd_sym(int32_t kernel, const GroupNormP& p) {
   if (kernel == K_GN_BWD_SUMS) return (const void*)k_gn_bwd_sums<T, VEC, ACT, FROM8>;
-  if (kernel == K_GN_BWD_APPLY) return (const void*)k_gn_bwd_apply<T, VEC, ACT, FROM8>;
+  if (kernel == K_GN_BWD_APPLY)
+    return p.join ? (const void*)k_gn_bwd_apply<T, VEC, ACT, FROM8, true> : (const void*)k_gn_bwd_apply<T, VEC, ACT, FROM8, false>;
   if (p.threads == 256) {
     switch (p.vecs_per_lane) {
       case 1: return (const void*)k_gn_bwd_slab<T, VEC, 1, ACT, FROM8, 256>;
@@ -374,13 +419,13 @@ const void* bwd_act_sym(int32_t kernel, const GroupNormP& p) {
 }
 template <typename T>
 const void* bwd_type_sym(int32_t kernel, const GroupNormP& p) {
-  if (kernel == K_GN_BWD_JOIN) return (const void*)k_gn_bwd_join<T>;
   return p.vec == 1 ? bwd_act_sym<T, 1>(kernel, p) : bwd_act_sym<T, Elem<T>::VEC>(kernel, p);
 }
 }  // namespace
 
 const void* group_norm_backward_kernel_symbol(int32_t kernel, const KernelArgs& a) {
   const GroupNormP& p = a.u.gn;
+  if (kernel == K_GN_BWD_JOIN) return (const void*)k_gn_bwd_join;
   switch (p.dt) {
     case DT_F32: return bwd_type_sym<float>(kernel, p);
     case DT_F16: return bwd_type_sym<f16_t>(kernel, p);

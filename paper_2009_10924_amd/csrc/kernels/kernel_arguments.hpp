@@ -120,12 +120,12 @@ FS_SHARED void units_second_axis(TransposeP* p, uint32_t word, uint32_t d2, uint
 struct GnShape {
   uint32_t batch, positions, groups, dim, channels, set_groups, sets, set_vecs, rows_at_once, set_vecs_m;
   FastDiv div_dim, div_per, div_sets, div_chunks;
-  uint32_t chunk_rows, chunks, fold_log2, join_cols, sum_pitch;   // sum_pitch: floats between the sums of neighbouring rows
+  uint32_t chunk_rows, chunks, fold_log2, means_log2, fold_blocks, whole, sum_pitch;   // sum_pitch: floats between the sums of neighbouring rows
   float eps, inv_count, inv_max, tiny;
 };
 inline GnShape gn_shape(const GroupNormP& p) {
   return GnShape{p.batch, p.positions, p.groups, p.dim, p.channels, p.set_groups, p.sets, p.set_vecs, p.rows_at_once, p.set_vecs_m,
-                 p.div_dim, p.div_per, p.div_sets, p.div_chunks, p.chunk_rows, p.chunks, (uint32_t)p.fold_log2, p.join_cols, colsum_pitch(p.channels),
+                 p.div_dim, p.div_per, p.div_sets, p.div_chunks, p.chunk_rows, p.chunks, (uint32_t)p.fold_log2, (uint32_t)p.means_log2, p.fold_blocks, p.whole ? 1u : 0u, colsum_pitch(p.channels),
                  p.eps, p.inv_count, p.inv_max, p.tiny};
 }
 
@@ -238,11 +238,11 @@ __attribute__((always_inline)) inline bool list_arguments(int32_t kernel, const 
     case K_GN_SLAB: l->add(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], gn_shape(a.u.gn)); return true;
     case K_GN_STATS: l->add(p[0], p[1], gn_shape(a.u.gn)); return true;
     case K_GN_JOIN: l->add(p[0], p[1], p[2], p[3], p[4], gn_shape(a.u.gn)); return true;
-    case K_GN_APPLY: l->add(p[0], p[1], p[2], p[3], p[4], p[5], gn_shape(a.u.gn)); return true;
-    case K_GN_BWD_SLAB: l->add(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], gn_shape(a.u.gn)); return true;
-    case K_GN_BWD_SUMS: l->add(p[0], p[1], p[2], p[3], p[4], p[5], p[6], gn_shape(a.u.gn)); return true;
-    case K_GN_BWD_JOIN: l->add(p[0], p[1], p[2], p[3], gn_shape(a.u.gn)); return true;
-    case K_GN_BWD_APPLY: l->add(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], gn_shape(a.u.gn)); return true;
+    case K_GN_APPLY: l->add(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], gn_shape(a.u.gn)); return true;
+    case K_GN_BWD_SLAB: l->add(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], gn_shape(a.u.gn)); return true;
+    case K_GN_BWD_SUMS: l->add(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], gn_shape(a.u.gn)); return true;
+    case K_GN_BWD_JOIN: l->add(p[0], p[1], gn_shape(a.u.gn)); return true;
+    case K_GN_BWD_APPLY: l->add(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], gn_shape(a.u.gn)); return true;
     default: return false;
   }
 }

@@ -55,11 +55,11 @@ enum KernelId : int32_t {
   K_GN_SLAB,           // p0 x, p1 gamma, p2 beta, p3 y, p4 mean, p5 rstd, p6 q, p7 scales (p4 to p7: or null)
   K_GN_STATS,          // p0 x, p1 chunk statistics
   K_GN_JOIN,           // p0 chunk statistics, p1 joined statistics, p2 mean, p3 rstd, p4 scales (or null)
-  K_GN_APPLY,          // p0 x, p1 gamma, p2 beta, p3 joined statistics, p4 y, p5 q (or null)
-  K_GN_BWD_SLAB,       // p0 x or q, p1 mean or scales, p2 rstd, p3 gamma, p4 beta, p5 dy, p6 dx, p7 sums [batch, 2, pitch]
-  K_GN_BWD_SUMS,       // p0 x or q, p1 mean or scales, p2 rstd, p3 gamma, p4 beta, p5 dy, p6 chunk sums [batch, chunks, 2, C]
-  K_GN_BWD_JOIN,       // p0 chunk sums, p1 gamma, p2 sums [batch, 2, pitch], p3 group means [batch, G, 2]
-  K_GN_BWD_APPLY,      // p0 x or q, p1 mean or scales, p2 rstd, p3 gamma, p4 beta, p5 dy, p6 dx, p7 group means
+  K_GN_APPLY,          // p0 x, p1 gamma, p2 beta, p3 chunk or joined statistics, p4 y, p5 q, p6 mean, p7 rstd, p8 scales (p5 to p8: or null)
+  K_GN_BWD_SLAB,       // p0 x or q, p1 mean or scales, p2 rstd, p3 gamma, p4 beta, p5 dy, p6 dx, p7 and p8 sums A and B, a row of 2 * pitch floats per batch entry
+  K_GN_BWD_SUMS,       // p0 x or q, p1 mean or scales, p2 rstd, p3 gamma, p4 beta, p5 dy, p6 chunk sums [batch, chunks, 2, pitch], p7 chunk means [batch, chunks, G, 2]
+  K_GN_BWD_JOIN,       // p0 chunk means, p1 group means [batch, G, 2]
+  K_GN_BWD_APPLY,      // p0 x or q, p1 mean or scales, p2 rstd, p3 gamma, p4 beta, p5 dy, p6 dx, p7 chunk or group means, p8 chunk sums, p9 dbeta, p10 dgamma
   K_COUNT
 };
 
@@ -187,6 +187,7 @@ struct CheckpointP {
   uint32_t n_row_blocks;
   int32_t stream;
 };
+constexpr uint32_t kGnMostRows = 128;   // positions of a chunk that one thread may have (see k_gn_stats)
 struct GroupNormP {
   int32_t dt, act;                  // x / y / dy / dx / gamma / beta share dt; statistics and sums are float32
   int32_t checkpoint;               // forward: q and its scales are written; backward: they are read instead of x and the mean
@@ -198,10 +199,12 @@ struct GroupNormP {
   uint32_t set_vecs_m;              // ceil(2^20 / set_vecs)
   FastDiv div_dim, div_per;         // by dim; by the items a position leaves in LDS for one group
   FastDiv div_sets, div_chunks;
-  int32_t fold_log2;                // log2 of the lanes that fold one group's items
+  int32_t fold_log2;                // log2 of the lanes that fold one group's items (one channel's in the backward kernels)
+  int32_t means_log2;               // backward: ... that add up one group's channels
   uint32_t chunk_rows, chunks;      // positions per chunk
   int32_t threads, vecs_per_lane;
-  uint32_t join_cols;               // K_GN_BWD_JOIN: channels of a workgroup, whole groups
+  int32_t join;                     // last launch: 1 = it joins the chunks itself
+  uint32_t fold_blocks;             // K_GN_BWD_APPLY: workgroups that add up the chunks' sums
   float eps, inv_count, inv_max, tiny;   // inv_count = 1 / (positions * dim)
   int32_t stream;
 };

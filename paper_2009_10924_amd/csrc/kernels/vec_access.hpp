@@ -6,6 +6,13 @@
 
 namespace fsk {
 
+// STREAM: with the streaming hint; without it where neighbouring workgroups write the rest of a line (the cache then puts it
+// together, with the hint every piece goes to memory by itself).
+template <bool STREAM, typename V, typename P> __device__ __forceinline__ void put(V v, P* p) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+  else *p = v;
+}
+
 template <typename T, int VEC> struct VecIo {
   static_assert(VEC == Elem<T>::VEC, "a whole vector, or one element");
   typedef u32x4 Raw;
@@ -15,19 +22,21 @@ template <typename T, int VEC> struct VecIo {
     return STREAM ? __builtin_nontemporal_load(q) : *q;
   }
   __device__ __forceinline__ static void widen(Raw r, float (&v)[VEC]) { unpack(r, v, (const T*)nullptr); }
-  __device__ __forceinline__ static void store(T* p, const float (&v)[VEC]) {
+  template <bool STREAM = true> __device__ __forceinline__ static void store(T* p, const float (&v)[VEC]) {
     u32x4 w;
     if constexpr (sizeof(T) == 4) w = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
     else w = u32x4{pack2(v[0], v[1], (const T*)nullptr), pack2(v[2], v[3], (const T*)nullptr), pack2(v[4], v[5], (const T*)nullptr),
                    pack2(v[6], v[7], (const T*)nullptr)};
-    __builtin_nontemporal_store(w, reinterpret_cast<Place*>(p));
+    put<STREAM>(w, reinterpret_cast<Place*>(p));
   }
 };
 template <typename T> struct VecIo<T, 1> {
   typedef float Raw;
   template <bool STREAM> __device__ __forceinline__ static Raw load(const T* p) { return load1(p); }
   __device__ __forceinline__ static void widen(Raw r, float (&v)[1]) { v[0] = r; }
-  __device__ __forceinline__ static void store(T* p, const float (&v)[1]) { store1(p, v[0]); }
+  template <bool STREAM = true> __device__ __forceinline__ static void store(T* p, const float (&v)[1]) { put1(p, v[0]); }
+  template <typename U> __device__ __forceinline__ static void put1(U* p, float v) { store1(p, v); }
+  __device__ __forceinline__ static void put1(e4m3_t* p, float v) { store1_in_range(p, v); }
 };
 template <> struct VecIo<e4m3_t, 8> {
   typedef u32x2 Raw;
@@ -40,9 +49,9 @@ template <> struct VecIo<e4m3_t, 8> {
     unpack_e4m3(r.x, v[0], v[1], v[2], v[3]);
     unpack_e4m3(r.y, v[4], v[5], v[6], v[7]);
   }
-  __device__ __forceinline__ static void store(e4m3_t* p, const float (&v)[8]) {
-    const u32x2 w = {pack_e4m3(v[0], v[1], v[2], v[3]), pack_e4m3(v[4], v[5], v[6], v[7])};
-    __builtin_nontemporal_store(w, reinterpret_cast<Place*>(p));
+  template <bool STREAM = true> __device__ __forceinline__ static void store(e4m3_t* p, const float (&v)[8]) {
+    const u32x2 w = {pack_e4m3_in_range(v[0], v[1], v[2], v[3]), pack_e4m3_in_range(v[4], v[5], v[6], v[7])};
+    put<STREAM>(w, reinterpret_cast<Place*>(p));
   }
 };
 template <> struct VecIo<e4m3_t, 4> {
@@ -53,8 +62,8 @@ template <> struct VecIo<e4m3_t, 4> {
     return STREAM ? __builtin_nontemporal_load(q) : *q;
   }
   __device__ __forceinline__ static void widen(Raw r, float (&v)[4]) { unpack_e4m3(r, v[0], v[1], v[2], v[3]); }
-  __device__ __forceinline__ static void store(e4m3_t* p, const float (&v)[4]) {
-    __builtin_nontemporal_store(pack_e4m3(v[0], v[1], v[2], v[3]), reinterpret_cast<Place*>(p));
+  template <bool STREAM = true> __device__ __forceinline__ static void store(e4m3_t* p, const float (&v)[4]) {
+    put<STREAM>(pack_e4m3_in_range(v[0], v[1], v[2], v[3]), reinterpret_cast<Place*>(p));
   }
 };
 

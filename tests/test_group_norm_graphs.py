@@ -21,10 +21,10 @@ def test_every_shape_has_a_plan(act, dtype):
     for shape in SHAPES:
         for keep in ("none", "stats", "checkpoint"):
             p = plan(group_norm_graph(*shape, dtype=dtype, act=act, keep=keep))
-            assert p.info["pattern"] == "group_norm" and p.info["n_kernels"] in (1, 3), shape
+            assert p.info["pattern"] == "group_norm" and p.info["n_kernels"] in (1, 2, 3), shape
             if keep != "none":
                 p = plan(group_norm_backward_graph(*shape, dtype=dtype, act=act, keep=keep))
-                assert p.info["pattern"] == "group_norm_backward" and p.info["n_kernels"] in (2, 4), shape
+                assert p.info["pattern"] == "group_norm_backward" and p.info["n_kernels"] in (1, 2, 3), shape
                 assert "at_once" not in p.describe()
 
 
@@ -68,7 +68,7 @@ def test_backward_axes_and_what_is_not_it():
 
 def test_workspace_and_scratch_are_checked():
     p = plan(group_norm_graph(16, 16384, 32, 8, "bf16", "silu", "stats"))
-    assert p.info["n_kernels"] == 3 and p.info["workspace_bytes"] > 0
+    assert p.info["n_kernels"] in (2, 3) and p.info["workspace_bytes"] > 0
     with pytest.raises(B.FsError, match="FS_ERR_WORKSPACE"):
         p.execute_ptrs([0x1000] * 3, [0x1000] * 3, 0x1000, p.info["workspace_bytes"] - 1, 0)
     with pytest.raises(B.FsError, match="FS_ERR_ALIGN"):
