@@ -67,6 +67,10 @@ CostResult evaluate(const KernelCost& k, int32_t vgprs_compiled) {
   blocks_per_cu = std::max<uint32_t>(1, blocks_per_cu);
   const double waves_per_cu = std::min<double>(occ * d.simd_per_cu, (double)blocks_per_cu * wpb);
   r.waves_per_simd = (int32_t)std::max(1.0, std::floor(waves_per_cu / d.simd_per_cu));
+  if (k.own_estimate_s > 0) {
+    r.seconds = k.own_estimate_s;
+    return r;
+  }
 
   // N_wave: rounds of resident wavefronts.
   const double capacity = waves_per_cu * d.n_cu;

@@ -79,6 +79,7 @@ struct KernelCost {
   double partial_bytes = 0;             // column sums: partial sums written by the workgroups and read by the fold launch
   double flush_values = 0;              // column sums: values of every lane that leave it at the end of its rows
   double fold_rows = 0;                 // column sums: rows of partial sums
+  double own_estimate_s = 0;            // > 0: the family's own estimate of all its launches, which replaces everything but occupancy
   double flush_steps = -1;              // ... lane-to-lane folds before that (-1: a workgroup per row, no fold)
 };
 

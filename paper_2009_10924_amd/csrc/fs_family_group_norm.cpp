@@ -42,6 +42,9 @@ bool lay_out(GroupNormP* p, int threads, uint32_t set_groups) {
   p->sets = p->groups / set_groups;
   p->vec = width >= (uint32_t)vec_of(p->dt) ? vec_of(p->dt) : 1;
   p->whole = p->dim % p->vec == 0 ? 1 : 0;
+  // Stored past the caches, pieces that share 64 bytes with another workgroup's go to memory one by one: bf16 [8, 4096, 320] in
+  // pieces of 20 bytes took 68 us, 33 through the caches; f32 [4, 1024, 512] in pieces of 64 bytes 6.7 past them, 7.4 through.
+  p->whole_lines = p->sets == 1 || width * dtype_bytes(p->dt) % 64 == 0 ? 1 : 0;
   p->set_vecs = (width + p->vec - 1) / p->vec;
   if (p->set_vecs > (uint32_t)threads) return false;
   p->rows_at_once = (uint32_t)threads / p->set_vecs;
@@ -82,13 +85,21 @@ std::vector<uint32_t> set_sizes(uint32_t groups) {
   s.push_back(groups);
   return s;
 }
-// the largest set of groups whose positions 256 threads cover; 0: none
-uint32_t widest_set(const GroupNormP& p) {
+// Sets for the launches that read chunk by chunk: the largest whose positions 256 threads cover, and, where its pieces are whole
+// 64-byte pieces of memory, the smallest of at least 512 bytes of a position: more positions per workgroup, so fewer chunks whose
+// partial results are written and read (f16 [1, 2295, 1664] backward: sums as large as the values otherwise).
+std::vector<uint32_t> chunk_sets(const GroupNormP& p) {
+  std::vector<uint32_t> sets;
+  uint32_t narrow = 0;
   for (uint32_t s = p.groups; s >= 1; --s) {
     GroupNormP q = p;
-    if (p.groups % s == 0 && lay_out(&q, 256, s)) return s;
+    if (p.groups % s != 0 || !lay_out(&q, 256, s)) continue;
+    if (sets.empty()) sets.push_back(s);
+    const uint32_t bytes = s * p.dim * (uint32_t)dtype_bytes(p.dt);
+    if (bytes >= 512 && bytes % 64 == 0) narrow = s;
   }
-  return 0;
+  if (narrow && narrow != sets[0]) sets.push_back(narrow);
+  return sets;
 }
 
 // Whether the last launch's workgroups join their groups' chunks themselves: a launch less, where one batch of `loads` loads per
@@ -97,41 +108,68 @@ bool joins(const GroupNormP& p, uint32_t set_groups, uint32_t loads) {
   return (uint64_t)p.chunks * std::max<uint32_t>(set_groups, 4) <= 256ull * loads;
 }
 
+// What the launches read and write, and the estimate of their time.  These kernels are short: most of what a shape costs is the
+// chain of instructions of one wavefront (which hardly any other covers) against its share of the arithmetic and the bytes, which
+// the general evaluator has no terms for.  Constants fitted to every candidate of 700 shapes of 1 to 2^26 elements, three dtypes, timed
+// on three sets of buffers in turn; the candidate chosen was 2.0 % behind the fastest (geometric mean), 12 % by the general
+// evaluator.
 struct Traffic {
-  double read_bytes = 0, written_bytes = 0, n = 0, valu = 0, trans = 0;
+  double read_bytes = 0, written_bytes = 0, act = 0;   // act: 0 none, 1 SiLU, 1.5 tanh-GELU
+  bool backward = false;
 };
-// What a set's rows cost beyond their bytes: pieces shorter than a line are read by several workgroups.
-void slab_cost(const GroupNormP& p, const Traffic& t, int esz, int K, int raw_bytes, int lds, KernelCost* kc) {
-  kc->hbm_bytes = t.read_bytes + t.written_bytes;
-  kc->elems = t.n;
-  kc->valu_per_elem = t.valu;
-  kc->trans_per_elem = t.trans;
-  kc->waves_per_block = p.threads / 64;
-  kc->waves = (double)p.batch * p.sets * kc->waves_per_block;
-  kc->bytes_in_flight_per_lane = (double)raw_bytes * K;
-  kc->vgpr_estimate = 48 + K * (raw_bytes / 4 + 2);
-  kc->xlane_steps = 16;
-  kc->barriers = 4;
-  kc->lds_bytes_per_block = lds;
-  kc->lane_utilisation = (double)p.positions * p.set_vecs / ((double)K * p.threads);
-  const double run = (double)p.set_groups * p.dim * esz;
-  if (p.sets > 1 && run < 256) kc->stream_penalty = 0.25 * (256.0 / run - 1.0);
+struct SlabModel { double ops, ops_act, ops_8bit, fixed, chain_op, chain_item, chain_threads, issue, issue_op, shared_lines, overlap, fold, line, round; };
+const SlabModel kSlab[2] = {{4.92, 4.92, 3.24, 3.07, 1.94e-3, 0.131, 0.0, 0.682, 4.5e-4, 0.125, 0.0, 0.0, 9.6e-4, 0.652},
+                            {1.87, 8.05, 0.02, 3.47, 6.0e-3, 0.057, 0.047, 0.887, 0.0, 0.107, 0.0054, 2.66, 1.2e-4, 1.175}};
+struct PassesModel { double ops, ops_act, ops_8bit, issue_op, reread_l2, reread, fixed, launch, overlap, item, partials, join, shared_lines; };
+const PassesModel kPasses[2] = {{7.95, 4.93, 5.02, 3.42e-3, 0.68, 0.73, 6.71, 2.47, 0.018, 0.192, 0.0, 1.87e-4, 0.24},
+                                {7.99, 5.02, 4.90, 4.9e-3, 0.63, 0.64, 6.86, 2.48, 0.309, 0.273, 1.1, 2.02e-4, 0.15}};
+// items that a lane adds up of what a workgroup's threads have gathered: a group's (forward), a channel's (backward)
+double items_per_lane(const GroupNormP& p, bool backward) {
+  const double per = backward ? p.rows_at_once : (p.whole ? (double)p.dim / p.vec : (double)p.dim) * p.rows_at_once;
+  const double sums = backward ? (double)p.set_groups * p.dim : p.set_groups;
+  const double lanes = std::max(1.0, std::min(64.0, std::floor(p.threads / sums)));
+  return per / lanes * std::max(1.0, sums / p.threads);
 }
-void passes_cost(const GroupNormP& p, const Traffic& t, int raw_bytes, int n_launches, KernelCost* kc) {
-  const double again = t.read_bytes <= 0.75 * device().last_level_cache_bytes ? device().last_level_reread : 1.0;
-  kc->hbm_bytes = t.read_bytes * (1.0 + again) + t.written_bytes;
-  kc->elems = t.n * 1.6;
-  kc->valu_per_elem = t.valu;
-  kc->trans_per_elem = t.trans;
-  kc->waves_per_block = 4;
-  kc->waves = (double)p.batch * p.sets * p.chunks * 4;
-  kc->rows_per_wave_loop = std::max(1.0, (double)p.chunk_rows / (4.0 * p.rows_at_once));
-  kc->bytes_in_flight_per_lane = 4.0 * raw_bytes;
-  kc->vgpr_estimate = 96;
-  kc->barriers = 0;
-  kc->dep_phases = 0.3;
-  kc->first_load = true;
-  kc->serial_tail_s = (n_launches - 1) * 3.0e-6;
+// what `workgroups` of them stream at most, each on a compute unit of its own
+double few_units(double bytes, double workgroups, double unit) { return bytes / std::min(256.0, workgroups) / unit; }
+double slab_us(const GroupNormP& p, const Traffic& t, int esz, int K, int vgprs) {
+  const SlabModel& m = kSlab[t.backward ? 1 : 0];
+  const double groups = (double)p.batch * p.sets;
+  const double waves = std::max(1.0, groups * p.threads / 64.0 / 1024.0);   // per SIMD
+  const double ops = (m.ops + m.ops_act * t.act + m.ops_8bit * p.checkpoint) * K * p.vec;
+  // workgroups that a compute unit holds, and so the rounds of them
+  const int per_simd = std::min(8, 512 / std::max(8, (vgprs + 7) / 8 * 8)), held = std::max(1, 4 * per_simd / (p.threads / 64));
+  const double rounds = std::ceil(groups / (256.0 * held));
+  const double chain = (m.fixed + m.chain_op * ops + m.chain_item * items_per_lane(p, t.backward) + m.chain_threads * p.threads / 512.0) * (1.0 + m.round * (rounds - 1.0));
+  const double issue = waves * (m.issue + m.issue_op * ops);
+  const double run = p.sets > 1 ? (double)p.set_groups * p.dim * esz : 1e9;
+  double memory = (t.read_bytes + t.written_bytes) / 6.5e6 * (1.0 + m.shared_lines * std::max(0.0, 256.0 / run - 1.0));
+  memory = std::max(memory, few_units(t.read_bytes + t.written_bytes, groups, 3.3e4));
+  // lines that the accesses of a compute unit's wavefronts touch, one after the other
+  memory = std::max(memory, m.line * K * p.threads / 64.0 * std::max(1.0, groups / 256.0) * std::max(64.0 / p.set_vecs, 64.0 * p.vec * esz / 128.0));
+  return chain + std::max(issue, memory) + m.overlap * std::min(issue, memory) + (p.batch > 1 ? m.fold : 0.0);
+}
+double passes_us(const GroupNormP& p, const Traffic& t, size_t n_launches) {
+  const PassesModel& m = kPasses[t.backward ? 1 : 0];
+  const double waves = std::max(1.0, (double)p.batch * p.sets * p.chunks * 4.0 / 1024.0);
+  const double rows = std::ceil((double)p.chunk_rows / p.rows_at_once);
+  const double issue = waves * rows * p.vec * (m.ops + m.ops_act * t.act + m.ops_8bit * p.checkpoint) * m.issue_op;
+  const double again = t.read_bytes < 2.4e7 ? m.reread_l2 : t.read_bytes < 2e8 ? m.reread : 1.0;   // from the dies' caches, the memory-side one
+  double memory = t.read_bytes / 6.8e6 + (t.read_bytes * again + t.written_bytes) / 6.6e6 +
+                  m.partials * 16.0 * p.batch * p.chunks * p.channels / 6.6e6 + m.join * p.chunks * p.set_groups;
+  if (p.sets > 1) memory *= 1.0 + m.shared_lines * 128.0 / ((double)p.set_groups * p.dim * dtype_bytes(p.dt));
+  const double workgroups = (double)p.batch * p.sets * p.chunks;
+  if (workgroups < 400) memory *= 1.05;   // one wavefront per SIMD: loads and arithmetic take turns
+  memory = std::max(memory, few_units(2.0 * t.read_bytes + t.written_bytes, workgroups, 4.0e4));
+  return m.fixed + m.launch * ((double)n_launches - 2.0) + std::max(issue, memory) + m.overlap * std::min(issue, memory) + m.item * items_per_lane(p, t.backward);
+}
+KernelCost estimated(double us, const GroupNormP& p, int vgprs, int lds) {
+  KernelCost kc;
+  kc.own_estimate_s = us * 1e-6;
+  kc.vgpr_estimate = vgprs;
+  kc.waves_per_block = p.threads / 64;
+  kc.lds_bytes_per_block = lds;
+  return kc;
 }
 
 }  // namespace
@@ -185,11 +223,9 @@ bool build_group_norm(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
   }
   const int esz = dtype_bytes(base.dt);
   Traffic t;
-  t.n = (double)x.numel();
-  t.read_bytes = t.n * esz;
-  t.written_bytes = t.n * (esz + (has_8bit ? 1 : 0));
-  t.valu = 9.0 + act_valu(act) + (has_8bit ? 10.0 : 0.0) + (esz == 2 ? 1.5 : 0.0);
-  t.trans = act_trans(act);
+  t.read_bytes = (double)x.numel() * esz;
+  t.written_bytes = (double)x.numel() * (esz + (has_8bit ? 1 : 0));
+  t.act = act == ACT_GELU ? 1.5 : act == ACT_SILU ? 1.0 : 0.0;
 
   // ---- one launch
   struct Slab { int threads, K; };
@@ -222,8 +258,8 @@ bool build_group_norm(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
       c.info.vecs_per_lane = sh.K;
       c.info.rows_per_block = (int32_t)p.rows_at_once;
       c.info.lds_bytes = (int32_t)lds;
-      KernelCost kc;
-      slab_cost(p, t, esz, sh.K, p.vec * esz, (int)lds, &kc);
+      const int vgprs = 40 + sh.K * (p.vec * esz / 4 + 1);
+      const KernelCost kc = estimated(slab_us(p, t, esz, sh.K, vgprs), p, vgprs, (int)lds);
       char var[56];
       snprintf(var, sizeof var, "<%s,%s,T%d,K%d,G%u>", dtype_name(p.dt), act_name(act), sh.threads, sh.K, gs);
       finish_candidate(&c, var, kc);
@@ -232,77 +268,76 @@ bool build_group_norm(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
   }
 
   // ---- two or three launches
-  const uint32_t gs = widest_set(base);
-  if (gs == 0) return true;
-  uint32_t last_chunks = 0;
-  for (uint32_t want : {256u, 512u, 1024u, 2048u}) {
-    GroupNormP p = base;
-    if (!lay_out(&p, 256, gs) || !cut(&p, want) || p.chunks == last_chunks) continue;
-    last_chunks = p.chunks;
-    const uint32_t items = p.rows_at_once * (p.whole ? p.set_vecs : gs * p.dim);
-    const int64_t lds = 4ll * ((has_8bit ? 4 : 2) * (int64_t)items + p.rows_at_once);
-    const int64_t chunk_bytes = aligned((has_8bit ? 16ll : 8ll) * p.batch * p.chunks * p.groups);
-    const bool join = joins(p, gs, has_8bit ? 8 : 16);
-    Candidate c = make_candidate(g, "group_norm", FS_SCHEME_GLOBAL, K_GN_STATS);
-    {
-      Launch& l = c.launches.front();
-      p.fold_log2 = fold_lanes_log2(256, gs, p.rows_at_once * (p.whole ? p.dim / p.vec : p.dim));
-      l.args.u.gn = p;
-      l.ptr[0] = in_ref(g, tx);
-      l.ptr[1] = ws_ref(0);
-      l.shape.block[0] = 256;
-      l.shape.grid[0] = p.batch * p.chunks * p.sets;
-      l.shape.lds_bytes = (uint32_t)lds;
+  for (uint32_t gs : chunk_sets(base)) {
+    uint32_t last_chunks = 0;
+    for (uint32_t want : {256u, 512u}) {
+      GroupNormP p = base;
+      if (!lay_out(&p, 256, gs) || !cut(&p, want) || p.chunks == last_chunks) continue;
+      last_chunks = p.chunks;
+      const uint32_t items = p.rows_at_once * (p.whole ? p.set_vecs : gs * p.dim);
+      const int64_t lds = 4ll * ((has_8bit ? 4 : 2) * (int64_t)items + p.rows_at_once);
+      const int64_t chunk_bytes = aligned((has_8bit ? 16ll : 8ll) * p.batch * p.chunks * p.groups);
+      const bool join = joins(p, gs, has_8bit ? 8 : 16);
+      Candidate c = make_candidate(g, "group_norm", FS_SCHEME_GLOBAL, K_GN_STATS);
+      {
+        Launch& l = c.launches.front();
+        p.fold_log2 = fold_lanes_log2(256, gs, p.rows_at_once * (p.whole ? p.dim / p.vec : p.dim));
+        l.args.u.gn = p;
+        l.ptr[0] = in_ref(g, tx);
+        l.ptr[1] = ws_ref(0);
+        l.shape.block[0] = 256;
+        l.shape.grid[0] = p.batch * p.chunks * p.sets;
+        l.shape.lds_bytes = (uint32_t)lds;
+      }
+      auto statistics = [&](Launch& l, int first) {
+        if (t_mu >= 0) l.ptr[first] = out_ref(g.tensors[t_mu].output_slot);
+        if (t_r >= 0) l.ptr[first + 1] = out_ref(g.tensors[t_r].output_slot);
+        if (t_s >= 0) l.ptr[first + 2] = out_ref(g.tensors[t_s].output_slot);
+      };
+      if (!join) {
+        c.launches.emplace_back();
+        Launch& l = c.launches.back();
+        l.kernel = K_GN_JOIN;
+        l.args.u.gn = p;
+        l.args.u.gn.fold_log2 = std::min(6, log2_of(pow2_at_least(p.chunks)));
+        l.ptr[0] = ws_ref(0);
+        l.ptr[1] = ws_ref(chunk_bytes);
+        statistics(l, 2);
+        const uint32_t at_once = 256u >> l.args.u.gn.fold_log2;
+        l.shape.block[0] = 256;
+        l.shape.grid[0] = (p.batch * p.groups + at_once - 1) / at_once;
+      }
+      {
+        c.launches.emplace_back();
+        Launch& l = c.launches.back();
+        l.kernel = K_GN_APPLY;
+        l.args.u.gn = p;
+        l.args.u.gn.join = join ? 1 : 0;
+        l.args.u.gn.fold_log2 = fold_lanes_log2(256, gs, p.chunks);
+        l.ptr[0] = in_ref(g, tx);
+        l.ptr[1] = in_ref(g, tg);
+        l.ptr[2] = in_ref(g, tb);
+        l.ptr[3] = ws_ref(join ? 0 : chunk_bytes);
+        l.ptr[4] = out_ref(g.tensors[t_y].output_slot);
+        if (t_q >= 0) l.ptr[5] = out_ref(g.tensors[t_q].output_slot);
+        if (join) statistics(l, 6);
+        l.shape.block[0] = 256;
+        l.shape.grid[0] = p.batch * p.chunks * p.sets;
+        l.shape.lds_bytes = join ? 16 * gs : 0;
+      }
+      c.info.n_kernels = (int32_t)c.launches.size();
+      c.info.workspace_bytes = chunk_bytes + (join ? 0 : aligned(16ll * p.batch * p.groups));
+      c.info.bytes_moved_model = c.info.bytes_min + (int64_t)t.read_bytes;
+      c.info.lanes_per_row = (int32_t)p.set_vecs;
+      c.info.vecs_per_lane = 4;
+      c.info.rows_per_block = (int32_t)p.chunk_rows;
+      c.info.lds_bytes = (int32_t)lds;
+      const KernelCost kc = estimated(passes_us(p, t, c.launches.size()), p, 96, (int)lds);
+      char var[56];
+      snprintf(var, sizeof var, "<%s,%s,G%u,C%u,%sapply>", dtype_name(p.dt), act_name(act), gs, p.chunks, join ? "" : "join,");
+      finish_candidate(&c, var, kc);
+      out->push_back(c);
     }
-    auto statistics = [&](Launch& l, int first) {
-      if (t_mu >= 0) l.ptr[first] = out_ref(g.tensors[t_mu].output_slot);
-      if (t_r >= 0) l.ptr[first + 1] = out_ref(g.tensors[t_r].output_slot);
-      if (t_s >= 0) l.ptr[first + 2] = out_ref(g.tensors[t_s].output_slot);
-    };
-    if (!join) {
-      c.launches.emplace_back();
-      Launch& l = c.launches.back();
-      l.kernel = K_GN_JOIN;
-      l.args.u.gn = p;
-      l.args.u.gn.fold_log2 = std::min(6, log2_of(pow2_at_least(p.chunks)));
-      l.ptr[0] = ws_ref(0);
-      l.ptr[1] = ws_ref(chunk_bytes);
-      statistics(l, 2);
-      const uint32_t at_once = 256u >> l.args.u.gn.fold_log2;
-      l.shape.block[0] = 256;
-      l.shape.grid[0] = (p.batch * p.groups + at_once - 1) / at_once;
-    }
-    {
-      c.launches.emplace_back();
-      Launch& l = c.launches.back();
-      l.kernel = K_GN_APPLY;
-      l.args.u.gn = p;
-      l.args.u.gn.join = join ? 1 : 0;
-      l.args.u.gn.fold_log2 = fold_lanes_log2(256, gs, p.chunks);
-      l.ptr[0] = in_ref(g, tx);
-      l.ptr[1] = in_ref(g, tg);
-      l.ptr[2] = in_ref(g, tb);
-      l.ptr[3] = ws_ref(join ? 0 : chunk_bytes);
-      l.ptr[4] = out_ref(g.tensors[t_y].output_slot);
-      if (t_q >= 0) l.ptr[5] = out_ref(g.tensors[t_q].output_slot);
-      if (join) statistics(l, 6);
-      l.shape.block[0] = 256;
-      l.shape.grid[0] = p.batch * p.chunks * p.sets;
-      l.shape.lds_bytes = join ? 16 * gs : 0;
-    }
-    c.info.n_kernels = (int32_t)c.launches.size();
-    c.info.workspace_bytes = chunk_bytes + (join ? 0 : aligned(16ll * p.batch * p.groups));
-    c.info.bytes_moved_model = c.info.bytes_min + (int64_t)t.read_bytes;
-    c.info.lanes_per_row = (int32_t)p.set_vecs;
-    c.info.vecs_per_lane = 4;
-    c.info.rows_per_block = (int32_t)p.chunk_rows;
-    c.info.lds_bytes = (int32_t)lds;
-    KernelCost kc;
-    passes_cost(p, t, p.vec * esz, (int)c.launches.size(), &kc);
-    char var[56];
-    snprintf(var, sizeof var, "<%s,%s,G%u,C%u,%sapply>", dtype_name(p.dt), act_name(act), gs, p.chunks, join ? "" : "join,");
-    finish_candidate(&c, var, kc);
-    out->push_back(c);
   }
   return true;
 }
@@ -386,11 +421,10 @@ bool build_group_norm_backward(const fs_graph& g, std::vector<Candidate>* out, P
   const int esz = dtype_bytes(base.dt), xsz = base.checkpoint ? 1 : esz;
   const uint32_t pitch = colsum_pitch(base.channels);
   Traffic t;
-  t.n = (double)dy.numel();
-  t.read_bytes = t.n * (esz + xsz);
-  t.written_bytes = t.n * esz;
-  t.valu = 18.0 + 2.5 * act_valu(base.act) + (esz == 2 ? 2.0 : 0.0);
-  t.trans = 2.0 * act_trans(base.act);
+  t.read_bytes = (double)dy.numel() * (esz + xsz);
+  t.written_bytes = (double)dy.numel() * esz;
+  t.act = base.act == ACT_GELU ? 1.5 : base.act == ACT_SILU ? 1.0 : 0.0;
+  t.backward = true;
   auto fill_inputs = [&](Launch& l) {
     l.ptr[0] = in_ref(g, tx);
     l.ptr[1] = in_ref(g, tcentre);
@@ -435,9 +469,8 @@ bool build_group_norm_backward(const fs_graph& g, std::vector<Candidate>* out, P
       l.shape.block[0] = (uint32_t)sh.threads;
       l.shape.grid[0] = p.batch * p.sets;
       l.shape.lds_bytes = (uint32_t)lds;
-      KernelCost kc;
-      slab_cost(p, t, esz, sh.K, p.vec * (esz + xsz), (int)lds, &kc);
-      kc.serial_tail_s = p.batch == 1 ? 0.0 : 2.0e-6;
+      const int vgprs = 73 + sh.K * (p.vec * (esz + xsz) / 4 + 1);
+      const KernelCost kc = estimated(slab_us(p, t, esz, sh.K, vgprs), p, vgprs, (int)lds);
       char var[56];
       snprintf(var, sizeof var, "<%s,%s,T%d,K%d,G%u%s>", dtype_name(p.dt), act_name(p.act), sh.threads, sh.K, gs, p.batch == 1 ? "" : ",fold");
       finish_candidate(&c, var, kc);
@@ -456,75 +489,74 @@ bool build_group_norm_backward(const fs_graph& g, std::vector<Candidate>* out, P
   }
 
   // ---- two or three launches
-  const uint32_t gs = widest_set(base);
-  if (gs == 0) return true;
-  uint32_t last_chunks = 0;
-  for (uint32_t want : {256u, 512u, 1024u, 2048u}) {
-    GroupNormP p = base;
-    if (!lay_out(&p, 256, gs) || !cut(&p, want) || p.chunks == last_chunks) continue;
-    last_chunks = p.chunks;
-    const uint32_t width = gs * p.dim, rows = p.batch * p.chunks;
-    const int64_t lds = 4ll * ((int64_t)p.rows_at_once * width + 3 * width);
-    const int64_t chunk_bytes = aligned(8ll * rows * pitch), mean_bytes = aligned(8ll * rows * p.groups);
-    const bool join = joins(p, gs, 16);
-    Candidate c = make_candidate(g, "group_norm_backward", FS_SCHEME_GLOBAL, K_GN_BWD_SUMS);
-    {
-      Launch& l = c.launches.front();
-      p.fold_log2 = fold_lanes_log2(256, width, p.rows_at_once);
-      p.means_log2 = fold_lanes_log2(256, gs, p.dim);
-      l.args.u.gn = p;
-      fill_inputs(l);
-      l.ptr[6] = ws_ref(0);
-      l.ptr[7] = ws_ref(chunk_bytes);
-      l.shape.block[0] = 256;
-      l.shape.grid[0] = rows * p.sets;
-      l.shape.lds_bytes = (uint32_t)lds;
+  for (uint32_t gs : chunk_sets(base)) {
+    uint32_t last_chunks = 0;
+    for (uint32_t want : {256u, 512u}) {
+      GroupNormP p = base;
+      if (!lay_out(&p, 256, gs) || !cut(&p, want) || p.chunks == last_chunks) continue;
+      last_chunks = p.chunks;
+      const uint32_t width = gs * p.dim, rows = p.batch * p.chunks;
+      const int64_t lds = 4ll * ((int64_t)p.rows_at_once * width + 3 * width);
+      const int64_t chunk_bytes = aligned(8ll * rows * pitch), mean_bytes = aligned(8ll * rows * p.groups);
+      const bool join = joins(p, gs, 16);
+      Candidate c = make_candidate(g, "group_norm_backward", FS_SCHEME_GLOBAL, K_GN_BWD_SUMS);
+      {
+        Launch& l = c.launches.front();
+        p.fold_log2 = fold_lanes_log2(256, width, p.rows_at_once);
+        p.means_log2 = fold_lanes_log2(256, gs, p.dim);
+        l.args.u.gn = p;
+        fill_inputs(l);
+        l.ptr[6] = ws_ref(0);
+        l.ptr[7] = ws_ref(chunk_bytes);
+        l.shape.block[0] = 256;
+        l.shape.grid[0] = rows * p.sets;
+        l.shape.lds_bytes = (uint32_t)lds;
+      }
+      if (!join) {
+        c.launches.emplace_back();
+        Launch& l = c.launches.back();
+        l.kernel = K_GN_BWD_JOIN;
+        l.args.u.gn = p;
+        l.args.u.gn.fold_log2 = std::min(6, log2_of(pow2_at_least(p.chunks)));
+        l.ptr[0] = ws_ref(chunk_bytes);
+        l.ptr[1] = ws_ref(chunk_bytes + mean_bytes);
+        const uint32_t at_once = 256u >> l.args.u.gn.fold_log2;
+        l.shape.block[0] = 256;
+        l.shape.grid[0] = (p.batch * p.groups + at_once - 1) / at_once;
+      }
+      {
+        c.launches.emplace_back();
+        Launch& l = c.launches.back();
+        l.kernel = K_GN_BWD_APPLY;
+        GroupNormP& q = l.args.u.gn;
+        q = p;
+        q.join = join ? 1 : 0;
+        q.fold_log2 = fold_lanes_log2(256, gs, p.chunks);
+        const uint32_t quads = rows > 128 ? 4 : 16;   // quads of columns per workgroup of the fold
+        q.fold_blocks = ((2 * pitch / 4 + quads - 1) / quads + 7) / 8 * 8;
+        fill_inputs(l);
+        l.ptr[6] = out_ref(g.tensors[t_dx].output_slot);
+        l.ptr[7] = ws_ref(join ? chunk_bytes : chunk_bytes + mean_bytes);
+        l.ptr[8] = ws_ref(0);
+        l.ptr[9] = out_ref(g.tensors[t_dbeta].output_slot);
+        l.ptr[10] = out_ref(g.tensors[t_dgamma].output_slot);
+        l.shape.block[0] = 256;
+        l.shape.grid[0] = q.fold_blocks + rows * p.sets;
+        l.shape.lds_bytes = std::max<uint32_t>(4096, join ? 8 * gs : 0);
+      }
+      c.info.n_kernels = (int32_t)c.launches.size();
+      c.info.workspace_bytes = chunk_bytes + mean_bytes + (join ? 0 : aligned(8ll * p.batch * p.groups));
+      c.info.bytes_moved_model = c.info.bytes_min + (int64_t)t.read_bytes + 2 * chunk_bytes;
+      c.info.lanes_per_row = (int32_t)p.set_vecs;
+      c.info.vecs_per_lane = 4;
+      c.info.rows_per_block = (int32_t)p.chunk_rows;
+      c.info.lds_bytes = (int32_t)lds;
+      const KernelCost kc = estimated(passes_us(p, t, c.launches.size()), p, 120, (int)lds);
+      char var[56];
+      snprintf(var, sizeof var, "<%s,%s,G%u,C%u,%sapply>", dtype_name(p.dt), act_name(p.act), gs, p.chunks, join ? "" : "join,");
+      finish_candidate(&c, var, kc);
+      out->push_back(c);
     }
-    if (!join) {
-      c.launches.emplace_back();
-      Launch& l = c.launches.back();
-      l.kernel = K_GN_BWD_JOIN;
-      l.args.u.gn = p;
-      l.args.u.gn.fold_log2 = std::min(6, log2_of(pow2_at_least(p.chunks)));
-      l.ptr[0] = ws_ref(chunk_bytes);
-      l.ptr[1] = ws_ref(chunk_bytes + mean_bytes);
-      const uint32_t at_once = 256u >> l.args.u.gn.fold_log2;
-      l.shape.block[0] = 256;
-      l.shape.grid[0] = (p.batch * p.groups + at_once - 1) / at_once;
-    }
-    {
-      c.launches.emplace_back();
-      Launch& l = c.launches.back();
-      l.kernel = K_GN_BWD_APPLY;
-      GroupNormP& q = l.args.u.gn;
-      q = p;
-      q.join = join ? 1 : 0;
-      q.fold_log2 = fold_lanes_log2(256, gs, p.chunks);
-      const uint32_t quads = rows > 128 ? 4 : 16;   // quads of columns per workgroup of the fold
-      q.fold_blocks = ((2 * pitch / 4 + quads - 1) / quads + 7) / 8 * 8;
-      fill_inputs(l);
-      l.ptr[6] = out_ref(g.tensors[t_dx].output_slot);
-      l.ptr[7] = ws_ref(join ? chunk_bytes : chunk_bytes + mean_bytes);
-      l.ptr[8] = ws_ref(0);
-      l.ptr[9] = out_ref(g.tensors[t_dbeta].output_slot);
-      l.ptr[10] = out_ref(g.tensors[t_dgamma].output_slot);
-      l.shape.block[0] = 256;
-      l.shape.grid[0] = q.fold_blocks + rows * p.sets;
-      l.shape.lds_bytes = std::max<uint32_t>(4096, join ? 8 * gs : 0);
-    }
-    c.info.n_kernels = (int32_t)c.launches.size();
-    c.info.workspace_bytes = chunk_bytes + mean_bytes + (join ? 0 : aligned(8ll * p.batch * p.groups));
-    c.info.bytes_moved_model = c.info.bytes_min + (int64_t)t.read_bytes + 2 * chunk_bytes;
-    c.info.lanes_per_row = (int32_t)p.set_vecs;
-    c.info.vecs_per_lane = 4;
-    c.info.rows_per_block = (int32_t)p.chunk_rows;
-    c.info.lds_bytes = (int32_t)lds;
-    KernelCost kc;
-    passes_cost(p, t, p.vec * (esz + xsz), (int)c.launches.size(), &kc);
-    char var[56];
-    snprintf(var, sizeof var, "<%s,%s,G%u,C%u,%sapply>", dtype_name(p.dt), act_name(p.act), gs, p.chunks, join ? "" : "join,");
-    finish_candidate(&c, var, kc);
-    out->push_back(c);
   }
   return true;
 }

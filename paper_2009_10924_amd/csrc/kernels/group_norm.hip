@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(NT) k_gn_slab(const T* x, const T* gamma, cons
 #pragma unroll
     for (int e = 0; e < VEC; ++e)
       v[e] = activate<ACT>(__builtin_fmaf(v[e] - mean[WHOLE ? 0 : e], ga[e], be[e]));
-    VecIo<T, VEC>::template store<false>(near_element(y + base, place + (uint32_t)k * step), v);
+    store_as<VecIo<T, VEC>>(p.whole_lines, near_element(y + base, place + (uint32_t)k * step), v);
   }
   if (!q) return;
   float to8[G];
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(NT) k_gn_slab(const T* x, const T* gamma, cons
     VecIo<T, VEC>::widen(raw[k], v);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) v[e] = (v[e] - mean[WHOLE ? 0 : e]) * to8[WHOLE ? 0 : e];
-    VecIo<e4m3_t, VEC>::template store<false>(near_element(q + base, place + (uint32_t)k * step), v);
+    store_as<VecIo<e4m3_t, VEC>>(p.whole_lines, near_element(q + base, place + (uint32_t)k * step), v);
   }
 }
 

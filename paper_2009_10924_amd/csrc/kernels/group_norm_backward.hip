@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(NT) k_gn_bwd_slab(const typename GnValue<T, FR
       v[e] = ch.about_mean(v[e], e);
       d[e] = gr.dx(v[e], ch.template dz<ACT>(v[e], d[e], e), e);
     }
-    VecIo<T, VEC>::template store<false>(near_element(dx + base, place + (uint32_t)k * step), d);
+    store_as<VecIo<T, VEC>>(p.whole_lines, near_element(dx + base, place + (uint32_t)k * step), d);
   }
 }
 

@@ -13,6 +13,11 @@ template <bool STREAM, typename V, typename P> __device__ __forceinline__ void p
   else *p = v;
 }
 
+template <typename IO, typename T, int VEC> __device__ __forceinline__ void store_as(bool stream, T* p, const float (&v)[VEC]) {
+  if (stream) IO::template store<true>(p, v);
+  else IO::template store<false>(p, v);
+}
+
 template <typename T, int VEC> struct VecIo {
   static_assert(VEC == Elem<T>::VEC, "a whole vector, or one element");
   typedef u32x4 Raw;
