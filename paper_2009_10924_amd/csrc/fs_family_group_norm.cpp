@@ -54,6 +54,8 @@ bool lay_out(GroupNormP* p, int threads, uint32_t set_groups) {
   p->div_chunks = make_fastdiv(1);
   p->chunks = 1;
   p->chunk_rows = p->positions;
+  p->entries = 1;
+  p->entry_blocks = p->batch;
   return p->div_per.d != 0 && p->div_sets.d != 0;
 }
 int pow2_at_most_log2(uint32_t v) {
@@ -134,20 +136,22 @@ double items_per_lane(const GroupNormP& p, bool backward) {
 double few_units(double bytes, double workgroups, double unit) { return bytes / std::min(256.0, workgroups) / unit; }
 double slab_us(const GroupNormP& p, const Traffic& t, int esz, int K, int vgprs) {
   const SlabModel& m = kSlab[t.backward ? 1 : 0];
-  const double groups = (double)p.batch * p.sets;
+  const double groups = (double)p.entry_blocks * p.sets;
   const double waves = std::max(1.0, groups * p.threads / 64.0 / 1024.0);   // per SIMD
   const double ops = (m.ops + m.ops_act * t.act + m.ops_8bit * p.checkpoint) * K * p.vec;
   // workgroups that a compute unit holds, and so the rounds of them
   const int per_simd = std::min(8, 512 / std::max(8, (vgprs + 7) / 8 * 8)), held = std::max(1, 4 * per_simd / (p.threads / 64));
-  const double rounds = std::ceil(groups / (256.0 * held));
+  const double rounds = std::min(8.0, std::ceil(groups / (256.0 * held)));
   const double chain = (m.fixed + m.chain_op * ops + m.chain_item * items_per_lane(p, t.backward) + m.chain_threads * p.threads / 512.0) * (1.0 + m.round * (rounds - 1.0));
+  const double more = std::max(0.0, chain - 1.5) * (p.entries - 1.0);   // the next entries' chains, without a launch
   const double issue = waves * (m.issue + m.issue_op * ops);
   const double run = p.sets > 1 ? (double)p.set_groups * p.dim * esz : 1e9;
   double memory = (t.read_bytes + t.written_bytes) / 6.5e6 * (1.0 + m.shared_lines * std::max(0.0, 256.0 / run - 1.0));
   memory = std::max(memory, few_units(t.read_bytes + t.written_bytes, groups, 3.3e4));
   // lines that the accesses of a compute unit's wavefronts touch, one after the other
   memory = std::max(memory, m.line * K * p.threads / 64.0 * std::max(1.0, groups / 256.0) * std::max(64.0 / p.set_vecs, 64.0 * p.vec * esz / 128.0));
-  return chain + std::max(issue, memory) + m.overlap * std::min(issue, memory) + (p.batch > 1 ? m.fold : 0.0);
+  if (t.backward && p.entry_blocks > 1) memory += 16.0 * p.entry_blocks * p.channels / 6.6e6;   // partial sums, written and read
+  return chain + more + std::max(issue, memory) + m.overlap * std::min(issue, memory) + (p.entry_blocks > 1 ? m.fold : 0.0);
 }
 double passes_us(const GroupNormP& p, const Traffic& t, size_t n_launches) {
   const PassesModel& m = kPasses[t.backward ? 1 : 0];
@@ -159,9 +163,10 @@ double passes_us(const GroupNormP& p, const Traffic& t, size_t n_launches) {
                   m.partials * 16.0 * p.batch * p.chunks * p.channels / 6.6e6 + m.join * p.chunks * p.set_groups;
   if (p.sets > 1) memory *= 1.0 + m.shared_lines * 128.0 / ((double)p.set_groups * p.dim * dtype_bytes(p.dt));
   const double workgroups = (double)p.batch * p.sets * p.chunks;
+  const double starts = 1.1 * std::max(0.0, waves - 2.0);   // very many short workgroups: their prologues, in both launches
   if (workgroups < 400) memory *= 1.05;   // one wavefront per SIMD: loads and arithmetic take turns
   memory = std::max(memory, few_units(2.0 * t.read_bytes + t.written_bytes, workgroups, 4.0e4));
-  return m.fixed + m.launch * ((double)n_launches - 2.0) + std::max(issue, memory) + m.overlap * std::min(issue, memory) + m.item * items_per_lane(p, t.backward);
+  return m.fixed + m.launch * ((double)n_launches - 2.0) + starts + std::max(issue, memory) + m.overlap * std::min(issue, memory) + m.item * items_per_lane(p, t.backward);
 }
 KernelCost estimated(double us, const GroupNormP& p, int vgprs, int lds) {
   KernelCost kc;
@@ -230,7 +235,7 @@ bool build_group_norm(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
   // ---- one launch
   struct Slab { int threads, K; };
   for (uint32_t gs : set_sizes(base.groups)) {
-    for (Slab sh : {Slab{256, 1}, Slab{256, 2}, Slab{256, 4}, Slab{256, 8}, Slab{512, 4}, Slab{512, 8}, Slab{512, 16}, Slab{512, 32}}) {
+    for (Slab sh : {Slab{64, 1}, Slab{64, 2}, Slab{64, 4}, Slab{256, 1}, Slab{256, 2}, Slab{256, 4}, Slab{256, 8}, Slab{512, 4}, Slab{512, 8}, Slab{512, 16}, Slab{512, 32}}) {
       GroupNormP p = base;
       if (!lay_out(&p, sh.threads, gs)) continue;
       const uint64_t held = (uint64_t)sh.K * p.rows_at_once;
@@ -433,21 +438,10 @@ bool build_group_norm_backward(const fs_graph& g, std::vector<Candidate>* out, P
     if (tb >= 0) l.ptr[4] = in_ref(g, tb);
     l.ptr[5] = in_ref(g, tdy);
   };
-  // the batch entries' sums added up: dbeta from the first half of each row, dgamma from the second
-  auto add_fold = [&](Candidate* c, int64_t at) {
-    c->launches.emplace_back();
-    Launch& f = c->launches.back();
-    make_fold_launch(&f, base.batch, 2 * pitch, pitch, base.channels);
-    f.ptr[0] = ws_ref(at);
-    f.ptr[1] = out_ref(g.tensors[t_dbeta].output_slot);
-    f.ptr[2] = out_ref(g.tensors[t_dgamma].output_slot);
-  };
-  const int64_t sum_bytes = aligned(8ll * base.batch * pitch);
-
   // ---- one launch and the fold
   struct Slab { int threads, K; };
   for (uint32_t gs : set_sizes(base.groups)) {
-    for (Slab sh : {Slab{256, 1}, Slab{256, 2}, Slab{256, 4}, Slab{512, 4}, Slab{512, 8}, Slab{512, 16}}) {
+    for (Slab sh : {Slab{64, 1}, Slab{64, 2}, Slab{64, 4}, Slab{256, 1}, Slab{256, 2}, Slab{256, 4}, Slab{512, 4}, Slab{512, 8}, Slab{512, 16}}) {
       GroupNormP p = base;
       if (!lay_out(&p, sh.threads, gs)) continue;
       const uint64_t held = (uint64_t)sh.K * p.rows_at_once;
@@ -457,25 +451,38 @@ bool build_group_norm_backward(const fs_graph& g, std::vector<Candidate>* out, P
       p.vecs_per_lane = sh.K;
       p.fold_log2 = fold_lanes_log2(sh.threads, width, p.rows_at_once);
       p.means_log2 = fold_lanes_log2(sh.threads, gs, p.dim);
-      const int64_t lds = 4ll * ((int64_t)p.rows_at_once * width + 3 * width + 2 * gs);
-      if (lds > 64 * 1024 || (uint64_t)p.batch * p.sets >= (1ull << 31)) continue;
+      // One batch entry per workgroup; of very many entries so many that the partial sums stay small beside the values (f16
+      // [65536, 1, 512]: 268 MB of them beside 200 MB otherwise).
+      const uint32_t most = std::max<uint32_t>(1, 8192 / p.sets);
+      const uint32_t e = p.batch > most && sh.threads <= 256 ? (p.batch + most / 4 - 1) / std::max<uint32_t>(1, most / 4) : 1;
+      p.entries = e;
+      p.entry_blocks = (p.batch + e - 1) / e;
+      const bool fold = p.entry_blocks > 1;
+      const int64_t sum_bytes = aligned(8ll * p.entry_blocks * pitch);
+      const int64_t lds = 4ll * ((int64_t)p.rows_at_once * width + 3 * width + 2 * gs + (e > 1 ? 2 * width : 0));
+      if (lds > 64 * 1024 || (uint64_t)p.entry_blocks * p.sets >= (1ull << 31)) continue;
       Candidate c = make_candidate(g, "group_norm_backward", FS_SCHEME_LDS, K_GN_BWD_SLAB);
       Launch& l = c.launches.front();
       l.args.u.gn = p;
       fill_inputs(l);
       l.ptr[6] = out_ref(g.tensors[t_dx].output_slot);
-      l.ptr[7] = p.batch == 1 ? out_ref(g.tensors[t_dbeta].output_slot) : ws_ref(0);
-      l.ptr[8] = p.batch == 1 ? out_ref(g.tensors[t_dgamma].output_slot) : ws_ref(4ll * pitch);
+      l.ptr[7] = fold ? ws_ref(0) : out_ref(g.tensors[t_dbeta].output_slot);
+      l.ptr[8] = fold ? ws_ref(4ll * pitch) : out_ref(g.tensors[t_dgamma].output_slot);
       l.shape.block[0] = (uint32_t)sh.threads;
-      l.shape.grid[0] = p.batch * p.sets;
+      l.shape.grid[0] = p.entry_blocks * p.sets;
       l.shape.lds_bytes = (uint32_t)lds;
       const int vgprs = 73 + sh.K * (p.vec * (esz + xsz) / 4 + 1);
       const KernelCost kc = estimated(slab_us(p, t, esz, sh.K, vgprs), p, vgprs, (int)lds);
       char var[56];
-      snprintf(var, sizeof var, "<%s,%s,T%d,K%d,G%u%s>", dtype_name(p.dt), act_name(p.act), sh.threads, sh.K, gs, p.batch == 1 ? "" : ",fold");
+      snprintf(var, sizeof var, "<%s,%s,T%d,K%d,G%u,E%u%s>", dtype_name(p.dt), act_name(p.act), sh.threads, sh.K, gs, e, fold ? ",fold" : "");
       finish_candidate(&c, var, kc);
-      if (p.batch > 1) {
-        add_fold(&c, 0);
+      if (fold) {   // dbeta from the first half of each row of sums, dgamma from the second
+        c.launches.emplace_back();
+        Launch& f = c.launches.back();
+        make_fold_launch(&f, p.entry_blocks, 2 * pitch, pitch, p.channels);
+        f.ptr[0] = ws_ref(0);
+        f.ptr[1] = out_ref(g.tensors[t_dbeta].output_slot);
+        f.ptr[2] = out_ref(g.tensors[t_dgamma].output_slot);
         c.info.n_kernels = 2;
         c.info.workspace_bytes = sum_bytes;
         c.info.bytes_moved_model = c.info.bytes_min + 2 * sum_bytes;

@@ -436,7 +436,13 @@ using namespace fsk;
 namespace {
 template <typename T, int VEC, bool WHOLE, int ACT>
 const void* slab_sym(const GroupNormP& p) {
-  if (p.threads == 256) {
+  if (p.threads == 64) {
+    switch (p.vecs_per_lane) {
+      case 1: return (const void*)k_gn_slab<T, VEC, 1, WHOLE, ACT, 64>;
+      case 2: return (const void*)k_gn_slab<T, VEC, 2, WHOLE, ACT, 64>;
+      case 4: return (const void*)k_gn_slab<T, VEC, 4, WHOLE, ACT, 64>;
+    }
+  } else if (p.threads == 256) {
     switch (p.vecs_per_lane) {
       case 1: return (const void*)k_gn_slab<T, VEC, 1, WHOLE, ACT, 256>;
       case 2: return (const void*)k_gn_slab<T, VEC, 2, WHOLE, ACT, 256>;

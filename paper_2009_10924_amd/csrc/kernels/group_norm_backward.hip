@@ -67,10 +67,11 @@ struct GnGradient {
 };
 
 // Sums over the workgroup's positions of what every thread has gathered per channel: channel c of the set to out[c], and times
-// gamma to weighted[c], by 1 << fold_log2 lanes each.  `items`: rows_at_once * width floats of LDS.
+// gamma to weighted[c], by 1 << fold_log2 lanes each.  `items`: rows_at_once * width floats of LDS.  Over several batch entries the
+// sums go into `totals` and, with the last one, to out.
 template <int VEC>
 __device__ __forceinline__ void gn_channel_sums(float* items, const GnShape& p, const GnLane& l, const float (&v)[VEC], const float* gain, float* weighted,
-                                                float* out) {
+                                                float* out, float* totals = nullptr, bool first = true, bool last = true) {
   const uint32_t width = p.set_groups * p.dim, lanes = 1u << p.fold_log2, lane = threadIdx.x & (lanes - 1u);
   gn_deposit<false, VEC>(items, p, l, v);
   __syncthreads();
@@ -82,7 +83,9 @@ __device__ __forceinline__ void gn_channel_sums(float* items, const GnShape& p, 
     a = group_allreduce<OpSum>(a, (int)lanes);
     if (lane == 0 && c < width) {
       weighted[c] = a * gain[c];
-      out[c] = a;
+      if (!first) a += totals[c];
+      if (last) out[c] = a;
+      else totals[c] = a;
     }
   }
   __syncthreads();
@@ -113,9 +116,10 @@ __device__ __forceinline__ void gn_group_means(const GnShape& p, const float* wa
   }
 }
 
-// ---- one launch (and, for more than one batch entry, the fold) -----------------------------------------------------------------
-// out_a, out_b: A and B of batch entry n, `2 * sum_pitch` floats behind those of n - 1 (with one entry they are dbeta and dgamma).
-template <typename T, int VEC, int K, int ACT, bool FROM8, int NT>
+// ---- one launch (and the fold, where more than one workgroup has a channel) ------------------------------------------------------
+// A and B go to row n of out_a and out_b, rows 2 * sum_pitch floats apart (with one batch entry they are dbeta and dgamma).  MANY: a
+// workgroup works through `entries` batch entries, one after the other, and adds up theirs, row i being the i-th workgroup's.
+template <typename T, int VEC, int K, int ACT, bool FROM8, int NT, bool MANY>
 __global__ void __launch_bounds__(NT) k_gn_bwd_slab(const typename GnValue<T, FROM8>::type* x, const float* centre, const float* rstd, const T* gamma,
                                                     const T* beta, const T* dy, T* dx, float* out_a, float* out_b, const GnShape p) {
   typedef typename GnValue<T, FROM8>::type X;
@@ -126,71 +130,75 @@ __global__ void __launch_bounds__(NT) k_gn_bwd_slab(const typename GnValue<T, FR
   float* const sum_a = gain + width;
   float* const sum_b = sum_a + width;
   float* const means = sum_b + width;   // [set_groups][2]
-  const uint32_t b = gn_block(p.batch * p.sets), n = fast_div(b, p.div_sets), set = b - n * p.sets;
+  float* const totals = means + 2u * p.set_groups;   // [2][width], for more than one entry
+  const uint32_t b = gn_block(p.entry_blocks * p.sets), row = fast_div(b, p.div_sets), set = b - row * p.sets;
   const GnLane l = gn_lane<VEC>(p);
-  const size_t base = (size_t)n * p.positions * p.channels + set * width;
-  const uint32_t place = l.row * p.channels + l.col, step = p.rows_at_once * p.channels, last = (p.positions - 1u) * p.channels + l.col;
-  typename VecIo<X, VEC>::Raw rx[K];
-  typename VecIo<T, VEC>::Raw rd[K];
+  const uint32_t n0 = MANY ? row * p.entries : row, n1 = MANY ? min(n0 + p.entries, p.batch) : n0 + 1u;
+  const size_t out = (size_t)row * 2u * p.sum_pitch + set * width;
+  for (uint32_t n = n0; n < n1; ++n) {
+    const size_t base = (size_t)n * p.positions * p.channels + set * width;
+    const uint32_t place = l.row * p.channels + l.col, step = p.rows_at_once * p.channels, last = (p.positions - 1u) * p.channels + l.col;
+    typename VecIo<X, VEC>::Raw rx[K];
+    typename VecIo<T, VEC>::Raw rd[K];
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    rx[k] = VecIo<X, VEC>::template load<false>(near_element(x + base, min(place + (uint32_t)k * step, last)));
-    rd[k] = VecIo<T, VEC>::template load<false>(near_element(dy + base, min(place + (uint32_t)k * step, last)));
-  }
-  GnChannels<T, VEC, FROM8> ch;
-  ch.load(p, l, n, set, centre, rstd, gamma, beta);
-  gn_keep_gain<VEC>(gain, l, ch.ga);
-  auto valid = [&](int k) { return l.live && place + (uint32_t)k * step <= last; };
-  float a[VEC], bb[VEC];
+    for (int k = 0; k < K; ++k) {
+      rx[k] = VecIo<X, VEC>::template load<false>(near_element(x + base, min(place + (uint32_t)k * step, last)));
+      rd[k] = VecIo<T, VEC>::template load<false>(near_element(dy + base, min(place + (uint32_t)k * step, last)));
+    }
+    GnChannels<T, VEC, FROM8> ch;
+    ch.load(p, l, n, set, centre, rstd, gamma, beta);
+    gn_keep_gain<VEC>(gain, l, ch.ga);
+    auto valid = [&](int k) { return l.live && place + (uint32_t)k * step <= last; };
+    float a[VEC], bb[VEC];
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) a[e] = bb[e] = 0.0f;
+    for (int e = 0; e < VEC; ++e) a[e] = bb[e] = 0.0f;
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    float v[VEC], d[VEC];
-    again(rx[k]);
-    again(rd[k]);
-    VecIo<X, VEC>::widen(rx[k], v);
-    VecIo<T, VEC>::widen(rd[k], d);
+    for (int k = 0; k < K; ++k) {
+      float v[VEC], d[VEC];
+      again(rx[k]);
+      again(rd[k]);
+      VecIo<X, VEC>::widen(rx[k], v);
+      VecIo<T, VEC>::widen(rd[k], d);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        v[e] = ch.about_mean(v[e], e);
+        const float dz = valid(k) ? ch.template dz<ACT>(v[e], d[e], e) : 0.0f;
+        a[e] += dz;
+        bb[e] = __builtin_fmaf(dz, valid(k) ? v[e] : 0.0f, bb[e]);
+      }
+      done(a);
+      done(bb);
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) bb[e] *= ch.scale[e];
+    gn_channel_sums<VEC>(items, p, l, a, gain, sum_a, out_a + out, totals, !MANY || n == n0, !MANY || n + 1u == n1);
+    gn_channel_sums<VEC>(items, p, l, bb, gain, sum_b, out_b + out, totals + width, !MANY || n == n0, !MANY || n + 1u == n1);
+    gn_group_means(p, sum_a, sum_b, [&](uint32_t g, float m1, float m2) {
+      means[2u * g] = m1;
+      means[2u * g + 1u] = m2;
+    });
+    __syncthreads();
+    GnGradient<VEC> gr;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-      v[e] = ch.about_mean(v[e], e);
-      const float dz = valid(k) ? ch.template dz<ACT>(v[e], d[e], e) : 0.0f;
-      a[e] += dz;
-      bb[e] = __builtin_fmaf(dz, valid(k) ? v[e] : 0.0f, bb[e]);
+      const uint32_t g = fast_div(l.col + e, p.div_dim);
+      gr.set(e, ch, FROM8 ? rstd[n * p.groups + set * p.set_groups + g] : ch.scale[e], means[2u * g], means[2u * g + 1u]);
     }
-    done(a);
-    done(bb);
-  }
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) bb[e] *= ch.scale[e];
-  const size_t out = (size_t)n * 2u * p.sum_pitch + set * width;
-  gn_channel_sums<VEC>(items, p, l, a, gain, sum_a, out_a + out);
-  gn_channel_sums<VEC>(items, p, l, bb, gain, sum_b, out_b + out);
-  gn_group_means(p, sum_a, sum_b, [&](uint32_t g, float m1, float m2) {
-    means[2u * g] = m1;
-    means[2u * g + 1u] = m2;
-  });
-  __syncthreads();
-  GnGradient<VEC> gr;
+    for (int k = 0; k < K; ++k) {
+      again(rx[k]);
+      again(rd[k]);
+      if (!valid(k)) continue;
+      float v[VEC], d[VEC];
+      VecIo<X, VEC>::widen(rx[k], v);
+      VecIo<T, VEC>::widen(rd[k], d);
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) {
-    const uint32_t g = fast_div(l.col + e, p.div_dim);
-    gr.set(e, ch, FROM8 ? rstd[n * p.groups + set * p.set_groups + g] : ch.scale[e], means[2u * g], means[2u * g + 1u]);
-  }
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    again(rx[k]);
-    again(rd[k]);
-    if (!valid(k)) continue;
-    float v[VEC], d[VEC];
-    VecIo<X, VEC>::widen(rx[k], v);
-    VecIo<T, VEC>::widen(rd[k], d);
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      v[e] = ch.about_mean(v[e], e);
-      d[e] = gr.dx(v[e], ch.template dz<ACT>(v[e], d[e], e), e);
+      for (int e = 0; e < VEC; ++e) {
+        v[e] = ch.about_mean(v[e], e);
+        d[e] = gr.dx(v[e], ch.template dz<ACT>(v[e], d[e], e), e);
+      }
+      store_as<VecIo<T, VEC>>(p.whole_lines, near_element(dx + base, place + (uint32_t)k * step), d);
     }
-    store_as<VecIo<T, VEC>>(p.whole_lines, near_element(dx + base, place + (uint32_t)k * step), d);
   }
 }
 
@@ -384,22 +392,31 @@ namespace fs {
 using namespace fsk;
 
 namespace {
+template <typename T, int VEC, int ACT, bool FROM8, int NT, bool MANY>
+const void* slab_sym(int vecs) {
+  switch (vecs) {
+    case 1: return (const void*)k_gn_bwd_slab<T, VEC, 1, ACT, FROM8, NT, MANY>;
+    case 2: return (const void*)k_gn_bwd_slab<T, VEC, 2, ACT, FROM8, NT, MANY>;
+    case 4: return (const void*)k_gn_bwd_slab<T, VEC, 4, ACT, FROM8, NT, MANY>;
+    default: return nullptr;
+  }
+}
 template <typename T, int VEC, int ACT, bool FROM8>
 const void* bwd_sym(int32_t kernel, const GroupNormP& p) {
   if (kernel == K_GN_BWD_SUMS) return (const void*)k_gn_bwd_sums<T, VEC, ACT, FROM8>;
   if (kernel == K_GN_BWD_APPLY)
     return p.join ? (const void*)k_gn_bwd_apply<T, VEC, ACT, FROM8, true> : (const void*)k_gn_bwd_apply<T, VEC, ACT, FROM8, false>;
-  if (p.threads == 256) {
+  if (p.entries > 1) {   // batches of very many entries: workgroups of one wavefront or four
+    if (p.threads == 64) return slab_sym<T, VEC, ACT, FROM8, 64, true>(p.vecs_per_lane);
+    return p.threads == 256 ? slab_sym<T, VEC, ACT, FROM8, 256, true>(p.vecs_per_lane) : nullptr;
+  }
+  if (p.threads == 64) return slab_sym<T, VEC, ACT, FROM8, 64, false>(p.vecs_per_lane);
+  if (p.threads == 256) return slab_sym<T, VEC, ACT, FROM8, 256, false>(p.vecs_per_lane);
+  if (p.threads == 512) {
     switch (p.vecs_per_lane) {
-      case 1: return (const void*)k_gn_bwd_slab<T, VEC, 1, ACT, FROM8, 256>;
-      case 2: return (const void*)k_gn_bwd_slab<T, VEC, 2, ACT, FROM8, 256>;
-      case 4: return (const void*)k_gn_bwd_slab<T, VEC, 4, ACT, FROM8, 256>;
-    }
-  } else if (p.threads == 512) {
-    switch (p.vecs_per_lane) {
-      case 4: return (const void*)k_gn_bwd_slab<T, VEC, 4, ACT, FROM8, 512>;
-      case 8: return (const void*)k_gn_bwd_slab<T, VEC, 8, ACT, FROM8, 512>;
-      case 16: return (const void*)k_gn_bwd_slab<T, VEC, 16, ACT, FROM8, 512>;
+      case 4: return (const void*)k_gn_bwd_slab<T, VEC, 4, ACT, FROM8, 512, false>;
+      case 8: return (const void*)k_gn_bwd_slab<T, VEC, 8, ACT, FROM8, 512, false>;
+      case 16: return (const void*)k_gn_bwd_slab<T, VEC, 16, ACT, FROM8, 512, false>;
     }
   }
   return nullptr;

@@ -205,6 +205,7 @@ struct GroupNormP {
   uint32_t chunk_rows, chunks;      // positions per chunk
   int32_t threads, vecs_per_lane;
   int32_t join;                     // last launch: 1 = it joins the chunks itself
+  uint32_t entries, entry_blocks;   // K_GN_BWD_SLAB: batch entries of a workgroup, workgroups per set
   uint32_t fold_blocks;             // K_GN_BWD_APPLY: workgroups that add up the chunks' sums
   float eps, inv_count, inv_max, tiny;   // inv_count = 1 / (positions * dim)
   int32_t stream;
