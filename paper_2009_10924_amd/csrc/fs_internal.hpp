@@ -105,6 +105,7 @@ struct Candidate {
   fs_plan_info info;
   std::vector<Launch> launches;
   KernelCost cost;               // description of the (single) stitched kernel; unused for unfused plans
+  bool apart = false;            // no output may share memory with an input or another output: refused when it is run
   bool fallback = false;         // offered only for the case that no other candidate can be used (the interpreted row
                                  // program beside the kernels generated for the same pattern): passed over by the choice
                                  // while another candidate stands, still reachable by index
@@ -234,6 +235,8 @@ fs_status create_plan(const fs_graph* g, int32_t scheme, const fs_plan_opts* opt
 fs_status run_launches(const fs_plan* p, const void* const* inputs, void* const* outputs, void* workspace, void* hip_stream,
                        size_t n_launches);
 // Whether an output shares memory with an input or with another output.
+// FS_ERR_INVALID_ARG if the chosen kernels need outputs of their own memory and these are not
+fs_status check_apart(const fs_plan* p, const void* const* inputs, void* const* outputs);
 bool outputs_share_memory(const std::vector<int64_t>& input_bytes, const std::vector<int64_t>& output_bytes, const void* const* inputs, void* const* outputs);
 // The checks every execute entry point makes on its pointer arrays (null, alignment); `who` names the caller in the message.
 fs_status check_execute_args(const fs_plan* p, const void* const* inputs, void* const* outputs, const char* who);

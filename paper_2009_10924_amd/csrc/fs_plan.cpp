@@ -227,6 +227,12 @@ static fs_status run_at_once(const SumsBesideRows& once, const void* const* inpu
   return err == 0 ? FS_OK : fail(FS_ERR_HIP, "fs_execute: launching rows and column sums failed: %s", hip_error_text(err));
 }
 
+fs_status fs::check_apart(const fs_plan* p, const void* const* inputs, void* const* outputs) {
+  const Candidate& c = p->candidates[p->chosen];
+  if (!c.apart || !outputs_share_memory(p->input_bytes, p->output_bytes, inputs, outputs)) return FS_OK;
+  return fail(FS_ERR_INVALID_ARG, "an output shares memory with an input or another output, which the kernels of pattern '%s' do not allow", c.info.pattern);
+}
+
 fs_status fs::run_launches(const fs_plan* p, const void* const* inputs, void* const* outputs, void* workspace, void* hip_stream,
                        size_t n_launches) {
   const Candidate& c = p->candidates[p->chosen];
@@ -595,6 +601,8 @@ fs_status fs_execute(const fs_plan* p, const void* const* inputs, void* const* o
       return fail(FS_ERR_WORKSPACE, "fs_execute: workspace of %lld bytes needed, %zu given", (long long)c.info.workspace_bytes, workspace_bytes);
     if ((uintptr_t)workspace & 15u) return fail(FS_ERR_ALIGN, "fs_execute: workspace is not 16-byte aligned");
   }
+  const fs_status apart = check_apart(p, inputs, outputs);
+  if (apart != FS_OK) return apart;
   return run_launches(p, inputs, outputs, workspace, hip_stream, c.launches.size());
 } catch (...) {
   return fs::fail_caught("fs_execute");

@@ -152,9 +152,19 @@ static fs_status run_program(const fs_program* p, int32_t first_stage, int32_t l
     }
     return FS_OK;
   }
-  std::vector<char> pack_done(p->packs.size(), 0);
   std::vector<const void*> in;
   std::vector<void*> out;
+  // what a step would refuse is refused before the first one is launched
+  for (const fs_program::Step& s : p->steps) {
+    if (s.stage < first_stage || s.stage > last_stage || !s.plan->candidates[s.plan->chosen].apart) continue;
+    in.clear();
+    out.clear();
+    for (const BufRef& r : s.in) in.push_back(address(r));
+    for (const BufRef& r : s.out) out.push_back(address(r));
+    const fs_status st = check_apart(s.plan, in.data(), out.data());
+    if (st != FS_OK) return st;
+  }
+  std::vector<char> pack_done(p->packs.size(), 0);
   for (size_t si = 0; si < p->steps.size(); ++si) {
     const fs_program::Step& s = p->steps[si];
     if (s.stage < first_stage || s.stage > last_stage) continue;

@@ -27,13 +27,13 @@ FastDiv make_fastdiv(uint32_t d) {
 std::string build_stitched(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack) {
   PackForm scratch_form;
   if (!pack) pack = &scratch_form;
-  struct Family { const char* name; bool (*build)(const fs_graph&, std::vector<Candidate>*, PackForm*); bool knows_8bit; };
+  struct Family { const char* name; bool (*build)(const fs_graph&, std::vector<Candidate>*, PackForm*); bool knows_8bit, apart; };
   static const Family families[] = {
-      {"softmax", build_softmax, false}, {"layernorm", build_layernorm, false}, {"bias_gelu", build_gelu, false},
-      {"transpose_chain", build_tchain, false}, {"softmax_backward", build_softmax_backward, false}, {"rmsnorm", build_rmsnorm, false},
-      {"layernorm_backward", build_layernorm_backward, false}, {"transpose", build_transpose, false},
-      {"group_norm", build_group_norm, true}, {"group_norm_backward", build_group_norm_backward, true},
-      {"checkpoint", build_checkpoint, true}, {"checkpoint_backward", build_checkpoint_backward, true},
+      {"softmax", build_softmax, false, false}, {"layernorm", build_layernorm, false, false}, {"bias_gelu", build_gelu, false, false},
+      {"transpose_chain", build_tchain, false, false}, {"softmax_backward", build_softmax_backward, false, false}, {"rmsnorm", build_rmsnorm, false, false},
+      {"layernorm_backward", build_layernorm_backward, false, false}, {"transpose", build_transpose, false, false},
+      {"group_norm", build_group_norm, true, true}, {"group_norm_backward", build_group_norm_backward, true, true},
+      {"checkpoint", build_checkpoint, true, true}, {"checkpoint_backward", build_checkpoint_backward, true, true},
   };
   const bool has_8bit = holds_8bit(g);
   std::string recognised;
@@ -43,6 +43,7 @@ std::string build_stitched(const fs_graph& g, std::vector<Candidate>* out, PackF
     *pack = PackForm();
     if (f.build(g, out, pack)) {
       if (!out->empty()) {
+        for (Candidate& c : *out) c.apart = f.apart;
         // a family that only has its slow catch-all kernel for these extents (ragged or very long rows): the row
         // program's candidates join the list, and the choice passes the catch-all over while one of them stands
         bool only_fallbacks = true;

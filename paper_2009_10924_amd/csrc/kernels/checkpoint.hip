@@ -108,25 +108,16 @@ __global__ void __launch_bounds__(1024) k_checkpoint_long(const T* x, const T* b
   if (threadIdx.x == 0) scale[row] = s.s;
 #pragma unroll 2
   for (uint32_t c = threadIdx.x * VEC; c < cols; c += 1024u * VEC) {
-    // a last vector that starts early keeps to its own elements here: with y in the place of x, its neighbour's may be
-    // written by now
     float z[VEC], d[VEC];
-    if (c + VEC <= cols) {
-      values(c, z);
+    const uint32_t col = min(c, cols - VEC);
+    values(col, z);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) d[e] = s.divide(z[e]);
-      VecIo<e4m3_t, VEC>::store(q + base + c, d);
-      if constexpr (ACT != ACT_NONE) {
+    for (int e = 0; e < VEC; ++e) d[e] = s.divide(z[e]);
+    VecIo<e4m3_t, VEC>::store(q + base + col, d);
+    if constexpr (ACT != ACT_NONE) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) d[e] = activate<ACT>(z[e]);
-        VecIo<T, VEC>::store(y + base + c, d);
-      }
-    } else {
-      for (uint32_t i = c; i < cols; ++i) {
-        const float v = load1(x + base + i) + (bias ? load1(bias + at + i) : 0.0f);
-        store1_in_range(q + base + i, s.divide(v));
-        if constexpr (ACT != ACT_NONE) store1(y + base + i, activate<ACT>(v));
-      }
+      for (int e = 0; e < VEC; ++e) d[e] = activate<ACT>(z[e]);
+      VecIo<T, VEC>::store(y + base + col, d);
     }
   }
 }
@@ -176,14 +167,7 @@ __global__ void __launch_bounds__(256) k_checkpoint_grad(const e4m3_t* q, const 
       z[e] *= STRADDLE && (uint32_t)e >= edge[u] ? s1[u] : s0[u];
       if constexpr (ACT != ACT_NONE) z[e] = d[e] * activation_slope<ACT>(z[e]);
     }
-    const uint32_t own = first + (uint32_t)u * 256u * VEC;
-    if (own + VEC <= n) {
-      VecIo<T, VEC>::store(out + own, z);
-    } else if (own < n) {   // the run's last elements: those that no other lane has (it may have written its own over dy's already)
-#pragma unroll
-      for (int e = 0; e < VEC; ++e)
-        if (at[u] + e >= own) store1(out + at[u] + e, z[e]);
-    }
+    if (first + (uint32_t)u * 256u * VEC < n) VecIo<T, VEC>::store(out + at[u], z);
   }
 }
 

@@ -49,6 +49,8 @@ extern "C" fs_status fs_execute_static(const fs_plan* p, const void* const* inpu
   if (c.info.workspace_bytes > (int64_t)FS_STATIC_SCRATCH_BYTES)
     return fs::fail(FS_ERR_WORKSPACE, "fs_execute_static: the plan needs %lld bytes of scratch, the static array holds %lld; use fs_execute with a workspace",
                     (long long)c.info.workspace_bytes, (long long)FS_STATIC_SCRATCH_BYTES);
+  const fs_status apart = fs::check_apart(p, inputs, outputs);
+  if (apart != FS_OK) return apart;
   void* ws = nullptr;
   if (c.info.workspace_bytes > 0) {
     const fs_status a = scratch_of_current_device(&ws);

@@ -4,7 +4,7 @@ import pytest
 
 from oracle import oracle as O
 from paper_2009_10924_amd import binding as B
-from workloads import group_norm_backward_graph, group_norm_graph, make_inputs
+from workloads import checkpoint_backward_graph, checkpoint_graph, checkpointed_block_graph, group_norm_backward_graph, group_norm_graph, make_inputs
 from workloads.graphs import GraphSpec, OpSpec, TensorSpec
 
 
@@ -109,3 +109,37 @@ def test_backward_descriptor_is_the_gradient_by_differences(act):
             assert np.allclose(ref[grad].reshape(got.shape), got, rtol=1e-6, atol=1e-7), grad
     finally:
         O.to_f64 = keep
+
+
+# ---- memory the outputs may not share, and the run of all four together ------------------------------------------------------
+def spaced(n, base):
+    return [base + 0x10000000 * i for i in range(n)]
+
+
+@pytest.mark.parametrize("spec", [group_norm_graph(2, 50, 4, 16, "bf16", "silu", "checkpoint"), group_norm_backward_graph(2, 50, 4, 16, "bf16", "gelu", "stats"),
+                                  checkpoint_graph(10, 4, 32, "f16", "gelu", True), checkpoint_backward_graph(10, 4, 32, "f32", "silu", True)], ids=lambda s: s.name)
+def test_outputs_that_share_memory_are_refused(spec):
+    """In place, partly over an input, over another output, by the last byte: refused before anything runs."""
+    p = plan(spec)
+    ins, outs = spaced(len(spec.inputs), 0x100000000), spaced(len(spec.outputs), 0x200000000)
+    size = int(np.prod(spec.inputs[0].dims)) * {"bf16": 2, "f16": 2, "f32": 4, "e4m3": 1}[spec.inputs[0].dtype]
+    for bad in ([ins[0]] + outs[1:], [ins[0] + (size - 1) // 16 * 16] + outs[1:], outs[:-1] + [ins[-1]], outs[:-1] + [outs[0] + 16]):
+        with pytest.raises(B.FsError, match="FS_ERR_INVALID_ARG.*shares memory"):
+            p.execute_ptrs(ins, bad, 0x300000000, p.info["workspace_bytes"], 0)
+        with pytest.raises(B.FsError, match="FS_ERR_INVALID_ARG.*shares memory"):
+            p.execute_static_ptrs(ins, bad, 0)
+
+
+def test_explorer_takes_the_block_apart_at_its_products():
+    spec = checkpointed_block_graph(2, 64, 4, 16, 256, 64)
+    prog = B.Program(B.Graph.from_spec(spec))
+    text = prog.describe()
+    assert prog.info["n_steps"] == prog.info["n_stages"] == 4 and prog.info["n_single_ops"] == 0
+    assert [w.split("=")[1] for w in text.split() if w.startswith("pattern=")] == ["group_norm", "checkpoint", "checkpoint_backward", "group_norm_backward"]
+    assert prog.info["n_joint_folds"] == 2, text      # the bias gradient's and the normalisation's, in one launch at the end
+    ins, outs = spaced(len(spec.inputs), 0x100000000), spaced(len(spec.outputs), 0x400000000)
+    names = [n for n, _ in spec.outputs]
+    bad = list(outs)
+    bad[names.index("b1_dx")] = ins[[t.name for t in spec.inputs].index("b1_dy")]
+    with pytest.raises(B.FsError, match="FS_ERR_INVALID_ARG.*shares memory"):   # refused before the first of the four steps
+        prog.bind(ins, bad, 0x900000000, prog.info["workspace_bytes"], 0)()

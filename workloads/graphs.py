@@ -393,6 +393,30 @@ def checkpoint_backward_graph(rows: int, blocks: int, block: int, dtype: str = "
                      outputs=outputs)
 
 
+def checkpointed_block_graph(batch: int = 8, positions: int = 4096, groups: int = 32, dim: int = 10, hidden: int = 1280, block: int = 128,
+                             dtype: str = "bf16", act: str = "silu") -> GraphSpec:
+    """Forward and backward of a residual branch that keeps 8-bit checkpoints, with the matrix products taken out (as in
+    transformer_block_graph): group normalisation and its activation (f1_), a product to `hidden` channels, bias and tanh-GELU
+    (f2_), the rest of the network; then back through the bias and GELU (b2_), the product, and the normalisation (b1_).  Backward
+    reads what forward stored: 20 + 8 + 4 + 25 ops with SiLU."""
+    rows = batch * positions
+    parts = [
+        ("f1_", group_norm_graph(batch, positions, groups, dim, dtype, act, "checkpoint"), {}),
+        ("f2_", checkpoint_graph(rows, hidden // block, block, dtype, "gelu", True), {}),
+        ("b2_", checkpoint_backward_graph(rows, hidden // block, block, dtype, "gelu", True), {"q": "f2_q", "s": "f2_s"}),
+        ("b1_", group_norm_backward_graph(batch, positions, groups, dim, dtype, act, "checkpoint"),
+         {"q": "f1_q", "s": "f1_s", "r": "f1_r", "gamma": "f1_gamma", "beta": "f1_beta"}),
+    ]
+    inputs, ops, outputs = [], [], []
+    for prefix, part, shared in parts:
+        ren = lambda n, prefix=prefix, shared=shared: shared.get(n, prefix + n)  # noqa: E731
+        inputs += [TensorSpec(ren(t.name), t.dtype, t.dims) for t in part.inputs if t.name not in shared]
+        ops += [OpSpec(ren(o.out), o.opcode, tuple(ren(i) for i in o.inputs), dict(o.attr)) for o in part.ops]
+        outputs += [(ren(n), d) for n, d in part.outputs]
+    return GraphSpec(name=f"pattern_checkpointed_block_{dtype}_{act}_{batch}x{positions}x{groups}x{dim}_{hidden}", inputs=inputs, ops=ops,
+                     outputs=outputs, external=[("f1_y", "f2_x"), ("f2_y", "b2_dy"), ("b2_dx", "b1_dy")])
+
+
 # The five configurations the build is measured on, at their full sizes, and a
 # small sibling of each that still spans several tiles and a ragged tail.
 # Backward patterns measured next to them (same transformer-block shapes).
