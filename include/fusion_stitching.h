@@ -264,6 +264,44 @@ int32_t fs_codegen_available(void);
  * kernel), or a negative error.  Errors: FS_ERR_INVALID_ARG.                            */
 int64_t fs_plan_source(const fs_plan *p, char *text, size_t capacity);
 
+/* ---- group normalisation and 8-bit checkpoints ----------------------------------
+ * Four patterns about what forward keeps for backward; any other spelling of the same
+ * values runs as the per-op plan.  T is FS_F32, FS_F16 or FS_BF16; act is nothing,
+ * z * FS_SIGMOID(z), or FS_GELU_TANH(z).
+ *
+ * An 8-bit checkpoint of v: s = max |v| over a block * inv_max + tiny (FS_ABS, FS_REDUCE_MAX,
+ * FS_SCALE, FS_ADD_SCALAR), q = v / s (FS_DIV) stored as FS_E4M3, directly or through
+ * FS_CONVERT; both are outputs, s as FS_F32.  inv_max between 1 / 448 and 1 / 8, tiny between
+ * 1e-37 and 1e30 (1 / 448 and 1e-30, say: a block of zeros keeps zeros).  q * s is off by at
+ * most 2^-4 of |v| (2^-10 s below 2^-6 s).  A NaN is kept as NaN and leaves the block's scale
+ * alone; an infinity makes the scale infinite, itself NaN and the block's other values zero.
+ *
+ * "group_norm": x [batch, positions, groups, dim] of T, channels last; gamma, beta [groups, dim]
+ *   (leading extents of 1 allowed) of T.
+ *     mu = mean of x, v = mean of (x - mu)^2 over dim and positions (FS_REDUCE_MEAN along axes
+ *     3 and 1, in either order), r = FS_RSQRT(v + eps), n = (x - mu) * r,
+ *     z = n * gamma + beta, y = act(z)
+ *   Outputs: y (T); if wanted mu, r (FS_F32, [batch, 1, groups, 1]); if wanted a checkpoint of n
+ *   with one block per batch entry and group.
+ * "group_norm_backward": dy like x; n = (x - mu) * r from inputs x, mu and r, or n = q * s from a
+ *   checkpoint, its scale and r; gamma, and with an activation beta.
+ *     dz = dy * act'(n * gamma + beta), g = dz * gamma,
+ *     dx = (g - mean(g) - n * mean(g * n)) * r, dgamma = sum of dz * n, dbeta = sum of dz
+ *     (FS_REDUCE_SUM along axes 0 and 1, in either order)
+ *   where SiLU' is s * (1 + z * (1 - s)) with s = FS_SIGMOID(z), (1 - s) as FS_SCALE by -1 and
+ *   FS_ADD_SCALAR of 1, and GELU' is FS_GELU_TANH_GRAD.  Outputs: dx (T), dgamma, dbeta (FS_F32).
+ * "checkpoint": z = x, or x + bias with a bias that repeats along leading axes; a checkpoint of z
+ *   with blocks along the last axis, and y = act(z) where there is an activation.  Rank 1 to 4.
+ * "checkpoint_backward": z = q * s, stored as T; or dx = dy * act'(z) and, if wanted, its sum over
+ *   the leading axes (FS_REDUCE_SUM along axis 0, or axes 0 to k), FS_F32.
+ *
+ * Means, variances, scales and sums are float32; a variance is that of differences from values
+ * near the mean, never a difference of two sums.  Outputs of these plans may share no memory
+ * with an input or with another output: fs_execute, fs_execute_static and
+ * fs_program_execute return FS_ERR_INVALID_ARG for such a call before anything is launched.
+ * Normalising more positions than a workgroup keeps in registers, and the sums over positions
+ * and rows, take two or three launches and a workspace.                                   */
+
 /* ---- execution (the run-time hot path) --------------------------------------- */
 
 /* Enqueues the plan's kernel(s) on `hip_stream` (a hipStream_t; null = the
@@ -281,6 +319,7 @@ int64_t fs_plan_source(const fs_plan *p, char *text, size_t capacity);
  * in different orders, so their last bits may differ; and where rows of an odd number of
  * 16-bit elements lie on the tensor's 16-byte grid, which lane adds which elements depends
  * on the row's index, so that equal rows of a tensor may round differently.
+ * Group normalisation and 8-bit checkpoints refuse outputs that share memory (above).
  * Two calls that share a workspace must be ordered on one stream.
  * Errors: FS_ERR_INVALID_ARG, FS_ERR_WORKSPACE, FS_ERR_ALIGN, FS_ERR_HIP.         */
 fs_status fs_execute(const fs_plan *p, const void *const *inputs, void *const *outputs,

@@ -5,6 +5,7 @@
 from __future__ import annotations
 
 import concurrent.futures as cf
+import fcntl
 import os
 import subprocess
 import sys
@@ -111,11 +112,17 @@ def build_host_sanitized(verbose: bool = False) -> str:
             raise RuntimeError(f"sanitizer build of the host core failed: {src}\n{r.stderr}")
         return obj
 
-    with cf.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
-        objs = list(pool.map(compile_one, srcs))
-    r = subprocess.run([cxx, "-shared", "-fsanitize=address,undefined", "-o", HOST_SAN_LIB, *objs], capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"sanitizer link of the host core failed\n{r.stderr}")
+    # two tests may ask for it at the same time (test workers), and the other may have the library loaded: one build at a time, into a
+    # file of its own that takes the old one's place
+    fresh = os.path.join(OBJ_DIR, "host_san.new")
+    with open(os.path.join(OBJ_DIR, "san.lock"), "w") as lock:
+        fcntl.flock(lock, fcntl.LOCK_EX)
+        with cf.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+            objs = list(pool.map(compile_one, srcs))
+        r = subprocess.run([cxx, "-shared", "-fsanitize=address,undefined", "-o", fresh, *objs], capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"sanitizer link of the host core failed\n{r.stderr}")
+        os.replace(fresh, HOST_SAN_LIB)
     return HOST_SAN_LIB
 
 

@@ -93,7 +93,7 @@ std::vector<uint32_t> set_sizes(uint32_t groups) {
 std::vector<uint32_t> chunk_sets(const GroupNormP& p) {
   std::vector<uint32_t> sets;
   uint32_t narrow = 0;
-  for (uint32_t s = p.groups; s >= 1; --s) {
+  for (uint32_t s = std::min(p.groups, 256u * 8); s >= 1; --s) {   // (a thread has at most 8 values of a position)
     GroupNormP q = p;
     if (p.groups % s != 0 || !lay_out(&q, 256, s)) continue;
     if (sets.empty()) sets.push_back(s);

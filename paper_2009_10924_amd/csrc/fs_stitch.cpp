@@ -42,6 +42,15 @@ std::string build_stitched(const fs_graph& g, std::vector<Candidate>* out, PackF
     out->clear();
     *pack = PackForm();
     if (f.build(g, out, pack)) {
+      // a launch counts its threads in 32 bits: what asks for more (millions of workgroups that hold next to nothing) is no candidate
+      auto too_many = [](const Launch& l) {
+        uint64_t threads = 1;
+        for (int k = 0; k < 3; ++k) threads *= (uint64_t)l.shape.grid[k] * l.shape.block[k];
+        return threads >= (1ull << 32);
+      };
+      out->erase(std::remove_if(out->begin(), out->end(),
+                                [&](const Candidate& c) { return std::any_of(c.launches.begin(), c.launches.end(), too_many); }),
+                 out->end());
       if (!out->empty()) {
         for (Candidate& c : *out) c.apart = f.apart;
         // a family that only has its slow catch-all kernel for these extents (ragged or very long rows): the row

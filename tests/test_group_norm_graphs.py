@@ -143,3 +143,15 @@ def test_explorer_takes_the_block_apart_at_its_products():
     bad[names.index("b1_dx")] = ins[[t.name for t in spec.inputs].index("b1_dy")]
     with pytest.raises(B.FsError, match="FS_ERR_INVALID_ARG.*shares memory"):   # refused before the first of the four steps
         prog.bind(ins, bad, 0x900000000, prog.info["workspace_bytes"], 0)()
+
+
+def test_no_launch_asks_for_more_threads_than_32_bits_count():
+    most = (1 << 31) - 1
+    for spec in (group_norm_graph(most, 1, 1, 1), group_norm_graph(most // 64, 1, 64, 1, keep="stats"), group_norm_graph(1, 1, most, 1), group_norm_graph(1, most, 1, 1),
+                 group_norm_backward_graph(most, 1, 1, 1), group_norm_backward_graph(1, 1, most, 1), checkpoint_graph(most, 1, 1), checkpoint_graph(1, 1, most),
+                 checkpoint_backward_graph(most, 1, 1), checkpoint_backward_graph(1, most, 1), checkpoint_backward_graph(most, 1, 1, act="none")):
+        p = plan(spec)
+        for c in p.candidates():
+            assert np.prod([int(g) * b for g, b in zip(c["grid"], c["block"])]) < 1 << 32, (spec.name, c["kernel"])
+    assert plan(group_norm_graph(most, 1, 1, 1)).info["pattern"] == "unfused"     # a workgroup per value: too many
+    assert plan(group_norm_backward_graph(most, 1, 1, 1)).info["pattern"] == "group_norm_backward"   # several entries per workgroup
