@@ -79,6 +79,11 @@ bool cut(GroupNormP* p, uint32_t want) {
   p->div_chunks = make_fastdiv(p->chunks);
   return p->div_chunks.d != 0 && (uint64_t)p->batch * p->chunks * p->sets < (1ull << 31);
 }
+// words of LDS that the items of a position's channels take (gn_pitch)
+uint32_t item_pitch(const GroupNormP& p) {
+  const uint32_t width = p.set_groups * p.dim;
+  return width + (p.vec > 1 ? width / p.vec : 0);
+}
 // sets of 1 group, of more by twos, of all
 std::vector<uint32_t> set_sizes(uint32_t groups) {
   std::vector<uint32_t> s;
@@ -241,7 +246,7 @@ bool build_group_norm(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
       const uint64_t held = (uint64_t)sh.K * p.rows_at_once;
       if (held < p.positions || (sh.K > 1 && held >= 2ull * p.positions + p.rows_at_once)) continue;
       if (held * p.channels * esz >= (1ull << 32)) continue;   // the kernel's distances within a batch entry
-      const uint32_t items = p.rows_at_once * (p.whole ? p.set_vecs : gs * p.dim);
+      const uint32_t items = p.rows_at_once * (p.whole ? p.set_vecs : item_pitch(p));
       p.vecs_per_lane = sh.K;
       p.fold_log2 = fold_lanes_log2(sh.threads, gs, p.rows_at_once * (p.whole ? p.dim / p.vec : p.dim));
       const int64_t lds = 4ll * ((has_8bit ? 2 : 1) * (int64_t)items + 3 * gs);
@@ -279,7 +284,7 @@ bool build_group_norm(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
       GroupNormP p = base;
       if (!lay_out(&p, 256, gs) || !cut(&p, want) || p.chunks == last_chunks) continue;
       last_chunks = p.chunks;
-      const uint32_t items = p.rows_at_once * (p.whole ? p.set_vecs : gs * p.dim);
+      const uint32_t items = p.rows_at_once * (p.whole ? p.set_vecs : item_pitch(p));
       const int64_t lds = 4ll * ((has_8bit ? 4 : 2) * (int64_t)items + p.rows_at_once);
       const int64_t chunk_bytes = aligned((has_8bit ? 16ll : 8ll) * p.batch * p.chunks * p.groups);
       const bool join = joins(p, gs, has_8bit ? 8 : 16);
@@ -459,7 +464,7 @@ bool build_group_norm_backward(const fs_graph& g, std::vector<Candidate>* out, P
       p.entry_blocks = (p.batch + e - 1) / e;
       const bool fold = p.entry_blocks > 1;
       const int64_t sum_bytes = aligned(8ll * p.entry_blocks * pitch);
-      const int64_t lds = 4ll * ((int64_t)p.rows_at_once * width + 3 * width + 2 * gs + (e > 1 ? 2 * width : 0));
+      const int64_t lds = 4ll * (2ll * p.rows_at_once * item_pitch(p) + 3 * width + 2 * gs + (e > 1 ? 2 * width : 0));
       if (lds > 64 * 1024 || (uint64_t)p.entry_blocks * p.sets >= (1ull << 31)) continue;
       Candidate c = make_candidate(g, "group_norm_backward", FS_SCHEME_LDS, K_GN_BWD_SLAB);
       Launch& l = c.launches.front();
@@ -503,7 +508,7 @@ bool build_group_norm_backward(const fs_graph& g, std::vector<Candidate>* out, P
       if (!lay_out(&p, 256, gs) || !cut(&p, want) || p.chunks == last_chunks) continue;
       last_chunks = p.chunks;
       const uint32_t width = gs * p.dim, rows = p.batch * p.chunks;
-      const int64_t lds = 4ll * ((int64_t)p.rows_at_once * width + 3 * width);
+      const int64_t lds = 4ll * (2ll * p.rows_at_once * item_pitch(p) + 3 * width);
       const int64_t chunk_bytes = aligned(8ll * rows * pitch), mean_bytes = aligned(8ll * rows * p.groups);
       const bool join = joins(p, gs, 16);
       Candidate c = make_candidate(g, "group_norm_backward", FS_SCHEME_GLOBAL, K_GN_BWD_SUMS);

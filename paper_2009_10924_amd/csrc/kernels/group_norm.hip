@@ -2,7 +2,10 @@
 // and channels of a group; beside it the 8-bit checkpoint of (x - mean) rstd.
 //
 // A group's values are read once where a workgroup can hold them (k_gn_slab).  Otherwise a first launch gathers mean and
-// sum of squared deviations per chunk of positions, a second joins the chunks, a third reads x again.  No variance is a
+// sum of squared deviations per chunk of positions, and a last one, which joins the chunks of its groups, reads x again; where
+// that joins too many for every workgroup, a launch in between does it once.  Bound by memory from some 30 MB on: bf16
+// [16, 16384, 256] with SiLU, 64 us for its 268 MB (24 us gather, 40 read and write again: 5.6 and 6.7 TB/s); smaller ones by what a
+// workgroup does one after the other: bf16 [8, 4096, 320] with a checkpoint 19.5 us, 8.5 for its bytes alone.  No variance is a
 // difference of large sums: inside registers it is the mean of squared deviations from the known mean, and partial results
 // join as M2 = M2a + M2b + (mean_b - mean_a)^2 na nb / (na + nb).
 #include <hip/hip_runtime.h>
@@ -19,8 +22,9 @@ __global__ void __launch_bounds__(NT) k_gn_slab(const T* x, const T* gamma, cons
                                                 float* scale_out, const GnShape p) {
   extern __shared__ __align__(16) float lds[];
   constexpr int G = WHOLE ? 1 : VEC;   // groups that a vector can touch
+  constexpr int ITEMS = WHOLE ? GN_ONE : GN_DENSE;
   const uint32_t width = p.set_groups * p.dim;
-  const uint32_t n_items = p.rows_at_once * (WHOLE ? p.set_vecs : width);
+  const uint32_t n_items = p.rows_at_once * gn_pitch<ITEMS, VEC>(p);
   float* const items = lds;
   float* const most = lds + n_items;                       // with a checkpoint only
   float* const stat = lds + (q ? 2u : 1u) * n_items;       // [3][set_groups]
@@ -49,10 +53,10 @@ __global__ void __launch_bounds__(NT) k_gn_slab(const T* x, const T* gamma, cons
     for (int e = 0; e < VEC; ++e) a[e] += valid(k) ? v[e] : 0.0f;
     done(a);
   }
-  gn_deposit<WHOLE, VEC>(items, p, l, a);
+  gn_deposit<ITEMS, VEC>(items, p, l, a);
   __syncthreads();
-  gn_groups<WHOLE, VEC>(p, [&](uint32_t g, uint32_t lane, bool writes, uint32_t first, uint32_t per, uint32_t pitch) {
-    const float s = gn_fold<OpSum>(items, p, lane, first, per, pitch);
+  gn_groups<ITEMS, VEC>(p, [&](uint32_t g, uint32_t lane, bool writes, uint32_t first, uint32_t per) {
+    const float s = gn_fold<ITEMS, VEC, OpSum>(items, p, lane, first, per);
     if (writes) stat[g] = s * p.inv_count;
   });
   __syncthreads();
@@ -80,12 +84,12 @@ __global__ void __launch_bounds__(NT) k_gn_slab(const T* x, const T* gamma, cons
     done(a);
     done(far);
   }
-  gn_deposit<WHOLE, VEC>(items, p, l, a);
-  if (q) gn_deposit_max<WHOLE, VEC>(most, p, l, far);
+  gn_deposit<ITEMS, VEC>(items, p, l, a);
+  if (q) gn_deposit_max<ITEMS, VEC>(most, p, l, far);
   __syncthreads();
-  gn_groups<WHOLE, VEC>(p, [&](uint32_t g, uint32_t lane, bool writes, uint32_t first, uint32_t per, uint32_t pitch) {
-    const float r = fast_rsqrt(gn_fold<OpSum>(items, p, lane, first, per, pitch) * p.inv_count + p.eps);
-    const float s = q ? scale_of(gn_fold<OpMax>(most, p, lane, first, per, pitch) * r, p.inv_max, p.tiny) : 0.0f;
+  gn_groups<ITEMS, VEC>(p, [&](uint32_t g, uint32_t lane, bool writes, uint32_t first, uint32_t per) {
+    const float r = fast_rsqrt(gn_fold<ITEMS, VEC, OpSum>(items, p, lane, first, per) * p.inv_count + p.eps);
+    const float s = q ? scale_of(gn_fold<ITEMS, VEC, OpMax>(most, p, lane, first, per) * r, p.inv_max, p.tiny) : 0.0f;
     if (writes) {
       stat[p.set_groups + g] = r;
       stat[2u * p.set_groups + g] = s;
@@ -140,9 +144,9 @@ __global__ void __launch_bounds__(NT) k_gn_slab(const T* x, const T* gamma, cons
 template <typename T, int VEC, bool WHOLE, bool RANGE>
 __global__ void __launch_bounds__(256) k_gn_stats(const T* x, float* out, const GnShape p) {
   extern __shared__ __align__(16) float lds[];
-  constexpr int U = 4;
+  constexpr int U = 4, ITEMS = WHOLE ? GN_ONE : RANGE ? GN_SPACED : GN_DENSE;
   const uint32_t width = p.set_groups * p.dim;
-  const uint32_t n_items = p.rows_at_once * (WHOLE ? p.set_vecs : width);
+  const uint32_t n_items = p.rows_at_once * gn_pitch<ITEMS, VEC>(p);
   float* const means = lds;
   float* const squares = lds + n_items;
   float* const weight = lds + (RANGE ? 4u : 2u) * n_items;   // [rows_at_once]
@@ -237,31 +241,30 @@ __global__ void __launch_bounds__(256) k_gn_stats(const T* x, float* out, const 
       squares[at] = d;
       if constexpr (RANGE) lds[2u * n_items + at] = lo[0], lds[3u * n_items + at] = hi[0];
     }
-  } else if (l.live) {
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      const uint32_t at = l.row * width + l.col + e;
-      means[at] = c[e];
-      squares[at] = s2[e];
-      if constexpr (RANGE) lds[2u * n_items + at] = lo[e], lds[3u * n_items + at] = hi[e];
+  } else {
+    gn_deposit<ITEMS, VEC>(means, p, l, c);
+    gn_deposit<ITEMS, VEC>(squares, p, l, s2);
+    if constexpr (RANGE) {
+      gn_deposit<ITEMS, VEC>(lds + 2u * n_items, p, l, lo);
+      gn_deposit<ITEMS, VEC>(lds + 3u * n_items, p, l, hi);
     }
   }
   if (l.live && l.vec == 0) weight[l.row] = WHOLE ? count * VEC : count;
   __syncthreads();
   const float inv = 1.0f / ((float)here * (float)p.dim);
-  gn_groups<WHOLE, VEC>(p, [&](uint32_t g, uint32_t lane, bool writes, uint32_t first, uint32_t per, uint32_t pitch) {
+  gn_groups<ITEMS, VEC>(p, [&](uint32_t g, uint32_t lane, bool writes, uint32_t first, uint32_t per) {
     const uint32_t n_it = p.rows_at_once * per, lanes = 1u << p.fold_log2;
     float m = 0.0f, d = 0.0f, low = __builtin_inff(), high = -__builtin_inff();
 #pragma unroll 4
     for (uint32_t i = lane; i < n_it; i += lanes) {
-      const uint32_t rr = fast_div(i, p.div_per), at = rr * pitch + first + (i - rr * per);
+      const uint32_t rr = fast_div(i, p.div_per), at = rr * gn_pitch<ITEMS, VEC>(p) + gn_item<ITEMS, VEC>(first + (i - rr * per));
       m = __builtin_fmaf(weight[rr], means[at], m);
       if constexpr (RANGE) low = fminf(low, lds[2u * n_items + at]), high = fmaxf(high, lds[3u * n_items + at]);
     }
     m = group_allreduce<OpSum>(m, (int)lanes) * inv;
 #pragma unroll 4
     for (uint32_t i = lane; i < n_it; i += lanes) {
-      const uint32_t rr = fast_div(i, p.div_per), at = rr * pitch + first + (i - rr * per);
+      const uint32_t rr = fast_div(i, p.div_per), at = rr * gn_pitch<ITEMS, VEC>(p) + gn_item<ITEMS, VEC>(first + (i - rr * per));
       const float apart = means[at] - m;
       d += __builtin_fmaf(apart * apart, weight[rr], squares[at]);
     }

@@ -34,54 +34,69 @@ __device__ __forceinline__ uint32_t gn_block(uint32_t blocks) {
   return (blocks & 7u) == 0 ? (b & 7u) * (blocks >> 3) + (b >> 3) : b;
 }
 
-// Items of a thread in LDS: WHOLE (its channels are of one group) one per vector, otherwise one per channel.
-template <bool WHOLE, int VEC>
+// What a workgroup's threads have gathered, in LDS for others to add up: gn_pitch items per position.  GN_ONE: a thread's channels are
+// of one group and one item.  Otherwise an item per channel, and GN_SPACED leaves a word out after every VEC of them: neighbouring
+// lanes write an odd distance apart, where eight of them meet in every bank that an access touches if the items are GN_DENSE, but
+// write single words, and reading takes more arithmetic.  Four items per channel (the statistics with their range) are 3 to 7 %
+// of the call faster spaced, the two of the backward pass 1 to 6 %; the one or two of k_gn_slab 8 to 10 % slower, two without a
+// range 1 %.
+enum GnItems { GN_ONE, GN_DENSE, GN_SPACED };
+template <int ITEMS, int VEC>
+__device__ __forceinline__ uint32_t gn_item(uint32_t i) {   // vector (GN_ONE) or channel i of the set
+  return i + (ITEMS == GN_SPACED && VEC > 1 ? i / VEC : 0u);
+}
+template <int ITEMS, int VEC>
+__device__ __forceinline__ uint32_t gn_pitch(const GnShape& p) {
+  return ITEMS == GN_ONE ? p.set_vecs : gn_item<ITEMS, VEC>(p.set_groups * p.dim);
+}
+template <int ITEMS, int VEC>
 __device__ __forceinline__ void gn_deposit(float* items, const GnShape& p, const GnLane& l, const float (&v)[VEC]) {
   if (!l.live) return;
-  if constexpr (WHOLE) {
+  float* const row = items + l.row * gn_pitch<ITEMS, VEC>(p);
+  if constexpr (ITEMS == GN_ONE) {
     float s = v[0];
 #pragma unroll
     for (int e = 1; e < VEC; ++e) s += v[e];
-    items[l.row * p.set_vecs + l.vec] = s;
+    row[l.vec] = s;
   } else {
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) items[l.row * (p.set_groups * p.dim) + l.col + e] = v[e];
+    for (int e = 0; e < VEC; ++e) row[gn_item<ITEMS, VEC>(l.col + e)] = v[e];
   }
 }
-template <bool WHOLE, int VEC>
+template <int ITEMS, int VEC>
 __device__ __forceinline__ void gn_deposit_max(float* items, const GnShape& p, const GnLane& l, const float (&v)[VEC]) {
-  if constexpr (WHOLE) {
+  if constexpr (ITEMS == GN_ONE) {
     float s = v[0];
 #pragma unroll
     for (int e = 1; e < VEC; ++e) s = fmaxf(s, v[e]);
     if (l.live) items[l.row * p.set_vecs + l.vec] = s;
   } else {
-    gn_deposit<false, VEC>(items, p, l, v);
+    gn_deposit<ITEMS, VEC>(items, p, l, v);
   }
 }
 
 // 1 << fold_log2 lanes per group run through its items, group by group where there are more groups than such lane sets:
-// f(group, lane among them, first item, items a position has of the group, distance from position to position), called by
-// whole wavefronts (with the last group again where lanes are left over).
-template <bool WHOLE, int VEC, typename F>
+// f(group, lane among them, first item, items a position has of the group), called by whole wavefronts (with the last group again
+// where lanes are left over).
+template <int ITEMS, int VEC, typename F>
 __device__ __forceinline__ void gn_groups(const GnShape& p, F&& f) {
   const uint32_t lanes = 1u << p.fold_log2, sets = blockDim.x >> p.fold_log2;
-  const uint32_t per = WHOLE ? p.dim / VEC : p.dim, pitch = WHOLE ? p.set_vecs : p.set_groups * p.dim;
+  const uint32_t per = ITEMS == GN_ONE ? p.dim / VEC : p.dim;
   for (uint32_t g0 = 0; g0 < p.set_groups; g0 += sets) {
     const uint32_t g = g0 + (threadIdx.x >> p.fold_log2), lane = threadIdx.x & (lanes - 1u);
     const uint32_t gc = min(g, p.set_groups - 1u);
-    f(gc, lane, lane == 0 && g < p.set_groups, gc * per, per, pitch);
+    f(gc, lane, lane == 0 && g < p.set_groups, gc * per, per);
   }
 }
 // sum (or maximum) of a group's items
-template <typename OP>
-__device__ __forceinline__ float gn_fold(const float* items, const GnShape& p, uint32_t lane, uint32_t first, uint32_t per, uint32_t pitch) {
+template <int ITEMS, int VEC, typename OP>
+__device__ __forceinline__ float gn_fold(const float* items, const GnShape& p, uint32_t lane, uint32_t first, uint32_t per) {
   float a = 0.0f;
   const uint32_t n = p.rows_at_once * per, lanes = 1u << p.fold_log2;
 #pragma unroll 4
   for (uint32_t i = lane; i < n; i += lanes) {
     const uint32_t row = fast_div(i, p.div_per);
-    a = OP::apply(a, items[row * pitch + first + (i - row * per)]);
+    a = OP::apply(a, items[row * gn_pitch<ITEMS, VEC>(p) + gn_item<ITEMS, VEC>(first + (i - row * per))]);
   }
   return group_allreduce<OP>(a, (int)lanes);
 }

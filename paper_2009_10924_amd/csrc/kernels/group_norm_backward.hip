@@ -66,26 +66,34 @@ struct GnGradient {
   }
 };
 
-// Sums over the workgroup's positions of what every thread has gathered per channel: channel c of the set to out[c], and times
-// gamma to weighted[c], by 1 << fold_log2 lanes each.  `items`: rows_at_once * width floats of LDS.  Over several batch entries the
-// sums go into `totals` and, with the last one, to out.
+// Sums over the workgroup's positions of what every thread has gathered per channel, for channel c of the set to out_a[c] and
+// out_b[c], and times gamma to weighted[c] and weighted[width + c], by 1 << fold_log2 lanes each.  Over several batch entries the sums
+// go into `totals`, and with the last one to the outputs.  (Both in one go: two barriers and a chain of loads less than one after the
+// other, 3 % of the calls with two launches and up to 20 % of those with many short entries.)
+constexpr int kGnSums = GN_SPACED;
 template <int VEC>
-__device__ __forceinline__ void gn_channel_sums(float* items, const GnShape& p, const GnLane& l, const float (&v)[VEC], const float* gain, float* weighted,
-                                                float* out, float* totals = nullptr, bool first = true, bool last = true) {
-  const uint32_t width = p.set_groups * p.dim, lanes = 1u << p.fold_log2, lane = threadIdx.x & (lanes - 1u);
-  gn_deposit<false, VEC>(items, p, l, v);
+__device__ __forceinline__ void gn_channel_sums(float* items, const GnShape& p, const GnLane& l, const float (&a)[VEC], const float (&b)[VEC], const float* gain,
+                                                float* weighted, float* out_a, float* out_b, float* totals = nullptr, bool first = true, bool last = true) {
+  const uint32_t width = p.set_groups * p.dim, pitch = gn_pitch<kGnSums, VEC>(p), n_items = p.rows_at_once * pitch, lanes = 1u << p.fold_log2, lane = threadIdx.x & (lanes - 1u);
+  gn_deposit<kGnSums, VEC>(items, p, l, a);
+  gn_deposit<kGnSums, VEC>(items + n_items, p, l, b);
   __syncthreads();
   for (uint32_t c0 = 0; c0 < width; c0 += blockDim.x >> p.fold_log2) {
-    const uint32_t c = c0 + (threadIdx.x >> p.fold_log2), cc = min(c, width - 1u);
-    float a = 0.0f;
+    const uint32_t c = c0 + (threadIdx.x >> p.fold_log2), cc = min(c, width - 1u), from = gn_item<kGnSums, VEC>(cc);
+    float sa = 0.0f, sb = 0.0f;
 #pragma unroll 4
-    for (uint32_t r = lane; r < p.rows_at_once; r += lanes) a += items[r * width + cc];
-    a = group_allreduce<OpSum>(a, (int)lanes);
+    for (uint32_t r = lane; r < p.rows_at_once; r += lanes) {
+      sa += items[from + r * pitch];
+      sb += items[n_items + from + r * pitch];
+    }
+    sa = group_allreduce<OpSum>(sa, (int)lanes);
+    sb = group_allreduce<OpSum>(sb, (int)lanes);
     if (lane == 0 && c < width) {
-      weighted[c] = a * gain[c];
-      if (!first) a += totals[c];
-      if (last) out[c] = a;
-      else totals[c] = a;
+      weighted[c] = sa * gain[c];
+      weighted[width + c] = sb * gain[c];
+      if (!first) sa += totals[c], sb += totals[width + c];
+      if (last) out_a[c] = sa, out_b[c] = sb;
+      else totals[c] = sa, totals[width + c] = sb;
     }
   }
   __syncthreads();
@@ -126,7 +134,7 @@ __global__ void __launch_bounds__(NT) k_gn_bwd_slab(const typename GnValue<T, FR
   extern __shared__ __align__(16) float lds[];
   const uint32_t width = p.set_groups * p.dim;
   float* const items = lds;
-  float* const gain = lds + p.rows_at_once * width;
+  float* const gain = lds + 2u * p.rows_at_once * gn_pitch<kGnSums, VEC>(p);
   float* const sum_a = gain + width;
   float* const sum_b = sum_a + width;
   float* const means = sum_b + width;   // [set_groups][2]
@@ -171,8 +179,7 @@ __global__ void __launch_bounds__(NT) k_gn_bwd_slab(const typename GnValue<T, FR
     }
 #pragma unroll
     for (int e = 0; e < VEC; ++e) bb[e] *= ch.scale[e];
-    gn_channel_sums<VEC>(items, p, l, a, gain, sum_a, out_a + out, totals, !MANY || n == n0, !MANY || n + 1u == n1);
-    gn_channel_sums<VEC>(items, p, l, bb, gain, sum_b, out_b + out, totals + width, !MANY || n == n0, !MANY || n + 1u == n1);
+    gn_channel_sums<VEC>(items, p, l, a, bb, gain, sum_a, out_a + out, out_b + out, totals, !MANY || n == n0, !MANY || n + 1u == n1);
     gn_group_means(p, sum_a, sum_b, [&](uint32_t g, float m1, float m2) {
       means[2u * g] = m1;
       means[2u * g + 1u] = m2;
@@ -211,6 +218,7 @@ __global__ void __launch_bounds__(256) k_gn_bwd_sums(const typename GnValue<T, F
   extern __shared__ __align__(16) float lds[];
   constexpr int U = 4;
   const uint32_t width = p.set_groups * p.dim;
+  float* const gain = lds + 2u * p.rows_at_once * gn_pitch<kGnSums, VEC>(p);
   const uint32_t bc = fast_div(blockIdx.x, p.div_sets), set = blockIdx.x - bc * p.sets;
   const uint32_t n = fast_div(bc, p.div_chunks), chunk = bc - n * p.chunks;
   const uint32_t r0 = chunk * p.chunk_rows, r1 = min(r0 + p.chunk_rows, p.positions);
@@ -235,7 +243,7 @@ __global__ void __launch_bounds__(256) k_gn_bwd_sums(const typename GnValue<T, F
     issue();
     GnChannels<T, VEC, FROM8> ch;
     ch.load(p, l, n, set, centre, rstd, gamma, beta);
-    gn_keep_gain<VEC>(lds + p.rows_at_once * width, l, ch.ga);
+    gn_keep_gain<VEC>(gain, l, ch.ga);
     auto add = [&](typename VecIo<X, VEC>::Raw rx, typename VecIo<T, VEC>::Raw rd) {
       float v[VEC], d[VEC];
       VecIo<X, VEC>::widen(rx, v);
@@ -265,11 +273,9 @@ __global__ void __launch_bounds__(256) k_gn_bwd_sums(const typename GnValue<T, F
     for (int e = 0; e < VEC; ++e) b[e] *= ch.scale[e];
   }
   float* const to = sums + (size_t)bc * 2u * p.sum_pitch + set * width;
-  float* const gain = lds + p.rows_at_once * width;
   float* const sum_a = gain + width;
   float* const sum_b = sum_a + width;
-  gn_channel_sums<VEC>(lds, p, l, a, gain, sum_a, to);
-  gn_channel_sums<VEC>(lds, p, l, b, gain, sum_b, to + p.sum_pitch);
+  gn_channel_sums<VEC>(lds, p, l, a, b, gain, sum_a, to, to + p.sum_pitch);
   float* const group_to = means + 2u * ((size_t)bc * p.groups + set * p.set_groups);
   gn_group_means(p, sum_a, sum_b,
                  [&](uint32_t g, float m1, float m2) { *reinterpret_cast<f32x2*>(group_to + 2u * g) = f32x2{m1, m2}; });
