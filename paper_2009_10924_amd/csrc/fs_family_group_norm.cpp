@@ -118,8 +118,8 @@ bool joins(const GroupNormP& p, uint32_t set_groups, uint32_t loads) {
 // What the launches read and write, and the estimate of their time.  These kernels are short: most of what a shape costs is the
 // chain of instructions of one wavefront (which hardly any other covers) against its share of the arithmetic and the bytes, which
 // the general evaluator has no terms for.  Constants fitted to every candidate of 700 shapes of 1 to 2^26 elements, three dtypes, timed
-// on three sets of buffers in turn; the candidate chosen was 2.0 % behind the fastest (geometric mean), 12 % by the general
-// evaluator.
+// on three sets of buffers in turn; the candidate chosen was 2.2 % behind the fastest (geometric mean of 500 further shapes), 12 % by
+// the general evaluator.
 struct Traffic {
   double read_bytes = 0, written_bytes = 0, act = 0;   // act: 0 none, 1 SiLU, 1.5 tanh-GELU
   bool backward = false;
@@ -168,7 +168,9 @@ double passes_us(const GroupNormP& p, const Traffic& t, size_t n_launches) {
                   m.partials * 16.0 * p.batch * p.chunks * p.channels / 6.6e6 + m.join * p.chunks * p.set_groups;
   if (p.sets > 1) memory *= 1.0 + m.shared_lines * 128.0 / ((double)p.set_groups * p.dim * dtype_bytes(p.dt));
   const double workgroups = (double)p.batch * p.sets * p.chunks;
-  const double starts = 1.1 * std::max(0.0, waves - 2.0);   // very many short workgroups: their prologues, in both launches
+  // very many short workgroups: their prologues, in both launches; and the second one of a compute unit, whose gathering ends when
+  // the first one's does (twice the workgroups are 5 % slower in calls of 12 us and 8 % faster in those of 50)
+  const double starts = 1.1 * std::max(0.0, waves - 2.0) + (workgroups > 256.0 ? 1.1 : 0.0);
   if (workgroups < 400) memory *= 1.05;   // one wavefront per SIMD: loads and arithmetic take turns
   memory = std::max(memory, few_units(2.0 * t.read_bytes + t.written_bytes, workgroups, 4.0e4));
   return m.fixed + m.launch * ((double)n_launches - 2.0) + starts + std::max(issue, memory) + m.overlap * std::min(issue, memory) + m.item * items_per_lane(p, t.backward);
