@@ -282,7 +282,7 @@ int64_t fs_plan_source(const fs_plan *p, char *text, size_t capacity);
  *     3 and 1, in either order), r = FS_RSQRT(v + eps), n = (x - mu) * r,
  *     z = n * gamma + beta, y = act(z)
  *   Outputs: y (T); if wanted mu, r (FS_F32, [batch, 1, groups, 1]); if wanted a checkpoint of n
- *   with one block per batch entry and group.
+ *   with one block per batch entry and group (eps > 0, and 1 / (sqrt(eps) * tiny) below 1e38).
  * "group_norm_backward": dy like x; n = (x - mu) * r from inputs x, mu and r, or n = q * s from a
  *   checkpoint, its scale and r; gamma, and with an activation beta.
  *     dz = dy * act'(n * gamma + beta), g = dz * gamma,

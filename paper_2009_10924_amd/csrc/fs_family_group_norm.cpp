@@ -230,6 +230,8 @@ bool build_group_norm(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
     return true;
   base.eps = (float)st.scalars[0];
   if (has_8bit) {
+    // values become 8 bits by one factor, rstd / scale: finite for groups of equal values too
+    if (!(st.scalars[0] > 0.0 && 1.0 / (std::sqrt(st.scalars[0]) * st.scalars[81]) < 1e38)) return true;
     base.inv_max = (float)st.scalars[80];
     base.tiny = (float)st.scalars[81];
   }

@@ -12,9 +12,9 @@ template <int ACT> __device__ __forceinline__ float activate(float z) {
 }
 template <int ACT> __device__ __forceinline__ float activation_slope(float z) {
   if constexpr (ACT == fs::ACT_GELU) {
-    // s + z s (1 - s) d(2u)/dz with s = 1 / (1 + exp(-2u)), u = c z (1 + a z^2): 16 operations, a transcendental one counted as 4
+    // s + z s (1 - s) d(2u)/dz with s = 1 / (1 + exp(-2u)), u = c z (1 + a z^2): 17 operations, a transcendental one counted as 4
     constexpr float c = 0.7978845608028654f, a = 0.044715f, k = -2.0f * c * kLog2e;
-    const float z2 = z * z;
+    const float z2 = fminf(z * z, 1e20f);   // (s is 0 or 1 long before: what it is multiplied with then has to be finite)
     const float s = fast_rcp(1.0f + __builtin_amdgcn_exp2f(z * __builtin_fmaf(k * a, z2, k)));
     const float y = z * s;
     return __builtin_fmaf(__builtin_fmaf(-y, s, y), __builtin_fmaf(6.0f * c * a, z2, 2.0f * c), s);

@@ -126,20 +126,13 @@ __global__ void __launch_bounds__(1024) k_checkpoint_long(const T* x, const T* b
 
 // ---- use, element by element -------------------------------------------------------------------------------------------
 // The tensor as one run of n values, block i of them at [i cols, (i + 1) cols).  With STRADDLE a lane's vector may reach into
-// the next block (which needs cols >= VEC: it reaches into one at most).
+// the next block (cols >= VEC, so it reaches into one at most, and n >= VEC).
 template <typename T, int VEC, int ACT, bool STRADDLE, bool STREAM>
 __global__ void __launch_bounds__(256) k_checkpoint_grad(const e4m3_t* q, const float* scale, const T* dy, T* out, uint32_t n, uint32_t cols_d,
                                                          uint32_t cols_m, uint32_t cols_s) {
   constexpr int U = 2;
   const FastDiv cols = {cols_d, cols_m, cols_s};
   const uint32_t first = (blockIdx.x * (256u * U) + threadIdx.x) * VEC;
-  if (n < VEC) {   // one short run
-    if (threadIdx.x < n && blockIdx.x == 0) {
-      const float z = load1(q + threadIdx.x) * scale[fast_div(threadIdx.x, cols)];
-      store1(out + threadIdx.x, ACT == ACT_NONE ? z : load1(dy + threadIdx.x) * activation_slope<ACT>(z));
-    }
-    return;
-  }
   typename VecIo<e4m3_t, VEC>::Raw rq[U];
   typename VecIo<T, VEC>::Raw rd[U];
   float s0[U], s1[U];

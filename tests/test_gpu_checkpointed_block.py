@@ -270,6 +270,35 @@ def test_checkpoint_of_a_nan_restores_a_nan_there_alone():
 
 
 @pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("size", [1e3, 1e15, 1e25, 1e35])
+def test_slopes_of_very_large_values_are_zero_and_one(act, size):
+    """dx = dy act'(q s) for q s up to 448 `size`, whose square is no float32."""
+    for dbias in (False, True):
+        spec = checkpoint_backward_graph(40, 2, 24, "f32", act, dbias)
+        inp = make_inputs(spec, seed=3)
+        inp["s"] = np.full_like(inp["s"], size)
+        with np.errstate(over="ignore"):
+            ref = O.evaluate(spec, inp)
+        got, _, info, _ = run_spec(spec, inp)
+        assert info["pattern"] == "checkpoint_backward"
+        for name, _ in spec.outputs:
+            within(got[name], ref[name], bounds(spec, inp, ref, "f32")[name], f"{info['kernel']}/{name}")
+
+
+@pytest.mark.parametrize("eps", [1e-5, 1e-15, 1e-18])
+def test_checkpoint_of_groups_of_zeros_is_zero(eps):
+    """1 / sqrt(eps) and the scale's reciprocal are as large as can be there: 0 all the same, in the kernels and where they are not taken."""
+    for shape in ((2, 40, 4, 8), (2, 40, 4, 7), (1, 9000, 2, 8)):
+        spec = group_norm_graph(*shape, dtype="bf16", act="none", keep="checkpoint", eps=eps)
+        inp = make_inputs(spec, seed=1)
+        inp["x"] = quantise(np.zeros(shape), "bf16")
+        for opts in [{"candidate": i} for i in range(B.Plan(B.Graph.from_spec(spec)).info["n_candidates"])]:
+            got, _, info, _ = run_spec(spec, inp, **opts)
+            assert not got["q"].any() and np.isfinite(got["s"]).all(), info["kernel"]
+            assert np.array_equal(got["z"], np.broadcast_to(O.to_f64(inp["beta"], "bf16"), shape)), info["kernel"]
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
 def test_gradient_through_a_checkpoint_stays_near_the_exact_one(act):
     """What the 8 bits cost a gradient: z is off by at most 2^-4 |z| (2^-10 s near zero), and the slope changes by at most
     max |act''| = 0.8 (0.5 for SiLU) times that; the sum over rows by the sum of these."""

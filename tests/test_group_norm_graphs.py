@@ -155,3 +155,12 @@ def test_no_launch_asks_for_more_threads_than_32_bits_count():
             assert np.prod([int(g) * b for g, b in zip(c["grid"], c["block"])]) < 1 << 32, (spec.name, c["kernel"])
     assert plan(group_norm_graph(most, 1, 1, 1)).info["pattern"] == "unfused"     # a workgroup per value: too many
     assert plan(group_norm_backward_graph(most, 1, 1, 1)).info["pattern"] == "group_norm_backward"   # several entries per workgroup
+
+
+def test_checkpoint_factors_stay_finite():
+    """rstd / scale of a group of equal values is 1 / (sqrt(eps) tiny): where that is no float32, the ops run one by one."""
+    for eps, tiny, pattern in ((1e-5, 1e-30, "group_norm"), (1e-12, 1e-30, "group_norm"), (1e-18, 1e-30, "unfused"), (1e-5, 1e-36, "unfused"), (0.0, 1e-30, "unfused")):
+        spec = rewired(group_norm_graph(2, 9, 4, 8, "f32", "silu", "checkpoint", eps=eps), "s", value=tiny)
+        assert plan(spec).info["pattern"] == pattern, (eps, tiny)
+        spec = group_norm_graph(2, 9, 4, 8, "f32", "silu", "stats", eps=eps)
+        assert plan(spec).info["pattern"] == "group_norm"
