@@ -299,8 +299,8 @@ int64_t fs_plan_source(const fs_plan *p, char *text, size_t capacity);
  * near the mean, never a difference of two sums.  Outputs of these plans may share no memory
  * with an input or with another output: fs_execute, fs_execute_static and
  * fs_program_execute return FS_ERR_INVALID_ARG for such a call before anything is launched.
- * Normalising more positions than a workgroup keeps in registers, and the sums over positions
- * and rows, take two or three launches and a workspace.                                   */
+ * Normalising more positions than a workgroup keeps in registers, and the sums over more than a
+ * few rows or batch entries, take two or three launches and a workspace.                                   */
 
 /* ---- execution (the run-time hot path) --------------------------------------- */
 

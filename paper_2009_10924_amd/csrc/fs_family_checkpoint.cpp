@@ -326,11 +326,15 @@ bool build_checkpoint_backward(const fs_graph& g, std::vector<Candidate>* out, P
     const uint32_t tile_rows = sh.waves * sh.unroll;
     const uint32_t max_rb = (p.rows + tile_rows - 1) / tile_rows;
     uint32_t last_rb = 0;
-    for (uint32_t want : {128u, 256u}) {
-      // enough workgroups to fill the chip, few enough that the partial sums stay small
+    for (uint32_t want : {0u, 128u, 256u}) {
+      // enough workgroups to fill the chip, few enough that the partial sums stay small; or one on all of few rows of its columns,
+      // whose sums are complete: a launch less, but a compute unit reads no faster for being alone (bf16 rows of 4096: 16 rows 6.9 ->
+      // 3.7 us, 33 6.6 -> 4.6, 64 level, 128 6.6 -> 11.7)
+      if (want == 0 && p.rows > 48) continue;
       const uint32_t n_rb = std::min(max_rb, std::max<uint32_t>(1, want * 6 / n_col_tiles));
       if (n_rb == last_rb) continue;
       last_rb = n_rb;
+      const bool fold = n_rb > 1;
       Candidate c = make_candidate(g, "checkpoint_backward", FS_SCHEME_GLOBAL, K_CHECKPOINT_GRAD_SUMS);
       const uint32_t pitch = colsum_pitch(cols);
       {
@@ -344,17 +348,19 @@ bool build_checkpoint_backward(const fs_graph& g, std::vector<Candidate>* out, P
         l.ptr[1] = in_ref(g, ts);
         l.ptr[2] = in_ref(g, tdy);
         l.ptr[3] = out_ref(g.tensors[t_out].output_slot);
-        l.ptr[4] = ws_ref(0);
+        l.ptr[4] = fold ? ws_ref(0) : out_ref(g.tensors[t_sum].output_slot);
         l.shape.block[0] = sh.waves * 64;
         l.shape.grid[0] = n_rb * n_col_tiles;
       }
-      c.launches.emplace_back();
-      Launch& f = c.launches.back();
-      make_fold_launch(&f, n_rb, pitch, pitch, cols);
-      f.ptr[0] = ws_ref(0);
-      f.ptr[1] = out_ref(g.tensors[t_sum].output_slot);
-      c.info.n_kernels = 2;
-      c.info.workspace_bytes = (int64_t)n_rb * pitch * 4;
+      if (fold) {
+        c.launches.emplace_back();
+        Launch& f = c.launches.back();
+        make_fold_launch(&f, n_rb, pitch, pitch, cols);
+        f.ptr[0] = ws_ref(0);
+        f.ptr[1] = out_ref(g.tensors[t_sum].output_slot);
+        c.info.n_kernels = 2;
+        c.info.workspace_bytes = (int64_t)n_rb * pitch * 4;
+      }
       c.info.rows_per_block = (int32_t)tile_rows;
       c.info.vecs_per_lane = sh.unroll;
       c.info.lanes_per_row = 64;
@@ -362,7 +368,7 @@ bool build_checkpoint_backward(const fs_graph& g, std::vector<Candidate>* out, P
       c.info.bytes_moved_model = c.info.bytes_min + 2 * c.info.workspace_bytes;
       KernelCost kc = base;
       kc.partial_bytes = 2.0 * (double)c.info.workspace_bytes;
-      kc.fold_rows = n_rb;
+      kc.fold_rows = fold ? n_rb : 0;
       kc.flush_values = p.vec;
       kc.flush_steps = 0;
       kc.waves_per_block = sh.waves;
@@ -376,7 +382,7 @@ bool build_checkpoint_backward(const fs_graph& g, std::vector<Candidate>* out, P
       kc.row_bytes = (double)cols * esz;
       kc.dep_phases = 0;
       char var[56];
-      snprintf(var, sizeof var, "<%s,%s,W%d,U%d,RB%u,fold>", dtype_name(p.dt), act_name(act), sh.waves, sh.unroll, n_rb);
+      snprintf(var, sizeof var, "<%s,%s,W%d,U%d,RB%u%s>", dtype_name(p.dt), act_name(act), sh.waves, sh.unroll, n_rb, fold ? ",fold" : "");
       finish_candidate(&c, var, kc);
       out->push_back(c);
     }

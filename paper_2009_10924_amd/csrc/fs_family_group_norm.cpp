@@ -148,6 +148,11 @@ double slab_us(const GroupNormP& p, const Traffic& t, int esz, int K, int vgprs)
   const int per_simd = std::min(8, 512 / std::max(8, (vgprs + 7) / 8 * 8)), held = std::max(1, 4 * per_simd / (p.threads / 64));
   const double rounds = std::min(8.0, std::ceil(groups / (256.0 * held)));
   const double chain = (m.fixed + m.chain_op * ops + m.chain_item * items_per_lane(p, t.backward) + m.chain_threads * p.threads / 512.0) * (1.0 + m.round * (rounds - 1.0));
+  if (p.entries > 1 && p.entry_blocks == 1) {   // a few entries after one another and no other launch (fitted to 420 such candidates, 7 % rms)
+    const double sums_per_lane = p.dim / std::max(1.0, std::min(64.0, std::floor((double)p.threads / p.set_groups)));
+    const double each = 0.61 + 6.0e-3 * ops + 0.094 * items_per_lane(p, true) + 0.71 * p.threads / 512.0 + 0.21 * sums_per_lane;
+    return 2.89 + std::max(each * p.entries, few_units(t.read_bytes + t.written_bytes, groups, 3.3e4));
+  }
   const double more = std::max(0.0, chain - 1.5) * (p.entries - 1.0);   // the next entries' chains, without a launch
   const double issue = waves * (m.issue + m.issue_op * ops);
   const double run = p.sets > 1 ? (double)p.set_groups * p.dim * esz : 1e9;
@@ -461,46 +466,51 @@ bool build_group_norm_backward(const fs_graph& g, std::vector<Candidate>* out, P
       p.fold_log2 = fold_lanes_log2(sh.threads, width, p.rows_at_once);
       p.means_log2 = fold_lanes_log2(sh.threads, gs, p.dim);
       // One batch entry per workgroup; of very many entries so many that the partial sums stay small beside the values (f16
-      // [65536, 1, 512]: 268 MB of them beside 200 MB otherwise).
+      // [65536, 1, 512]: 268 MB of them beside 200 MB otherwise); or, of two to four, all: their sums are complete, a launch less
+      // (bf16 [2, 16, 256] 7.8 -> 6.6 us, [3, 1, 128] 7.7 -> 5.4, [8, 1, 128] no faster).
       const uint32_t most = std::max<uint32_t>(1, 8192 / p.sets);
-      const uint32_t e = p.batch > most && sh.threads <= 256 ? (p.batch + most / 4 - 1) / std::max<uint32_t>(1, most / 4) : 1;
-      p.entries = e;
-      p.entry_blocks = (p.batch + e - 1) / e;
-      const bool fold = p.entry_blocks > 1;
-      const int64_t sum_bytes = aligned(8ll * p.entry_blocks * pitch);
-      const int64_t lds = 4ll * (2ll * p.rows_at_once * item_pitch(p) + 3 * width + 2 * gs + (e > 1 ? 2 * width : 0));
-      if (lds > 64 * 1024 || (uint64_t)p.entry_blocks * p.sets >= (1ull << 31)) continue;
-      Candidate c = make_candidate(g, "group_norm_backward", FS_SCHEME_LDS, K_GN_BWD_SLAB);
-      Launch& l = c.launches.front();
-      l.args.u.gn = p;
-      fill_inputs(l);
-      l.ptr[6] = out_ref(g.tensors[t_dx].output_slot);
-      l.ptr[7] = fold ? ws_ref(0) : out_ref(g.tensors[t_dbeta].output_slot);
-      l.ptr[8] = fold ? ws_ref(4ll * pitch) : out_ref(g.tensors[t_dgamma].output_slot);
-      l.shape.block[0] = (uint32_t)sh.threads;
-      l.shape.grid[0] = p.entry_blocks * p.sets;
-      l.shape.lds_bytes = (uint32_t)lds;
-      const int vgprs = 73 + sh.K * (p.vec * (esz + xsz) / 4 + 1);
-      const KernelCost kc = estimated(slab_us(p, t, esz, sh.K, vgprs), p, vgprs, (int)lds);
-      char var[56];
-      snprintf(var, sizeof var, "<%s,%s,T%d,K%d,G%u,E%u%s>", dtype_name(p.dt), act_name(p.act), sh.threads, sh.K, gs, e, fold ? ",fold" : "");
-      finish_candidate(&c, var, kc);
-      if (fold) {   // dbeta from the first half of each row of sums, dgamma from the second
-        c.launches.emplace_back();
-        Launch& f = c.launches.back();
-        make_fold_launch(&f, p.entry_blocks, 2 * pitch, pitch, p.channels);
-        f.ptr[0] = ws_ref(0);
-        f.ptr[1] = out_ref(g.tensors[t_dbeta].output_slot);
-        f.ptr[2] = out_ref(g.tensors[t_dgamma].output_slot);
-        c.info.n_kernels = 2;
-        c.info.workspace_bytes = sum_bytes;
-        c.info.bytes_moved_model = c.info.bytes_min + 2 * sum_bytes;
+      const uint32_t many = p.batch > most && sh.threads <= 256 ? (p.batch + most / 4 - 1) / std::max<uint32_t>(1, most / 4) : 1;
+      std::vector<uint32_t> entries = {many};
+      if (p.batch > 1 && p.batch <= 4 && sh.threads <= 256) entries.push_back(p.batch);
+      for (uint32_t e : entries) {
+        p.entries = e;
+        p.entry_blocks = (p.batch + e - 1) / e;
+        const bool fold = p.entry_blocks > 1;
+        const int64_t sum_bytes = aligned(8ll * p.entry_blocks * pitch);
+        const int64_t lds = 4ll * (2ll * p.rows_at_once * item_pitch(p) + 3 * width + 2 * gs + (e > 1 ? 2 * width : 0));
+        if (lds > 64 * 1024 || (uint64_t)p.entry_blocks * p.sets >= (1ull << 31)) continue;
+        Candidate c = make_candidate(g, "group_norm_backward", FS_SCHEME_LDS, K_GN_BWD_SLAB);
+        Launch& l = c.launches.front();
+        l.args.u.gn = p;
+        fill_inputs(l);
+        l.ptr[6] = out_ref(g.tensors[t_dx].output_slot);
+        l.ptr[7] = fold ? ws_ref(0) : out_ref(g.tensors[t_dbeta].output_slot);
+        l.ptr[8] = fold ? ws_ref(4ll * pitch) : out_ref(g.tensors[t_dgamma].output_slot);
+        l.shape.block[0] = (uint32_t)sh.threads;
+        l.shape.grid[0] = p.entry_blocks * p.sets;
+        l.shape.lds_bytes = (uint32_t)lds;
+        const int vgprs = 73 + sh.K * (p.vec * (esz + xsz) / 4 + 1);
+        const KernelCost kc = estimated(slab_us(p, t, esz, sh.K, vgprs), p, vgprs, (int)lds);
+        char var[56];
+        snprintf(var, sizeof var, "<%s,%s,T%d,K%d,G%u,E%u%s>", dtype_name(p.dt), act_name(p.act), sh.threads, sh.K, gs, e, fold ? ",fold" : "");
+        finish_candidate(&c, var, kc);
+        if (fold) {   // dbeta from the first half of each row of sums, dgamma from the second
+          c.launches.emplace_back();
+          Launch& f = c.launches.back();
+          make_fold_launch(&f, p.entry_blocks, 2 * pitch, pitch, p.channels);
+          f.ptr[0] = ws_ref(0);
+          f.ptr[1] = out_ref(g.tensors[t_dbeta].output_slot);
+          f.ptr[2] = out_ref(g.tensors[t_dgamma].output_slot);
+          c.info.n_kernels = 2;
+          c.info.workspace_bytes = sum_bytes;
+          c.info.bytes_moved_model = c.info.bytes_min + 2 * sum_bytes;
+        }
+        c.info.lanes_per_row = (int32_t)p.set_vecs;
+        c.info.vecs_per_lane = sh.K;
+        c.info.rows_per_block = (int32_t)p.rows_at_once;
+        c.info.lds_bytes = (int32_t)lds;
+        out->push_back(c);
       }
-      c.info.lanes_per_row = (int32_t)p.set_vecs;
-      c.info.vecs_per_lane = sh.K;
-      c.info.rows_per_block = (int32_t)p.rows_at_once;
-      c.info.lds_bytes = (int32_t)lds;
-      out->push_back(c);
     }
   }
 

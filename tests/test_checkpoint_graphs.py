@@ -77,10 +77,11 @@ def test_store_is_one_launch(act, bias, dtype):
 
 
 @pytest.mark.parametrize("act,dbias", [("none", False), ("gelu", False), ("gelu", True), ("silu", False), ("silu", True)])
-def test_use_is_one_launch_and_a_fold(act, dbias):
-    for shape in ((1, 1, 1), (3, 2, 5), (64, 4, 32), (7, 3, 100), (5, 1, 1537)):
+def test_use_is_one_launch_and_a_fold_of_many_rows(act, dbias):
+    for shape in ((1, 1, 1), (3, 2, 5), (7, 3, 100), (5, 1, 1537), (5000, 4, 32)):
         p = plan(checkpoint_backward_graph(*shape, act=act, dbias=dbias))
-        assert (p.info["pattern"], p.info["n_kernels"]) == ("checkpoint_backward", 2 if dbias else 1), shape
+        folds = dbias and shape[0] > 100
+        assert (p.info["pattern"], p.info["n_kernels"], p.info["workspace_bytes"] > 0) == ("checkpoint_backward", 2 if folds else 1, folds), shape
         assert "at_once" not in p.describe()
 
 

@@ -131,7 +131,7 @@ def test_outputs_that_share_memory_are_refused(spec):
 
 
 def test_explorer_takes_the_block_apart_at_its_products():
-    spec = checkpointed_block_graph(2, 64, 4, 16, 256, 64)
+    spec = checkpointed_block_graph(6, 64, 4, 16, 256, 64)
     prog = B.Program(B.Graph.from_spec(spec))
     text = prog.describe()
     assert prog.info["n_steps"] == prog.info["n_stages"] == 4 and prog.info["n_single_ops"] == 0
@@ -143,6 +143,13 @@ def test_explorer_takes_the_block_apart_at_its_products():
     bad[names.index("b1_dx")] = ins[[t.name for t in spec.inputs].index("b1_dy")]
     with pytest.raises(B.FsError, match="FS_ERR_INVALID_ARG.*shares memory"):   # refused before the first of the four steps
         prog.bind(ins, bad, 0x900000000, prog.info["workspace_bytes"], 0)()
+
+
+def test_few_batch_entries_need_no_fold():
+    """Up to four short ones in one workgroup per set of groups: the sums are complete, nothing is folded, no workspace is needed."""
+    for batch, kernels in ((1, 1), (2, 1), (3, 1), (5, 2)):
+        p = plan(group_norm_backward_graph(batch, 2, 32, 4, "bf16", "silu", "checkpoint"))
+        assert (p.info["n_kernels"], p.info["workspace_bytes"] > 0) == (kernels, kernels > 1), batch
 
 
 def test_no_launch_asks_for_more_threads_than_32_bits_count():
