@@ -150,7 +150,6 @@ bool build_checkpoint(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
     Launch& l = c.launches.front();
     CheckpointP& q = l.args.u.checkpoint;
     q = p;
-    q.lanes_per_row = (int32_t)L;
     q.lanes_log2 = log2_of(L);
     q.vecs_per_lane = K;
     fill_ptrs(l);
@@ -178,7 +177,6 @@ bool build_checkpoint(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
     Launch& l = c.launches.front();
     CheckpointP& q = l.args.u.checkpoint;
     q = p;
-    q.lanes_per_row = (int32_t)T;
     q.vecs_per_lane = K;
     fill_ptrs(l);
     l.shape.block[0] = T;

@@ -49,7 +49,7 @@ enum KernelId : int32_t {
   K_CHECKPOINT_BLOCK,  // a workgroup per block
   K_CHECKPOINT_LONG,   // a workgroup per block, which it reads twice
   K_CHECKPOINT_GRAD,   // p0 q, p1 scales, p2 dy (or null), p3 dx or the values themselves
-  K_CHECKPOINT_GRAD_SUMS,   // p0 q, p1 scales, p2 dy, p3 dx, p4 partials [n_row_blocks, pitch] f32 (folded by K_COLFOLD)
+  K_CHECKPOINT_GRAD_SUMS,   // p0 q, p1 scales, p2 dy, p3 dx, p4 partials [n_row_blocks, pitch] f32 (folded by K_COLFOLD; the sums themselves where n_row_blocks is 1)
   // group normalisation: a workgroup per batch entry and set of groups holds their values (SLAB), or the statistics are
   // gathered chunk by chunk of positions, joined, and the values read again
   K_GN_SLAB,           // p0 x, p1 gamma, p2 beta, p3 y, p4 mean, p5 rstd, p6 q, p7 scales (p4 to p7: or null)
@@ -182,7 +182,7 @@ struct CheckpointP {
   FastDiv div_cols;                 // use: block of an element
   float inv_max, tiny;              // scale = max * inv_max + tiny
   int32_t vec;                      // elements per access: a whole vector, or 1 for blocks shorter than one
-  int32_t lanes_per_row, lanes_log2, vecs_per_lane;
+  int32_t lanes_log2, vecs_per_lane;
   int32_t waves, unroll;            // K_CHECKPOINT_GRAD_SUMS: workgroup = waves x 64 lanes, a row tile = waves * unroll rows
   uint32_t n_row_blocks;
   int32_t stream;
@@ -208,7 +208,6 @@ struct GroupNormP {
   uint32_t entries, entry_blocks;   // K_GN_BWD_SLAB: batch entries of a workgroup, workgroups per set
   uint32_t fold_blocks;             // K_GN_BWD_APPLY: workgroups that add up the chunks' sums
   float eps, inv_count, inv_max, tiny;   // inv_count = 1 / (positions * dim)
-  int32_t stream;
 };
 enum RowPattern : int32_t { ROW_SOFTMAX_BWD = 0, ROW_RMSNORM = 1 };
 struct RowP {
