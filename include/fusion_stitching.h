@@ -277,7 +277,7 @@ int64_t fs_plan_source(const fs_plan *p, char *text, size_t capacity);
  * alone; an infinity makes the scale infinite, itself NaN and the block's other values zero.
  *
  * "group_norm": x [batch, positions, groups, dim] of T, channels last; gamma, beta [groups, dim]
- *   (leading extents of 1 allowed) of T.
+ *   (leading extents of 1 allowed), both of T or both FS_F32.
  *     mu = mean of x, v = mean of (x - mu)^2 over dim and positions (FS_REDUCE_MEAN along axes
  *     3 and 1, in either order), r = FS_RSQRT(v + eps), n = (x - mu) * r,
  *     z = n * gamma + beta, y = act(z)

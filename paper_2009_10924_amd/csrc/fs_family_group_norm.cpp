@@ -20,7 +20,13 @@ bool match_over_group(const fs_graph& g, const char* op, const std::string& inne
 bool per_group(const Tensor& t, const Tensor& x) {
   return t.rank == 4 && t.dims[0] == x.dims[0] && t.dims[1] == 1 && t.dims[2] == x.dims[2] && t.dims[3] == 1 && t.dtype == FS_F32;
 }
-bool per_channel(const Tensor& t, const Tensor& x) { return t.numel() == x.dims[2] * x.dims[3] && is_trailing(t, x) && t.dtype == x.dtype; }
+bool per_channel(const Tensor& t, const Tensor& x) { return t.numel() == x.dims[2] * x.dims[3] && is_trailing(t, x); }
+// gamma and (if there is one) beta: both of x's type, or both float32
+bool params_of(const Tensor& gamma, const Tensor* beta, const Tensor& x, GroupNormP* p) {
+  if (!per_channel(gamma, x) || (beta && (!per_channel(*beta, x) || beta->dtype != gamma.dtype))) return false;
+  p->wide_params = gamma.dtype != x.dtype ? 1 : 0;
+  return gamma.dtype == x.dtype || gamma.dtype == FS_F32;
+}
 
 bool shape_of(const Tensor& x, GroupNormP* p) {
   p->batch = (uint32_t)x.dims[0];
@@ -231,7 +237,7 @@ bool build_group_norm(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
   base.act = act;
   base.checkpoint = has_8bit ? 1 : 0;
   if (x.rank != 4 || !is_float_dtype(x.dtype) || !same_dims(x, g.tensors[t_y]) || g.tensors[t_y].store_as != x.dtype ||
-      !per_channel(g.tensors[tg], x) || !per_channel(g.tensors[tb], x) || !shape_of(x, &base))
+      !params_of(g.tensors[tg], &g.tensors[tb], x, &base) || !shape_of(x, &base))
     return true;
   base.eps = (float)st.scalars[0];
   if (has_8bit) {
@@ -434,7 +440,7 @@ bool build_group_norm_backward(const fs_graph& g, std::vector<Candidate>* out, P
   const Tensor& x = g.tensors[tx];
   if (dy.rank != 4 || !is_float_dtype(dy.dtype) || !same_dims(x, dy) || (!base.checkpoint && x.dtype != dy.dtype) || !same_dims(g.tensors[t_dx], dy) ||
       g.tensors[t_dx].store_as != dy.dtype || g.tensors[t_dbeta].store_as != FS_F32 || g.tensors[t_dgamma].store_as != FS_F32 ||
-      !per_group(g.tensors[tcentre], dy) || !per_group(g.tensors[tr], dy) || !per_channel(g.tensors[tg], dy) || (tb >= 0 && !per_channel(g.tensors[tb], dy)) ||
+      !per_group(g.tensors[tcentre], dy) || !per_group(g.tensors[tr], dy) || !params_of(g.tensors[tg], tb >= 0 ? &g.tensors[tb] : nullptr, dy, &base) ||
       !shape_of(dy, &base))
     return true;
   const int esz = dtype_bytes(base.dt), xsz = base.checkpoint ? 1 : esz;

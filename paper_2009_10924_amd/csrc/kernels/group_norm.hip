@@ -37,8 +37,9 @@ __global__ void __launch_bounds__(NT) k_gn_slab(const T* x, const T* gamma, cons
   typename VecIo<T, VEC>::Raw raw[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) raw[k] = VecIo<T, VEC>::template load<false>(near_element(x + base, min(place + (uint32_t)k * step, last)));
-  const auto raw_gamma = VecIo<T, VEC>::template load<false>(gamma + set * width + l.col);
-  const auto raw_beta = VecIo<T, VEC>::template load<false>(beta + set * width + l.col);
+  GnParams<T, VEC> gains, shifts;
+  gains.load(gamma, set * width + l.col, p.wide_params);
+  shifts.load(beta, set * width + l.col, p.wide_params);
 
   auto valid = [&](int k) { return l.live && place + (uint32_t)k * step <= last; };
   float a[VEC];
@@ -103,8 +104,8 @@ __global__ void __launch_bounds__(NT) k_gn_slab(const T* x, const T* gamma, cons
   float rstd[G], ga[VEC], be[VEC];
 #pragma unroll
   for (int i = 0; i < G; ++i) rstd[i] = stat[p.set_groups + group[i]];
-  VecIo<T, VEC>::widen(raw_gamma, ga);
-  VecIo<T, VEC>::widen(raw_beta, be);
+  gains.widen(p.wide_params, ga);
+  shifts.widen(p.wide_params, be);
 #pragma unroll
   for (int e = 0; e < VEC; ++e) ga[e] *= rstd[WHOLE ? 0 : e];
 #pragma unroll
@@ -369,9 +370,9 @@ __global__ void __launch_bounds__(256) k_gn_apply(const T* x, const T* gamma, co
   typename VecIo<T, VEC>::Raw next[U], now[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) next[u] = load(row + u * step);
-  float ga[VEC], be[VEC];
-  VecIo<T, VEC>::widen(VecIo<T, VEC>::template load<false>(gamma + set * width + l.col), ga);
-  VecIo<T, VEC>::widen(VecIo<T, VEC>::template load<false>(beta + set * width + l.col), be);
+  GnParams<T, VEC> gains, shifts;
+  gains.load(gamma, set * width + l.col, p.wide_params);
+  shifts.load(beta, set * width + l.col, p.wide_params);
   if constexpr (JOIN) {
     const uint32_t lanes = 1u << p.fold_log2, sets = 256u >> p.fold_log2, lane = threadIdx.x & (lanes - 1u);
     for (uint32_t g0 = 0; g0 < p.set_groups; g0 += sets) {
@@ -399,6 +400,9 @@ __global__ void __launch_bounds__(256) k_gn_apply(const T* x, const T* gamma, co
     rstd[i] = j.y;
     if constexpr (STORE8) to8[i] = j.y * Divisor(j.z).inv;
   }
+  float ga[VEC], be[VEC];
+  gains.widen(p.wide_params, ga);
+  shifts.widen(p.wide_params, be);
 #pragma unroll
   for (int e = 0; e < VEC; ++e) ga[e] *= rstd[WHOLE ? 0 : e];
   auto put = [&](typename VecIo<T, VEC>::Raw raw, uint32_t at) {

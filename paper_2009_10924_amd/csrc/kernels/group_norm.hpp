@@ -7,6 +7,8 @@
 // neighbouring threads read neighbouring memory.  The last vector of a set starts early where the width is no multiple of VEC;
 // the channels it then shares with its neighbour have the same values in both and are deposited twice in the same place.
 #pragma once
+#include <type_traits>
+
 #include "activation.hpp"
 #include "kernel_arguments.hpp"
 #include "vec_access.hpp"
@@ -27,6 +29,42 @@ __device__ __forceinline__ GnLane gn_lane(const GnShape& p) {
   l.live = l.row < p.rows_at_once;
   return l;
 }
+
+// gamma or beta of a thread's channels, from channel `at` on: stored like x, or (wide) in float32 beside a 16-bit x.  Loaded without a
+// branch, whose end would wait for these loads and all before them (2 to 3 % of calls with two launches), so the second half of
+// wide ones is always loaded, of the others the first again.
+template <typename T, int VEC>
+struct GnParams {
+  static constexpr bool kHalves = sizeof(T) < 4;
+  typedef typename std::conditional<VEC == 1 && kHalves, uint16_t, typename VecIo<T, VEC>::Raw>::type Raw;
+  Raw lo, hi;
+  __device__ __forceinline__ static Raw one(const T* p) {
+    if constexpr (VEC == 1 && kHalves) return *reinterpret_cast<const uint16_t*>(p);
+    else return VecIo<T, VEC>::template load<false>(p);
+  }
+  __device__ __forceinline__ void load(const T* from, uint32_t at, bool wide) {
+    const T* const p = from + at + (kHalves && wide ? at : 0u);
+    lo = one(p);
+    if constexpr (kHalves) hi = one(wide ? p + VEC : p);
+  }
+  __device__ __forceinline__ void widen(bool wide, float (&v)[VEC]) const {
+    if constexpr (VEC == 1 && kHalves) {
+      const T own = __builtin_bit_cast(T, lo);
+      v[0] = wide ? __builtin_bit_cast(float, (uint32_t)lo | (uint32_t)hi << 16) : load1(&own);
+    } else {
+      VecIo<T, VEC>::widen(lo, v);
+      if constexpr (kHalves) {
+        if (wide) {
+          const f32x4 a = __builtin_bit_cast(f32x4, lo), b = __builtin_bit_cast(f32x4, hi);
+          const float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) v[e] = w[e];
+          done(v);   // (a branch, not a choice per value)
+        }
+      }
+    }
+  }
+};
 
 // Workgroups go to the dies in turn; neighbouring sets, which share lines of memory, belong on one die and behind its cache.
 __device__ __forceinline__ uint32_t gn_block(uint32_t blocks) {

@@ -31,8 +31,13 @@ struct GnChannels {
   __device__ __forceinline__ void load(const GnShape& p, const GnLane& l, uint32_t n, uint32_t set, const float* centre, const float* rstd,
                                        const T* gamma, const T* beta) {
     const uint32_t c = set * p.set_groups * p.dim + l.col, g0 = n * p.groups;
-    VecIo<T, VEC>::widen(VecIo<T, VEC>::template load<false>(gamma + c), ga);
-    if (beta) VecIo<T, VEC>::widen(VecIo<T, VEC>::template load<false>(beta + c), be);
+    GnParams<T, VEC> params;
+    params.load(gamma, c, p.wide_params);
+    params.widen(p.wide_params, ga);
+    if (beta) {
+      params.load(beta, c, p.wide_params);
+      params.widen(p.wide_params, be);
+    }
     // one group: one pair of values (as many loads as channels otherwise, which in the small shapes is what a thread mostly does)
     const uint32_t first = g0 + fast_div(c, p.div_dim);
     const float t0 = centre[first], r0 = FROM8 ? t0 : rstd[first];

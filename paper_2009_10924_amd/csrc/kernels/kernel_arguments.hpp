@@ -120,12 +120,12 @@ FS_SHARED void units_second_axis(TransposeP* p, uint32_t word, uint32_t d2, uint
 struct GnShape {
   uint32_t batch, positions, groups, dim, channels, set_groups, sets, set_vecs, rows_at_once, set_vecs_m;
   FastDiv div_dim, div_per, div_sets, div_chunks;
-  uint32_t chunk_rows, chunks, fold_log2, means_log2, fold_blocks, whole, whole_lines, entries, entry_blocks, sum_pitch;   // sum_pitch: floats between the sums of neighbouring rows
+  uint32_t chunk_rows, chunks, fold_log2, means_log2, fold_blocks, whole, whole_lines, entries, entry_blocks, sum_pitch, wide_params;   // sum_pitch: floats between the sums of neighbouring rows
   float eps, inv_count, inv_max, tiny;
 };
 inline GnShape gn_shape(const GroupNormP& p) {
   return GnShape{p.batch, p.positions, p.groups, p.dim, p.channels, p.set_groups, p.sets, p.set_vecs, p.rows_at_once, p.set_vecs_m,
-                 p.div_dim, p.div_per, p.div_sets, p.div_chunks, p.chunk_rows, p.chunks, (uint32_t)p.fold_log2, (uint32_t)p.means_log2, p.fold_blocks, p.whole ? 1u : 0u, p.whole_lines ? 1u : 0u, p.entries, p.entry_blocks, colsum_pitch(p.channels),
+                 p.div_dim, p.div_per, p.div_sets, p.div_chunks, p.chunk_rows, p.chunks, (uint32_t)p.fold_log2, (uint32_t)p.means_log2, p.fold_blocks, p.whole ? 1u : 0u, p.whole_lines ? 1u : 0u, p.entries, p.entry_blocks, colsum_pitch(p.channels), p.wide_params ? 1u : 0u,
                  p.eps, p.inv_count, p.inv_max, p.tiny};
 }
 

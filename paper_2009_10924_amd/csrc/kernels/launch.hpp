@@ -189,7 +189,8 @@ struct CheckpointP {
 };
 constexpr uint32_t kGnMostRows = 128;   // positions of a chunk that one thread may have (see k_gn_stats)
 struct GroupNormP {
-  int32_t dt, act;                  // x / y / dy / dx / gamma / beta share dt; statistics and sums are float32
+  int32_t dt, act;                  // x / y / dy / dx share dt; statistics and sums are float32
+  int32_t wide_params;              // 0: gamma and beta are of dt too, 1: float32 beside a 16-bit dt
   int32_t checkpoint;               // forward: q and its scales are written; backward: they are read instead of x and the mean
   uint32_t batch, positions, groups, dim, channels;   // channels = groups * dim
   uint32_t set_groups, sets;        // groups that a workgroup works on, sets of them

@@ -99,3 +99,17 @@ def test_backward(shape, dtype):
         inp = make_inputs(spec, seed=k)
         env = O.evaluate(spec, inp, keep_all=True)
         every_candidate(spec, inp, backward_bounds(env, dtype), env)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 33, 32, 10), (3, 197, 5, 7), (1, 64, 32, 8), (1, 9000, 3, 5), (4, 7, 16, 1), (2, 2048, 4, 16), (1, 60000, 32, 8)], ids=NAME)
+def test_float32_parameters(shape, dtype):
+    for keep in ("checkpoint", "stats"):
+        spec = group_norm_graph(*shape, dtype=dtype, act="silu", keep=keep, param_dtype="f32")
+        inp = make_inputs(spec, seed=5)
+        env = O.evaluate(spec, inp, keep_all=True)
+        every_candidate(spec, inp, forward_bounds(spec, env, "silu", dtype), env)
+        spec = group_norm_backward_graph(*shape, dtype=dtype, act=("silu", "none")[keep == "stats"], keep=keep, param_dtype="f32")
+        inp = make_inputs(spec, seed=5)
+        env = O.evaluate(spec, inp, keep_all=True)
+        every_candidate(spec, inp, backward_bounds(env, dtype), env)

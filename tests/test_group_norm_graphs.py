@@ -171,3 +171,14 @@ def test_checkpoint_factors_stay_finite():
         assert plan(spec).info["pattern"] == pattern, (eps, tiny)
         spec = group_norm_graph(2, 9, 4, 8, "f32", "silu", "stats", eps=eps)
         assert plan(spec).info["pattern"] == "group_norm"
+
+
+def test_parameters_may_be_float32_beside_16_bit_values():
+    for dtype in ("f16", "bf16"):
+        assert plan(group_norm_graph(2, 9, 4, 8, dtype, "silu", "checkpoint", param_dtype="f32")).info["pattern"] == "group_norm"
+        for act in ("none", "gelu"):
+            assert plan(group_norm_backward_graph(2, 9, 4, 8, dtype, act, "stats", param_dtype="f32")).info["pattern"] == "group_norm_backward"
+    assert plan(group_norm_graph(2, 9, 4, 8, "f32", "silu", "stats", param_dtype="bf16")).info["pattern"] == "unfused"
+    spec = group_norm_graph(2, 9, 4, 8, "bf16", "silu", "stats")
+    mixed = GraphSpec(spec.name, [TensorSpec(t.name, "f32" if t.name == "beta" else t.dtype, t.dims) for t in spec.inputs], spec.ops, spec.outputs)
+    assert plan(mixed).info["pattern"] == "unfused"

@@ -304,11 +304,11 @@ def _store_8bit_ops(src: str, axes: Sequence[int]) -> List[OpSpec]:
 
 
 def group_norm_graph(batch: int, positions: int, groups: int, dim: int, dtype: str = "bf16", act: str = "silu", keep: str = "none",
-                     eps: float = 1e-5) -> GraphSpec:
+                     eps: float = 1e-5, param_dtype: str = "") -> GraphSpec:
     """Group normalisation of [batch, positions, groups, dim] (channels last: channel = group * dim + d) and an activation:
-    mean and population variance over a group's positions and channels, gain and shift per channel.  keep: "stats" hands out
-    mean and reciprocal deviation, "checkpoint" the normalised values in 8 bits with a scale per batch entry and group, and
-    the reciprocal deviation."""
+    mean and population variance over a group's positions and channels, gain and shift per channel (stored in param_dtype, or
+    like x).  keep: "stats" hands out mean and reciprocal deviation, "checkpoint" the normalised values in 8 bits with a scale
+    per batch entry and group, and the reciprocal deviation."""
     ops = [
         _op("mu_d", "reduce_mean", "x", axis=3), _op("mu", "reduce_mean", "mu_d", axis=1),
         _op("c", "sub", "x", "mu"), _op("c2", "square", "c"),
@@ -326,14 +326,15 @@ def group_norm_graph(batch: int, positions: int, groups: int, dim: int, dtype: s
         outputs += [("q", "e4m3"), ("s", "f32"), ("r", "f32")]
     elif keep == "stats":
         outputs += [("mu", "f32"), ("r", "f32")]
+    params = param_dtype or dtype
     return GraphSpec(name=f"group_norm_{dtype}_{act}_{keep}_{batch}x{positions}x{groups}x{dim}",
-                     inputs=[TensorSpec("x", dtype, (batch, positions, groups, dim)), TensorSpec("gamma", dtype, (groups, dim)),
-                             TensorSpec("beta", dtype, (groups, dim))],
+                     inputs=[TensorSpec("x", dtype, (batch, positions, groups, dim)), TensorSpec("gamma", params, (groups, dim)),
+                             TensorSpec("beta", params, (groups, dim))],
                      ops=ops, outputs=outputs)
 
 
 def group_norm_backward_graph(batch: int, positions: int, groups: int, dim: int, dtype: str = "bf16", act: str = "silu",
-                              keep: str = "stats") -> GraphSpec:
+                              keep: str = "stats", param_dtype: str = "") -> GraphSpec:
     """Its backward pass, from the input and the statistics (keep = "stats") or from the 8-bit checkpoint: dx, and the sums
     dgamma and dbeta over batch and positions."""
     full, per_group, chan = (batch, positions, groups, dim), (batch, 1, groups, 1), (groups, dim)
@@ -343,10 +344,10 @@ def group_norm_backward_graph(batch: int, positions: int, groups: int, dim: int,
     else:
         inputs = [TensorSpec("x", dtype, full), TensorSpec("mu", "f32", per_group)]
         ops = [_op("c", "sub", "x", "mu"), _op("n", "mul", "c", "r")]
-    inputs += [TensorSpec("dy", dtype, full), TensorSpec("r", "f32", per_group), TensorSpec("gamma", dtype, chan)]
+    inputs += [TensorSpec("dy", dtype, full), TensorSpec("r", "f32", per_group), TensorSpec("gamma", param_dtype or dtype, chan)]
     dz = "dy"
     if act != "none":
-        inputs.append(TensorSpec("beta", dtype, chan))
+        inputs.append(TensorSpec("beta", param_dtype or dtype, chan))
         ops += [_op("ng", "mul", "n", "gamma"), _op("z", "add", "ng", "beta"), *_act_grad_ops(act, "z", "da"), _op("dz", "mul", "dy", "da")]
         dz = "dz"
     ops += [
