@@ -5,7 +5,7 @@
 // sum of squared deviations per chunk of positions, and a last one, which joins the chunks of its groups, reads x again; where
 // that joins too many for every workgroup, a launch in between does it once.  Bound by memory from some 30 MB on: bf16
 // [16, 16384, 256] with SiLU, 64 us for its 268 MB (24 us gather, 40 read and write again: 5.6 and 6.7 TB/s); smaller ones by what a
-// workgroup does one after the other: bf16 [8, 4096, 320] with a checkpoint 19.5 us, 8.5 for its bytes alone.  No variance is a
+// workgroup does one after the other: bf16 [8, 4096, 320] with a checkpoint 19.4 us, 8.5 for its bytes alone.  No variance is a
 // difference of large sums: inside registers it is the mean of squared deviations from the known mean, and partial results
 // join as M2 = M2a + M2b + (mean_b - mean_a)^2 na nb / (na + nb).
 #include <hip/hip_runtime.h>

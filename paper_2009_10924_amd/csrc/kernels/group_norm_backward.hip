@@ -5,9 +5,9 @@
 //     m1 = sum_d gamma A / n,   m2 = sum_d gamma B / n,   dx = (gamma dz - m1 - xh m2) rstd.
 // A workgroup that holds a set's values (k_gn_bwd_slab) reads them once, and K_COLFOLD adds up the batch; otherwise a first launch
 // gathers A and B per chunk of positions and a second one, which adds up the chunks, reads the values again.
-// Large calls are bound by memory and, with the GELU's slope, by arithmetic: f16 [8, 16384, 512] from x, 117 us for 403 MB (54 us
+// Large calls are bound by memory and, with the GELU's slope, by arithmetic: f16 [8, 16384, 512] from x, 118 us for 403 MB (54 us
 // gather at 5.0 TB/s, the vector units two thirds busy; 66 read and write at 6.2).  Smaller ones by what a workgroup does one after
-// the other: bf16 [8, 4096, 320] from a checkpoint 23.1 us (12.0 + 12.4 as kernels), 8.5 for its bytes alone.
+// the other: bf16 [8, 4096, 320] from a checkpoint 23.4 us (11.9 + 12.3 as kernels), 8.5 for its bytes alone.
 #include <hip/hip_runtime.h>
 
 #include "fold.hpp"
