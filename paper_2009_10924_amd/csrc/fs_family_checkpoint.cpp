@@ -275,8 +275,10 @@ bool build_checkpoint_backward(const fs_graph& g, std::vector<Candidate>* out, P
   p.blocks = 1;
   p.stream = streams_inputs(g) ? 1 : 0;
   p.vec = access_of(p.dt, p.cols);
-  // one scale per block of the last axis
-  if (!is_float_dtype(p.dt) || s.dtype != FS_F32 || s.rank != q.rank || s.dims[s.rank - 1] != 1 || s.numel() != (int64_t)p.rows) return true;
+  // one scale per block of the last axis: q's extents but for the last (others of as many values would stretch q with them)
+  Tensor scales = q;
+  scales.dims[q.rank - 1] = 1;
+  if (!is_float_dtype(p.dt) || s.dtype != FS_F32 || !same_dims(s, scales)) return true;
   if (tdy >= 0 && (!same_dims(g.tensors[tdy], q) || g.tensors[tdy].dtype != p.dt)) return true;
   const int esz = dtype_bytes(p.dt);
   const double n = (double)p.rows * p.cols;
