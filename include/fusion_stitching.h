@@ -296,9 +296,13 @@ int64_t fs_plan_source(const fs_plan *p, char *text, size_t capacity);
  *   the leading axes (FS_REDUCE_SUM along axis 0, or axes 0 to k), FS_F32.
  *
  * Means, variances, scales and sums are float32; a variance is that of differences from values
- * near the mean, never a difference of two sums.  Outputs of these plans may share no memory
- * with an input or with another output: fs_execute, fs_execute_static and
- * fs_program_execute return FS_ERR_INVALID_ARG for such a call before anything is launched.
+ * near the mean, never a difference of two sums.  The kernels' outputs may share no memory
+ * with an input or with another output.  Where one does (group normalisation in place, say) and
+ * no tensor of the graph is FS_E4M3, fs_execute runs the ops one by one, in their order, if its
+ * workspace holds what the FS_SCHEME_UNFUSED plan's fs_plan_info.workspace_bytes says;
+ * fs_program_execute does so for a step, in what its workspace has behind
+ * fs_program_info.workspace_bytes rounded up to 256 (not for steps with a joint fold).  Any other
+ * such call, fs_execute_static's too, returns FS_ERR_INVALID_ARG before anything is launched.
  * Normalising more positions than a workgroup keeps in registers, and the sums over more than a
  * few rows or batch entries, take two or three launches and a workspace.                                   */
 
@@ -319,7 +323,7 @@ int64_t fs_plan_source(const fs_plan *p, char *text, size_t capacity);
  * in different orders, so their last bits may differ; and where rows of an odd number of
  * 16-bit elements lie on the tensor's 16-byte grid, which lane adds which elements depends
  * on the row's index, so that equal rows of a tensor may round differently.
- * Group normalisation and 8-bit checkpoints refuse outputs that share memory (above).
+ * Group normalisation and 8-bit checkpoints have rules of their own for outputs that share memory (above).
  * Two calls that share a workspace must be ordered on one stream.
  * Errors: FS_ERR_INVALID_ARG, FS_ERR_WORKSPACE, FS_ERR_ALIGN, FS_ERR_HIP.         */
 fs_status fs_execute(const fs_plan *p, const void *const *inputs, void *const *outputs,

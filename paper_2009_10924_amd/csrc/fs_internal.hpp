@@ -105,7 +105,7 @@ struct Candidate {
   fs_plan_info info;
   std::vector<Launch> launches;
   KernelCost cost;               // description of the (single) stitched kernel; unused for unfused plans
-  bool apart = false;            // no output may share memory with an input or another output: refused when it is run
+  bool apart = false;            // no output may share memory with an input or another output: a call where one does is not its
   bool fallback = false;         // offered only for the case that no other candidate can be used (the interpreted row
                                  // program beside the kernels generated for the same pattern): passed over by the choice
                                  // while another candidate stands, still reachable by index
@@ -159,6 +159,8 @@ struct fs_plan {
   std::vector<int64_t> input_bytes, output_bytes;
   fs::PackForm pack;
   std::unique_ptr<fs::SumsBesideRows> at_once;   // what fs_execute runs instead of the chosen candidate where it may; null: nothing
+  std::unique_ptr<fs::Candidate> op_by_op;       // the per-op launches, for calls whose outputs share memory where the chosen candidate needs
+                                                 // them apart; null: such calls are refused
   int64_t bytes_min = 0;
   fs_plan_opts opts = {-1, 0, 0, 0};   // what the caller asked for (a re-choice after a failed compile honours it)
 };
@@ -230,13 +232,14 @@ bool codegen_enabled();
 // kernels that it will compile first, for gen_compile_together().
 void compiled_ahead(const fs_plan& p, std::vector<GenSource>* out);
 fs_status create_plan(const fs_graph* g, int32_t scheme, const fs_plan_opts* opts, bool complete, fs_plan** out);
-// The first `n_launches` launches of the plan's chosen candidate, all of them as one launch where the plan has that form and may take
+// The first `n_launches` launches of the candidate `c` of the plan, all of them as one launch where the plan has that form and may take
 // it (arguments already validated by the caller).
-fs_status run_launches(const fs_plan* p, const void* const* inputs, void* const* outputs, void* workspace, void* hip_stream,
+fs_status run_launches(const fs_plan* p, const Candidate& c, const void* const* inputs, void* const* outputs, void* workspace, void* hip_stream,
                        size_t n_launches);
+// What a call runs: the chosen candidate, or, if that needs outputs of their own memory and these are not, the per-op launches
+// where `workspace_bytes` hold their intermediates; null (and FS_ERR_INVALID_ARG's text set) if neither can.
+const Candidate* candidate_for(const fs_plan* p, const void* const* inputs, void* const* outputs, size_t workspace_bytes);
 // Whether an output shares memory with an input or with another output.
-// FS_ERR_INVALID_ARG if the chosen kernels need outputs of their own memory and these are not
-fs_status check_apart(const fs_plan* p, const void* const* inputs, void* const* outputs);
 bool outputs_share_memory(const std::vector<int64_t>& input_bytes, const std::vector<int64_t>& output_bytes, const void* const* inputs, void* const* outputs);
 // The checks every execute entry point makes on its pointer arrays (null, alignment); `who` names the caller in the message.
 fs_status check_execute_args(const fs_plan* p, const void* const* inputs, void* const* outputs, const char* who);

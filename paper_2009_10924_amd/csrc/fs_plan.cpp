@@ -227,15 +227,19 @@ static fs_status run_at_once(const SumsBesideRows& once, const void* const* inpu
   return err == 0 ? FS_OK : fail(FS_ERR_HIP, "fs_execute: launching rows and column sums failed: %s", hip_error_text(err));
 }
 
-fs_status fs::check_apart(const fs_plan* p, const void* const* inputs, void* const* outputs) {
+const Candidate* fs::candidate_for(const fs_plan* p, const void* const* inputs, void* const* outputs, size_t workspace_bytes) {
   const Candidate& c = p->candidates[p->chosen];
-  if (!c.apart || !outputs_share_memory(p->input_bytes, p->output_bytes, inputs, outputs)) return FS_OK;
-  return fail(FS_ERR_INVALID_ARG, "an output shares memory with an input or another output, which the kernels of pattern '%s' do not allow", c.info.pattern);
+  if (!c.apart || !outputs_share_memory(p->input_bytes, p->output_bytes, inputs, outputs)) return &c;
+  if (p->op_by_op && workspace_bytes >= (size_t)p->op_by_op->info.workspace_bytes) return p->op_by_op.get();
+  std::string way_out;
+  if (p->op_by_op) way_out = "; op by op, such a call takes " + std::to_string((long long)p->op_by_op->info.workspace_bytes) + " bytes of workspace";
+  fail(FS_ERR_INVALID_ARG, "an output shares memory with an input or another output, which the kernels of pattern '%s' do not allow%s", c.info.pattern,
+       way_out.c_str());
+  return nullptr;
 }
 
-fs_status fs::run_launches(const fs_plan* p, const void* const* inputs, void* const* outputs, void* workspace, void* hip_stream,
+fs_status fs::run_launches(const fs_plan* p, const Candidate& c, const void* const* inputs, void* const* outputs, void* workspace, void* hip_stream,
                        size_t n_launches) {
-  const Candidate& c = p->candidates[p->chosen];
   const size_t end = std::min(n_launches, c.launches.size());
   // (a call under capture cannot load the kernel; the two launches of a compiled-in family need nothing loaded)
   if (p->at_once && end == c.launches.size() && !outputs_share_memory(p->input_bytes, p->output_bytes, inputs, outputs) &&
@@ -404,6 +408,11 @@ fs_status fs::create_plan(const fs_graph* g, int32_t scheme, const fs_plan_opts*
   p->n_outputs = (int32_t)g->outputs.size();
   for (int t : g->inputs) p->input_bytes.push_back(g->tensors[t].numel() * dtype_bytes(g->tensors[t].dtype));
   for (int t : g->outputs) p->output_bytes.push_back(g->tensors[t].numel() * dtype_bytes(g->tensors[t].store_as));
+  // (8-bit tensors came with the families that need their outputs apart; what runs in float32 and 16 bits never had to be)
+  if (p->candidates[best].apart && !holds_8bit(*g)) {
+    Candidate u;
+    if (build_unfused(*g, &u) == FS_OK) p->op_by_op = std::make_unique<Candidate>(std::move(u));
+  }
   if (scheme != FS_SCHEME_UNFUSED && codegen_enabled()) fill_generic_forms(*g, p);
   if (complete) {
     SumsBesideRows once;
@@ -601,9 +610,9 @@ fs_status fs_execute(const fs_plan* p, const void* const* inputs, void* const* o
       return fail(FS_ERR_WORKSPACE, "fs_execute: workspace of %lld bytes needed, %zu given", (long long)c.info.workspace_bytes, workspace_bytes);
     if ((uintptr_t)workspace & 15u) return fail(FS_ERR_ALIGN, "fs_execute: workspace is not 16-byte aligned");
   }
-  const fs_status apart = check_apart(p, inputs, outputs);
-  if (apart != FS_OK) return apart;
-  return run_launches(p, inputs, outputs, workspace, hip_stream, c.launches.size());
+  const Candidate* const run = candidate_for(p, inputs, outputs, workspace && ((uintptr_t)workspace & 15u) == 0 ? workspace_bytes : 0);
+  if (!run) return FS_ERR_INVALID_ARG;
+  return run_launches(p, *run, inputs, outputs, workspace, hip_stream, run->launches.size());
 } catch (...) {
   return fs::fail_caught("fs_execute");
 }

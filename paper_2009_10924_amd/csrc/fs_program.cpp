@@ -154,6 +154,13 @@ static fs_status run_program(const fs_program* p, int32_t first_stage, int32_t l
   }
   std::vector<const void*> in;
   std::vector<void*> out;
+  // workspace behind the program's own, for steps that run op by op (one after the other; a step whose last launches have moved to
+  // the program's end has to run them as planned)
+  const size_t own = ((size_t)p->info.workspace_bytes + 255u) & ~(size_t)255u;
+  const size_t spare = ws && ((uintptr_t)ws & 15u) == 0 && workspace_bytes > own ? workspace_bytes - own : 0;
+  auto candidate_of = [&](const fs_program::Step& s) {
+    return candidate_for(s.plan, in.data(), out.data(), s.own_launches == s.plan->candidates[s.plan->chosen].launches.size() ? spare : 0);
+  };
   // what a step would refuse is refused before the first one is launched
   for (const fs_program::Step& s : p->steps) {
     if (s.stage < first_stage || s.stage > last_stage || !s.plan->candidates[s.plan->chosen].apart) continue;
@@ -161,8 +168,7 @@ static fs_status run_program(const fs_program* p, int32_t first_stage, int32_t l
     out.clear();
     for (const BufRef& r : s.in) in.push_back(address(r));
     for (const BufRef& r : s.out) out.push_back(address(r));
-    const fs_status st = check_apart(s.plan, in.data(), out.data());
-    if (st != FS_OK) return st;
+    if (!candidate_of(s)) return FS_ERR_INVALID_ARG;
   }
   std::vector<char> pack_done(p->packs.size(), 0);
   for (size_t si = 0; si < p->steps.size(); ++si) {
@@ -199,8 +205,10 @@ static fs_status run_program(const fs_program* p, int32_t first_stage, int32_t l
     out.clear();
     for (const BufRef& r : s.in) in.push_back(address(r));
     for (const BufRef& r : s.out) out.push_back(address(r));
-    const int64_t need = s.plan->candidates[s.plan->chosen].info.workspace_bytes;
-    const fs_status st = run_launches(s.plan, in.data(), out.data(), need > 0 ? ws + s.plan_ws_offset : nullptr, hip_stream, s.own_launches);
+    const Candidate& planned = s.plan->candidates[s.plan->chosen];
+    const Candidate& c = planned.apart ? *candidate_of(s) : planned;
+    const fs_status st = &c == &planned ? run_launches(s.plan, c, in.data(), out.data(), c.info.workspace_bytes > 0 ? ws + s.plan_ws_offset : nullptr, hip_stream, s.own_launches)
+                                        : run_launches(s.plan, c, in.data(), out.data(), ws + own, hip_stream, c.launches.size());
     if (st != FS_OK) return st;
   }
   if (last_stage < p->info.n_stages - 1 || p->carrier.step >= 0) return FS_OK;
