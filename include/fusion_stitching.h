@@ -283,6 +283,8 @@ int64_t fs_plan_source(const fs_plan *p, char *text, size_t capacity);
  *     z = n * gamma + beta, y = act(z)
  *   Outputs: y (T); if wanted mu, r (FS_F32, [batch, 1, groups, 1]); if wanted a checkpoint of n
  *   with one block per batch entry and group (eps > 0, and 1 / (sqrt(eps) * tiny) below 1e38).
+ *   A NaN or an infinity in x makes all of its group NaN, r and what is kept of n included, and
+ *   the scale NaN or infinite.
  * "group_norm_backward": dy like x; n = (x - mu) * r from inputs x, mu and r, or n = q * s from a
  *   checkpoint, its scale and r; gamma, and with an activation beta.
  *     dz = dy * act'(n * gamma + beta), g = dz * gamma,
