@@ -196,7 +196,8 @@ struct GroupNormP {
   uint32_t set_groups, sets;        // groups that a workgroup works on, sets of them
   int32_t vec;                      // elements per access: a whole vector, or 1 where a set has fewer channels
   int32_t whole;                    // 1: a vector lies within one group
-  int32_t whole_lines;              // 1: a workgroup's pieces of a position are whole 64-byte pieces of memory, stored past the caches
+  int32_t whole_lines;              // K_GN_SLAB, K_GN_BWD_SLAB: 1: a workgroup's pieces of a position of x are whole 64-byte pieces of memory,
+                                    // and what it stores goes past the caches (the chunked kernels' stores always do)
   uint32_t set_vecs, rows_at_once;  // vectors of a position in a set; positions that a workgroup's threads cover
   uint32_t set_vecs_m;              // ceil(2^20 / set_vecs)
   FastDiv div_dim, div_per;         // by dim; by the items a position leaves in LDS for one group
