@@ -215,6 +215,10 @@ bool build_checkpoint(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
     kc.lds_bytes_per_block = 64;
     estimate(&kc, 1024.0, 4, true);
     kc.own_estimate_s += 0.5 * n * esz / 6.4e12;   // the second read finds a part of the row in the caches
+    // A compute unit by itself takes a block at 4500 to 10800 values a us, 2-byte and 4-byte ones alike (bf16 [1, 2^26] 7677 us, with bias and
+    // GELU [1, 2^22] 950, f32 [1, 2^22] 511, with GELU [16, 2^18] 43): what fewer blocks than compute units take.
+    const double per_value = 1.05e-4 + 0.45e-4 * (act == ACT_GELU ? 1.5 : act == ACT_SILU ? 1.0 : 0.0) + (tb >= 0 ? 0.5e-4 : 0.0);
+    kc.own_estimate_s = std::max(kc.own_estimate_s, (2.0 + per_value * p.cols) * 1e-6);
     char var[48];
     snprintf(var, sizeof var, "<%s,%s>", dtype_name(p.dt), act_name(act));
     finish_candidate(&c, var, kc);
