@@ -8,9 +8,11 @@ namespace fsk {
 
 // STREAM: with the streaming hint; without it where neighbouring workgroups write the rest of a line (the cache then puts it
 // together, with the hint every piece goes to memory by itself).
-template <bool STREAM, typename V, typename P> __device__ __forceinline__ void put(V v, P* p) {
-  if constexpr (STREAM) __builtin_nontemporal_store(v, p);
-  else *p = v;
+// ALIGN: the bytes that p's address is a multiple of (an alignment in the type of a deduced pointer would be lost).
+template <bool STREAM, int ALIGN, typename V> __device__ __forceinline__ void put(V v, void* p) {
+  typename AtAlignment<V, ALIGN>::type* const q = reinterpret_cast<typename AtAlignment<V, ALIGN>::type*>(p);
+  if constexpr (STREAM) __builtin_nontemporal_store(v, q);
+  else *q = v;
 }
 
 template <typename IO, typename T, int VEC> __device__ __forceinline__ void store_as(bool stream, T* p, const float (&v)[VEC]) {
@@ -32,7 +34,7 @@ template <typename T, int VEC> struct VecIo {
     if constexpr (sizeof(T) == 4) w = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
     else w = u32x4{pack2(v[0], v[1], (const T*)nullptr), pack2(v[2], v[3], (const T*)nullptr), pack2(v[4], v[5], (const T*)nullptr),
                    pack2(v[6], v[7], (const T*)nullptr)};
-    put<STREAM>(w, reinterpret_cast<Place*>(p));
+    put<STREAM, sizeof(T)>(w, p);
   }
 };
 template <typename T> struct VecIo<T, 1> {
@@ -56,7 +58,7 @@ template <> struct VecIo<e4m3_t, 8> {
   }
   template <bool STREAM = true> __device__ __forceinline__ static void store(e4m3_t* p, const float (&v)[8]) {
     const u32x2 w = {pack_e4m3_in_range(v[0], v[1], v[2], v[3]), pack_e4m3_in_range(v[4], v[5], v[6], v[7])};
-    put<STREAM>(w, reinterpret_cast<Place*>(p));
+    put<STREAM, 1>(w, p);
   }
 };
 template <> struct VecIo<e4m3_t, 4> {
@@ -68,7 +70,7 @@ template <> struct VecIo<e4m3_t, 4> {
   }
   __device__ __forceinline__ static void widen(Raw r, float (&v)[4]) { unpack_e4m3(r, v[0], v[1], v[2], v[3]); }
   template <bool STREAM = true> __device__ __forceinline__ static void store(e4m3_t* p, const float (&v)[4]) {
-    put<STREAM>(pack_e4m3_in_range(v[0], v[1], v[2], v[3]), reinterpret_cast<Place*>(p));
+    put<STREAM, 1>(pack_e4m3_in_range(v[0], v[1], v[2], v[3]), p);
   }
 };
 
