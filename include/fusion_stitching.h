@@ -306,7 +306,10 @@ int64_t fs_plan_source(const fs_plan *p, char *text, size_t capacity);
  * fs_program_info.workspace_bytes rounded up to 256 (not for steps with a joint fold).  Any other
  * such call, fs_execute_static's too, returns FS_ERR_INVALID_ARG before anything is launched.
  * Normalising more positions than a workgroup keeps in registers, and the sums over more than a
- * few rows or batch entries, take two or three launches and a workspace.                                   */
+ * few rows or batch entries, take two or three launches and a workspace.  Groups of more than 1024
+ * channels of FS_F32, 2048 of a 16-bit type (some of few positions: up to twice that) run as the
+ * per-op plan, and so does the normalisation of so many short groups that a wavefront for each
+ * would be 2^32 threads.                                                                  */
 
 /* ---- execution (the run-time hot path) --------------------------------------- */
 
