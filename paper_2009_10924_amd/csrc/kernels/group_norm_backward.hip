@@ -23,10 +23,11 @@ template <typename T> struct GnValue<T, true> { typedef e4m3_t type; };
 
 // What a thread knows of its channels.  Its values are worked on about their mean, v - shift (an 8-bit value as it is), and the
 // factor that makes xh of them is multiplied into what is per channel: z = (v - shift) (scale gamma) + beta,  sum dz xh = scale
-// sum dz (v - shift).
+// sum dz (v - shift).  dx needs scale rstd, of values and their mean a square that is no float32 for deviations below 1e-19: then
+// they are worked on times 2^50, exactly and at no cost (the subtraction is the end of a product), and scale is that much smaller.
 template <typename T, int VEC, bool FROM8>
 struct GnChannels {
-  float shift[VEC], scale[VEC], slope[VEC], be[VEC], ga[VEC];
+  float shift[VEC], scale[VEC], slope[VEC], be[VEC], ga[VEC], times;
   // `centre`: means, or the checkpoint's scales
   __device__ __forceinline__ void load(const GnShape& p, const GnLane& l, uint32_t n, uint32_t set, const float* centre, const float* rstd,
                                        const T* gamma, const T* beta) {
@@ -51,10 +52,20 @@ struct GnChannels {
         scale[e] = FROM8 ? centre[g] : rstd[g];
       }
     }
+    if constexpr (!FROM8) {
+      float most = scale[0];
+#pragma unroll
+      for (int e = 1; e < VEC; ++e) most = fmaxf(most, scale[e]);
+      const bool large = most > 0x1p50f;
+      times = large ? 0x1p50f : 1.0f;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) shift[e] *= -times, scale[e] *= large ? 0x1p-50f : 1.0f;
+    }
 #pragma unroll
     for (int e = 0; e < VEC; ++e) slope[e] = scale[e] * ga[e];
   }
-  __device__ __forceinline__ float about_mean(float v, int e) const { return FROM8 ? v : v - shift[e]; }
+  __device__ __forceinline__ float about_mean(float v, int e) const { return FROM8 ? v : __builtin_fmaf(v, times, shift[e]); }
+  __device__ __forceinline__ float rstd_of(int e) const { return scale[e] * times; }   // of values and their mean
   template <int ACT>
   __device__ __forceinline__ float dz(float v, float dy, int e) const {   // v: about its mean
     if constexpr (ACT == ACT_NONE) return dy;
@@ -197,7 +208,7 @@ __global__ void __launch_bounds__(NT) k_gn_bwd_slab(const typename GnValue<T, FR
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       const uint32_t g = fast_div(l.col + e, p.div_dim);
-      gr.set(e, ch, FROM8 ? rstd[n * p.groups + set * p.set_groups + g] : ch.scale[e], means[2u * g], means[2u * g + 1u]);
+      gr.set(e, ch, FROM8 ? rstd[n * p.groups + set * p.set_groups + g] : ch.rstd_of(e), means[2u * g], means[2u * g + 1u]);
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -369,7 +380,7 @@ __global__ void __launch_bounds__(256) k_gn_bwd_apply(const typename GnValue<T, 
   for (int e = 0; e < VEC; ++e) {
     const uint32_t g = fast_div(l.col + e, p.div_dim), at = n * p.groups + set * p.set_groups + g;
     const f32x2 m = *reinterpret_cast<const f32x2*>(JOIN ? lds + 2u * g : means + 2u * (size_t)at);
-    gr.set(e, ch, FROM8 ? rstd[at] : ch.scale[e], m.x, m.y);
+    gr.set(e, ch, FROM8 ? rstd[at] : ch.rstd_of(e), m.x, m.y);
   }
   auto put = [&](typename VecIo<X, VEC>::Raw rx, typename VecIo<T, VEC>::Raw rd, uint32_t at) {
     float v[VEC], d[VEC];

@@ -122,3 +122,20 @@ def test_sums_over_very_many_entries(shape, dtype):
             per_term = 1e-5 + 4 * U + 1.13 * group_norm_chain(info, shape, dtype, True) * U
             return {"dx": bound["dx"], "dbeta": per_term * dy.sum((0, 1), keepdims=True), "dgamma": per_term * (dy * n).sum((0, 1), keepdims=True)}
         compare(spec, inp, env, allowed, "group_norm_backward")
+
+
+@pytest.mark.parametrize("size", [1e-19, 1e-10, 1e10, 1e18])
+@pytest.mark.parametrize("shape", [(2, 60, 4, 8), (2, 5000, 4, 10), (3, 7, 4, 3)], ids=NAME)
+def test_backward_of_very_small_and_very_large_values(shape, size):
+    """x, its mean and its deviation times `size`, the reciprocal deviation divided by it: its square is no float32, dx still is one."""
+    for act in ("none", "silu"):
+        spec = group_norm_backward_graph(*shape, dtype="f32", act=act, keep="stats")
+        inp = make_inputs(spec, seed=6)
+        for name in ("x", "mu"):
+            inp[name] = (inp[name].astype(np.float64) * size).astype(np.float32)
+        inp["r"] = (inp["r"].astype(np.float64) / size).astype(np.float32)
+        inp["dy"] = inp["dy"] * np.float32(8)   # (group means of g xh up to about 8)
+        inp["dy"] = np.copysign(np.abs(inp["dy"]), (inp["x"] - inp["mu"]) * inp["gamma"]).astype(np.float32)
+        env = O.evaluate(spec, inp, keep_all=True)
+        allowed = backward_bounds(env, "f32")
+        compare(spec, inp, env, lambda info: allowed, "group_norm_backward")
