@@ -128,7 +128,7 @@ bool build_checkpoint(const fs_graph& g, std::vector<Candidate>* out, PackForm*)
     l.ptr[4] = out_ref(g.tensors[t_s].output_slot);
   };
   // The estimate of a launch (us), fitted to every candidate of 360 shapes of 1 to 2^26 values, three dtypes: the one chosen is 1.0 %
-  // behind the fastest (geometric mean; 2.7 % by the general evaluator, which knows nothing of 8-bit stores, whose runs are the
+  // behind the fastest on 50 others (geometric mean; 2.7 % by the general evaluator, which knows nothing of 8-bit stores, whose runs are the
   // shortest of a lane group's).  A step of few lanes writes a part of a line; rows that are no multiple of an access end inside one.
   auto estimate = [&](KernelCost* kc, double lanes, int K, bool workgroup) {
     const double bytes = n * esz * (t_y >= 0 ? 2 : 1) + n + 4.0 * p.rows;

@@ -396,7 +396,7 @@ def checkpoint_backward_graph(rows: int, blocks: int, block: int, dtype: str = "
 
 def checkpointed_block_graph(batch: int = 8, positions: int = 4096, groups: int = 32, dim: int = 10, hidden: int = 1280, block: int = 128,
                              dtype: str = "bf16", act: str = "silu") -> GraphSpec:
-    """Forward and backward of a residual branch that keeps 8-bit checkpoints, with the matrix products taken out (as in
+    """Forward and backward of the branch beside a residual connection (its adds left out) that keeps 8-bit checkpoints, with the matrix products taken out (as in
     transformer_block_graph): group normalisation and its activation (f1_), a product to `hidden` channels, bias and tanh-GELU
     (f2_), the rest of the network; then back through the bias and GELU (b2_), the product, and the normalisation (b1_).  Backward
     reads what forward stored: 20 + 8 + 4 + 25 ops with SiLU."""
