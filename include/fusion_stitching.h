@@ -308,8 +308,8 @@ int64_t fs_plan_source(const fs_plan *p, char *text, size_t capacity);
  * Normalising more positions than a workgroup keeps in registers, and the sums over more than a
  * few rows or batch entries, take two or three launches and a workspace.  Groups of more than 1024
  * channels of FS_F32, 2048 of a 16-bit type (some of few positions: up to twice that) run as the
- * per-op plan, and so does the normalisation of so many short groups that a wavefront for each
- * would be 2^32 threads.                                                                  */
+ * per-op plan, and so does the normalisation of so many short groups that a workgroup for each
+ * would be 2^32 threads or take longer than the ops one by one.                             */
 
 /* ---- execution (the run-time hot path) --------------------------------------- */
 

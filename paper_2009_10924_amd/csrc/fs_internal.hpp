@@ -105,7 +105,7 @@ struct Candidate {
   fs_plan_info info;
   std::vector<Launch> launches;
   KernelCost cost;               // description of the (single) stitched kernel; unused for unfused plans
-  bool apart = false;            // no output may share memory with an input or another output: a call where one does is not its
+  bool apart = false;            // no output may share memory with an input or another output: where one does, the call is not run by it
   bool fallback = false;         // offered only for the case that no other candidate can be used (the interpreted row
                                  // program beside the kernels generated for the same pattern): passed over by the choice
                                  // while another candidate stands, still reachable by index

@@ -223,8 +223,9 @@ extern "C" fs_status fs_execute_static(const fs_plan* p, const void* const* inpu
   if (c.info.workspace_bytes > (int64_t)FS_STATIC_SCRATCH_BYTES)
     return fs::fail(FS_ERR_WORKSPACE, "fs_execute_static: the plan needs %lld bytes of scratch, the static array holds %lld",
                     (long long)c.info.workspace_bytes, (long long)FS_STATIC_SCRATCH_BYTES);
-  if (!fs::candidate_for(p, inputs, outputs, 0)) return FS_ERR_INVALID_ARG;   // (per-op launches only in a workspace of the caller's)
-  return fs::run_launches(p, c, inputs, outputs, reinterpret_cast<void*>(0x7000000), hip_stream, c.launches.size());
+  const fs::Candidate* const run = fs::candidate_for(p, inputs, outputs, 0);   // (per-op launches only in a workspace of the caller's)
+  if (!run) return FS_ERR_INVALID_ARG;
+  return fs::run_launches(p, *run, inputs, outputs, reinterpret_cast<void*>(0x7000000), hip_stream, run->launches.size());
 }
 extern "C" fs_status fs_stream_probe(void*, const void*, size_t, size_t, int32_t, int32_t, int32_t, void*) {
   return fs::fail(FS_ERR_HIP, "fs_stream_probe: not part of the host stub");

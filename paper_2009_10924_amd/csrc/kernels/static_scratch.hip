@@ -49,7 +49,8 @@ extern "C" fs_status fs_execute_static(const fs_plan* p, const void* const* inpu
   if (c.info.workspace_bytes > (int64_t)FS_STATIC_SCRATCH_BYTES)
     return fs::fail(FS_ERR_WORKSPACE, "fs_execute_static: the plan needs %lld bytes of scratch, the static array holds %lld; use fs_execute with a workspace",
                     (long long)c.info.workspace_bytes, (long long)FS_STATIC_SCRATCH_BYTES);
-  if (!fs::candidate_for(p, inputs, outputs, 0)) return FS_ERR_INVALID_ARG;   // (per-op launches only in a workspace of the caller's)
+  const fs::Candidate* const run = fs::candidate_for(p, inputs, outputs, 0);   // (per-op launches only in a workspace of the caller's)
+  if (!run) return FS_ERR_INVALID_ARG;
   void* ws = nullptr;
   if (c.info.workspace_bytes > 0) {
     const fs_status a = scratch_of_current_device(&ws);
@@ -57,7 +58,7 @@ extern "C" fs_status fs_execute_static(const fs_plan* p, const void* const* inpu
   }
   // Nothing has to start at zero: every kernel that reads the scratch reads what a launch of the same call
   // wrote there before it (the fold reads the partial sums of the launch in front of it).
-  return fs::run_launches(p, c, inputs, outputs, ws, hip_stream, c.launches.size());
+  return fs::run_launches(p, *run, inputs, outputs, ws, hip_stream, run->launches.size());
 } catch (...) {
   return fs::fail_caught("fs_execute_static");
 }
