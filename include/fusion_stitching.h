@@ -88,7 +88,9 @@ enum fs_opcode {
   FS_SIGMOID = 20,       /* 1 / (1 + exp(-x))                                                      */
   FS_RELU = 21,          /* max(x, 0)                                                              */
   FS_ABS = 22, FS_SQRT = 23,                                  /* 1 operand, attr: none             */
-  FS_OPCODE_COUNT = 24
+  FS_DROPOUT = 24,       /* 2 operands: x, state           attr: fs_attr_dropout                   */
+  FS_ROTARY = 25,        /* 2 operands: x, positions       attr: fs_attr_rotary                    */
+  FS_OPCODE_COUNT = 26
 };
 
 typedef struct fs_attr_scalar { double value; } fs_attr_scalar;
@@ -96,6 +98,34 @@ typedef struct fs_attr_axis { int32_t axis; } fs_attr_axis;               /* 0 <
 typedef struct fs_attr_perm { int32_t perm[FS_MAX_RANK]; } fs_attr_perm;   /* first `rank` entries    */
 typedef struct fs_attr_dims { int32_t rank; int64_t dims[FS_MAX_RANK]; } fs_attr_dims;
 typedef struct fs_attr_dtype { int32_t dtype; } fs_attr_dtype;
+
+/* FS_DROPOUT: x where an element is kept, times 1 / (1 - probability), and 0 where it is not.  What is kept follows from the
+ * element's place and from `state`, an FS_I32 graph input of extents [4]: seed (low word, high word) and offset (low, high).  The
+ * mask is never stored: the gradient is FS_DROPOUT of the incoming gradient with the same state, sequence and probability at the
+ * same extents.  A step of training gives each call a new offset in device memory, so a captured graph draws anew at each replay.
+ *   The probability is held in 16 bits: t = round(65536 * probability), 0 <= t <= 65535 (else FS_ERR_INVALID_ARG).  Element (row,
+ * column) of x, rows counted along the leading axes, has the number w of 16 bits that stands at place column % 8 (the low half of
+ * a word first) among the four words that Philox4x32-10 (Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", 2011)
+ * makes of the counter (row * ceil(columns / 8) + column / 8, sequence, offset low, offset high) under the key (seed low, seed
+ * high).  It is kept if w >= t, and multiplied by 65536 / (65536 - t) rounded to float32.  Dropouts that share a state
+ * take a `sequence` each.                                                                          */
+typedef struct fs_attr_dropout { double probability; uint32_t sequence; uint32_t reserved; /* 0 */ } fs_attr_dropout;
+
+/* FS_ROTARY: pairs of elements of x's last axis, turned by angles that grow with the row's position along one of n_axes axes
+ * (text: 1; time, height, width of a picture: 3).  `positions` is an FS_I32 tensor [.., n_axes] whose leading extents stretch over those of
+ * x (ranks right-aligned, each 1 or x's own; [B,S,1,3] beside [B,S,H,D]); positions may be any 32-bit numbers, negative too.
+ *   Of R = pairs[0] + .. pairs, the first pairs[0] belong to axis 0, the next pairs[1] to axis 1, and so on.  Pair i is elements
+ * (i, i + R), or (2i, 2i + 1) with `interleaved`; what lies behind the first 2R elements is left as it is.  Its angle is
+ * position[axis] * base^(-i / R), or with `restart` base^(-j / pairs[axis]) for the j-th pair of its axis; with `inverse` the
+ * negative of that (the gradient of the forward rotation).  (a, b) becomes (a cos - b sin, b cos + a sin).  Angles are formed in
+ * 64 bits.  1 <= n_axes <= FS_MAX_RANK, every pairs[k] >= 1, 2R <= x's last extent, R <= 4096, 1 <= base <= 1e30 (else
+ * FS_ERR_INVALID_ARG); a positions tensor that does not stretch: FS_ERR_SHAPE.                       */
+typedef struct fs_attr_rotary {
+  double base;
+  int32_t n_axes;
+  int32_t pairs[FS_MAX_RANK];
+  int32_t interleaved, restart, inverse;   /* 0 or 1 */
+} fs_attr_rotary;
 
 /* Composition schemes (Section 4.1).  LOCAL = kernel packing + thread composition
  * (values stay in the lane that made them); WAVE = warp composition on a 64-wide

@@ -19,6 +19,8 @@ Readings of points the paper leaves open (it states no numerics at all):
   * tanh-GELU: gelu(z) = z/2 * (1 + tanh(u)), u = sqrt(2/pi) * (z + 0.044715 z^3),
     and gelu_tanh_grad is its derivative with respect to z;
   * log is the natural logarithm, sigmoid(x) = 1 / (1 + exp(-x)), relu(x) = max(x, 0);
+  * dropout keeps an element where its 16-bit number (Philox4x32-10 of its place, see dropout_kept) reaches round(65536 p);
+  * rotary turns pairs of the last axis by position * base^-e;
   * `convert` rounds to the target dtype (nearest-even) when other ops consume
     it; when it produces a subgraph output the un-rounded float64 value is
     reported unless `round_outputs=True`, so the comparison tolerance, not the
@@ -190,6 +192,56 @@ def op_convert(a, dtype):
     return round_to(a, dtype)
 
 
+def philox_words(counter, key, rounds: int = 10):
+    """Philox4x32 (Salmon et al., 2011) of counters [.., 4] under a key of two words, in
+    64-bit integers: each round multiplies words 0 and 2 by a constant each, and the high half of one product joins the
+    other counter words with the key, which grows by a constant a round."""
+    u64, mask, half = np.uint64, np.uint64(0xFFFFFFFF), np.uint64(32)
+    c = [np.asarray(counter, dtype=np.uint64)[..., i] & mask for i in range(4)]
+    k = [int(key[0]) & 0xFFFFFFFF, int(key[1]) & 0xFFFFFFFF]
+    for _ in range(rounds):
+        p0, p1 = c[0] * u64(0xD2511F53), c[2] * u64(0xCD9E8D57)
+        c = [(p1 >> half) ^ c[1] ^ u64(k[0]), p1 & mask, (p0 >> half) ^ c[3] ^ u64(k[1]), p0 & mask]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    return np.stack(c, axis=-1)
+
+
+def dropout_kept(dims, state, probability, sequence=0):
+    """Which elements of a tensor of extents `dims` a dropout keeps (bool), and the integer threshold."""
+    cols = dims[-1]
+    rows = int(np.prod(dims[:-1], dtype=np.int64))
+    groups = -(-cols // 8)
+    words = [int(w) & 0xFFFFFFFF for w in np.asarray(state).reshape(-1)]
+    counter = np.zeros((rows * groups, 4), dtype=np.uint64)
+    counter[:, 0] = np.arange(rows * groups)
+    counter[:, 1], counter[:, 2], counter[:, 3] = sequence & 0xFFFFFFFF, words[2], words[3]
+    w = philox_words(counter, words[:2])
+    numbers = np.stack([w & np.uint64(0xFFFF), w >> np.uint64(16)], axis=-1).reshape(rows, groups * 8)[:, :cols]
+    threshold = int(np.rint(probability * 65536.0))
+    return (numbers >= np.uint64(threshold)).reshape(dims), threshold
+
+
+def op_dropout(a, state, probability, sequence=0):
+    kept, threshold = dropout_kept(a.shape, state, probability, sequence)
+    scale = float(np.float32(65536.0 / (65536 - threshold)))   # the factor is a float32
+    return np.where(kept, a * scale, 0.0)
+
+
+def op_rotary(a, positions, base, pairs, interleaved=False, restart=False, inverse=False):
+    total, angles = sum(pairs), []
+    for axis, n in enumerate(pairs):
+        i = np.arange(n, dtype=np.float64) + (0 if restart else sum(pairs[:axis]))
+        angles.append(np.asarray(positions, dtype=np.float64)[..., axis:axis + 1] * float(base) ** (-i / (n if restart else total)))
+    angle = np.concatenate(angles, axis=-1) * (-1.0 if inverse else 1.0)
+    c, s = np.cos(angle), np.sin(angle)
+    first = slice(0, 2 * total, 2) if interleaved else slice(0, total)
+    second = slice(1, 2 * total, 2) if interleaved else slice(total, 2 * total)
+    out = np.array(a, dtype=np.float64)
+    out[..., first] = a[..., first] * c - a[..., second] * s
+    out[..., second] = a[..., second] * c + a[..., first] * s
+    return out
+
+
 _BINARY = {"add": op_add, "sub": op_sub, "mul": op_mul, "div": op_div, "max": op_max}
 _UNARY = {"square": op_square, "exp": op_exp, "rsqrt": op_rsqrt, "tanh": op_tanh,
           "gelu_tanh": op_gelu_tanh, "gelu_tanh_grad": op_gelu_tanh_grad,
@@ -238,6 +290,10 @@ def evaluate(graph, inputs: Mapping[str, np.ndarray], round_outputs: bool = Fals
             r = op_reduce_mean(args[0], op.attr["axis"])
         elif code == "transpose":
             r = op_transpose(args[0], op.attr["perm"])
+        elif code == "dropout":
+            r = op_dropout(args[0], args[1].astype(np.int64), op.attr["probability"], op.attr.get("sequence", 0))
+        elif code == "rotary":
+            r = op_rotary(args[0], args[1], **op.attr)
         elif code == "convert":
             pre_convert[op.out] = args[0]
             r = op_convert(args[0], op.attr["dtype"])

@@ -18,7 +18,7 @@ OPCODE = {
     "add": 0, "sub": 1, "mul": 2, "div": 3, "max": 4, "scale": 5, "add_scalar": 6, "square": 7,
     "exp": 8, "rsqrt": 9, "tanh": 10, "gelu_tanh": 11, "gelu_tanh_grad": 12, "broadcast": 13,
     "log": 19, "sigmoid": 20, "relu": 21, "abs": 22, "sqrt": 23,
-    "reduce_sum": 14, "reduce_max": 15, "reduce_mean": 16, "transpose": 17, "convert": 18,
+    "reduce_sum": 14, "reduce_max": 15, "reduce_mean": 16, "transpose": 17, "convert": 18, "dropout": 24, "rotary": 25,
 }
 SCHEME = {"auto": 0, "unfused": 1, "local": 2, "wave": 3, "lds": 4, "global": 5}
 SCHEME_NAME = {v: k for k, v in SCHEME.items()}
@@ -63,6 +63,15 @@ class fs_attr_dims(C.Structure):
 
 class fs_attr_dtype(C.Structure):
     _fields_ = [("dtype", C.c_int32)]
+
+
+class fs_attr_dropout(C.Structure):
+    _fields_ = [("probability", C.c_double), ("sequence", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class fs_attr_rotary(C.Structure):
+    _fields_ = [("base", C.c_double), ("n_axes", C.c_int32), ("pairs", C.c_int32 * FS_MAX_RANK), ("interleaved", C.c_int32),
+                ("restart", C.c_int32), ("inverse", C.c_int32)]
 
 
 class fs_plan_opts(C.Structure):
@@ -257,6 +266,12 @@ class Graph:
             a = fs_attr_dims(len(dims), (C.c_int64 * FS_MAX_RANK)(*(dims + [1] * (FS_MAX_RANK - len(dims)))))
         elif opcode == "convert":
             a = fs_attr_dtype(DTYPE[attr["dtype"]])
+        elif opcode == "dropout":
+            a = fs_attr_dropout(float(attr["probability"]), int(attr.get("sequence", 0)), 0)
+        elif opcode == "rotary":
+            pairs = list(attr["pairs"])
+            a = fs_attr_rotary(float(attr["base"]), len(pairs), (C.c_int32 * FS_MAX_RANK)(*pairs[:FS_MAX_RANK]), int(attr.get("interleaved", False)),
+                               int(attr.get("restart", False)), int(attr.get("inverse", False)))
         if a is None:
             return _check(self._lib.fs_graph_op(self.handle, OPCODE[opcode], len(inputs), ins, None, 0))
         return _check(self._lib.fs_graph_op(self.handle, OPCODE[opcode], len(inputs), ins,
@@ -596,7 +611,7 @@ def output_shapes(spec) -> Dict[str, tuple]:
     dims = {t.name: tuple(t.dims) for t in spec.inputs}
     for op in spec.ops:
         a = dims[op.inputs[0]]
-        if len(op.inputs) == 2:
+        if len(op.inputs) == 2 and op.opcode not in ("dropout", "rotary"):
             b = dims[op.inputs[1]]
             r = max(len(a), len(b))
             pa, pb = (1,) * (r - len(a)) + a, (1,) * (r - len(b)) + b

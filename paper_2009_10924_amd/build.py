@@ -17,9 +17,11 @@ LIB_PATH = os.path.join(PKG_DIR, "libfusion_stitching.so")
 
 SOURCES = [
     "fs_graph.cpp", "fs_unfused.cpp", "fs_match.cpp", "fs_cost.cpp", "fs_stitch.cpp", "fs_family_softmax.cpp", "fs_family_layernorm.cpp", "fs_family_gelu.cpp",
-    "fs_family_transpose.cpp", "fs_family_rows.cpp", "fs_family_checkpoint.cpp", "fs_family_group_norm.cpp", "fs_plan.cpp", "fs_pack.cpp", "fs_rowprog.cpp", "fs_explore.cpp", "fs_program.cpp", "fs_codegen.cpp",
+    "fs_family_transpose.cpp", "fs_family_rows.cpp", "fs_family_checkpoint.cpp", "fs_family_group_norm.cpp", "fs_family_dropout.cpp", "fs_family_rmsnorm_8bit.cpp", "fs_family_rotary.cpp",
+    "fs_plan.cpp", "fs_pack.cpp", "fs_rowprog.cpp", "fs_explore.cpp", "fs_program.cpp", "fs_codegen.cpp",
     "kernels/launch.hip", "kernels/unfused.hip", "kernels/softmax.hip", "kernels/layernorm.hip",
     "kernels/gelu.hip", "kernels/tchain.hip", "kernels/rowops.hip", "kernels/pack.hip", "kernels/rowprog.hip", "kernels/checkpoint.hip", "kernels/group_norm.hip", "kernels/group_norm_backward.hip",
+    "kernels/dropout.hip", "kernels/rmsnorm_8bit.hip", "kernels/rotary.hip",
     "kernels/gen_runtime.hip", "kernels/gen_sample.hip", "kernels/static_scratch.hip", "kernels/stream_probe.hip",
 ]
 

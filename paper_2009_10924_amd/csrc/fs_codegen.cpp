@@ -71,6 +71,13 @@ std::string expression(int op, const std::string& a, const std::string& b, int a
   }
 }
 
+// the states of the program's dropouts
+std::string state_loads(const RowProgP& p) {
+  std::string t;
+  for (int i = 0; i < p.n_states; ++i) t += fmt("  const DropKey drop%d = drop_key(a.rscal[%d]);\n", i, p.n_rscal + i);
+  return t;
+}
+
 // row index of an operand stretched or permuted along the leading axes, from the row's index (lead0, lead1, lead2) along them
 std::string stretched_row(const uint32_t (&ms)[3], const char* pre = "") {
   return fmt("(size_t)(%slead0 * %uu + %slead1 * %uu + %slead2 * %uu)", pre, ms[0], pre, ms[1], pre, ms[2]);
@@ -178,7 +185,7 @@ std::vector<int> generated_ptr_slots(const RowProgP& p) {
   std::vector<int> slots;
   for (int i = 0; i < p.n_full; ++i) slots.push_back(kSlotFull + i);
   for (int i = 0; i < p.n_col; ++i) slots.push_back(kSlotCol + i);
-  for (int i = 0; i < p.n_rscal; ++i) slots.push_back(kSlotRscal + i);
+  for (int i = 0; i < p.n_rscal + p.n_states; ++i) slots.push_back(kSlotRscal + i);
   for (int i = 0; i < p.n_instr; ++i) {
     if (p.instr[i].op == PO_STORE) slots.push_back(kSlotOut + p.instr[i].dst);
     if (p.instr[i].op == PO_STORE_SCAL) slots.push_back(kSlotRout + p.instr[i].dst);
@@ -261,6 +268,10 @@ std::string instruction_text(const RowProgP& p, const ProgInstr& in, bool block,
     case PO_COLSUM:
       t += fmt("  row.colsum_add(acc, cs%d);\n", in.dst);
       return t;
+    case PO_DROPOUT:
+      t += fmt("  row.dropout(acc, drop%d, %uu, %uu, %s);\n", p.drop_state[in.b], p.drop_sequence[in.b], p.drop_threshold[in.b], literal(p.drop_scale[in.b]).c_str());
+      if (keep) t += fmt("#pragma unroll\n  for (int j = 0; j < KV; ++j) r%d[j] = acc[j];\n", in.dst);
+      return t;
     case PO_RSUM: case PO_RMAX: case PO_RSUMSQ: {
       const bool is_max = in.op == PO_RMAX;
       const std::string slot = block ? fmt("slots + %d", n_waves * *reduction_no) : std::string("nullptr");
@@ -325,7 +336,7 @@ std::string chunked_body(const RowProgP& p, const char* entry) {
   row_type("HeadRow", chunk, "EDGE_FIRST", "the row's first chunk");
   row_type("TailRow", tail, "EDGE_LAST", "the row's last chunk");
   auto chunk_type = [&](uint32_t c) { return c == NC - 1u ? "TailRow" : (c == 0 ? "HeadRow" : "Row"); };
-  s += "  constexpr int KV = Row::KV;\n";
+  s += "  constexpr int KV = Row::KV;\n" + state_loads(p);
   if (n_red > 0) s += fmt("  __shared__ float slots[%d];\n", n_waves * n_red);
   for (int q = 0; q < n_red; ++q) s += fmt("  float red%d;\n", q);
   s += "  const Row row0(fs_block);\n";
@@ -486,7 +497,7 @@ std::string body_with_entry(const RowProgP& p, const char* entry, bool member) {
   else if (CT > 1 || p.stream) rest = fmt(", %uu%s", CT, p.stream ? ", true" : "");
   s += fmt("  typedef GenRow<%uu, %uu, %d, %d, %uu, %s, %uu, %uu%s> Row;\n", p.rows, tile_cols, p.vec, p.vecs_per_lane,
            (uint32_t)p.lanes_per_row, block ? "true" : "false", R, p.cols, rest.c_str());
-  s += "  constexpr int KV = Row::KV;\n";
+  s += "  constexpr int KV = Row::KV;\n" + state_loads(p);
   const int n_waves = block ? p.lanes_per_row / 64 : 4;
   const bool looped = p.n_colsum > 0 || R > 1u;
   // a workgroup that walks several rows alternates between two sets of reduction slots: a wave may write the next
@@ -659,7 +670,7 @@ static std::string column_sum_member(const RowProgP& p, const char* entry, int l
   const uint32_t tile_cols = CT > 1 ? Q * (uint32_t)p.vec : p.cols, U = (p.rows + G - 1u) / G;   // U rows per thread
   std::string s = fmt("static __device__ __forceinline__ void %s(const GenArgs& a, const uint32_t fs_block) {\n", entry);
   s += fmt("  typedef GenRow<%uu, %uu, %d, 1, %uu, false, %uu, %uu, %uu> Row;\n", p.rows, tile_cols, p.vec, Q, U, p.cols, CT);
-  s += "  constexpr int KV = Row::KV;\n";
+  s += "  constexpr int KV = Row::KV;\n" + state_loads(p);
   s += fmt("  __shared__ __attribute__((aligned(16))) float colred[%d][4 * Row::PADDED_COLS];\n", p.n_colsum);
   for (int i = 0; i < p.n_colsum; ++i) s += fmt("  float cs%d[KV];\n#pragma unroll\n  for (int j = 0; j < KV; ++j) cs%d[j] = 0.0f;\n", i, i);
   s += "  const Row first(0u, fs_block);\n";

@@ -178,6 +178,14 @@ struct Explorer {
           r = fs_graph_op(sub->g, op.opcode, op.n_in, in, &a, sizeof a);
           break;
         }
+        case FS_DROPOUT: {
+          fs_attr_dropout a = {op.probability, op.draw.sequence, 0};
+          r = fs_graph_op(sub->g, op.opcode, op.n_in, in, &a, sizeof a);
+          break;
+        }
+        case FS_ROTARY:
+          r = fs_graph_op(sub->g, op.opcode, op.n_in, in, &op.rotary, sizeof op.rotary);
+          break;
         default:
           r = fs_graph_op(sub->g, op.opcode, op.n_in, in, nullptr, 0);
           break;

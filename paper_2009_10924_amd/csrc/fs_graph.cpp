@@ -5,6 +5,7 @@
 #include <cstring>
 
 #include <algorithm>
+#include <cmath>
 #include <exception>
 #include <new>
 
@@ -52,7 +53,7 @@ const char* opcode_name(int32_t op) {
   static const char* names[FS_OPCODE_COUNT] = {
       "add", "sub", "mul", "div", "max", "scale", "add_scalar", "square", "exp", "rsqrt", "tanh",
       "gelu_tanh", "gelu_tanh_grad", "broadcast", "reduce_sum", "reduce_max", "reduce_mean", "transpose", "convert",
-      "log", "sigmoid", "relu", "abs", "sqrt"};
+      "log", "sigmoid", "relu", "abs", "sqrt", "dropout", "rotary"};
   return (op >= 0 && op < FS_OPCODE_COUNT) ? names[op] : "?";
 }
 const char* scheme_name(int32_t s) {
@@ -69,7 +70,18 @@ bool holds_8bit(const fs_graph& g) {
   return false;
 }
 
-static int operand_count(int32_t opcode) { return opcode <= FS_MAX ? 2 : 1; }
+static bool reads_integers(int32_t opcode) { return opcode == FS_DROPOUT || opcode == FS_ROTARY; }   // as operand 1
+static int operand_count(int32_t opcode) { return opcode <= FS_MAX || reads_integers(opcode) ? 2 : 1; }
+
+// `positions` [.., n_axes] stretches over the leading extents of `x`
+static bool positions_stretch(const Tensor& positions, const Tensor& x, int32_t n_axes) {
+  if (positions.rank > x.rank || positions.dims[positions.rank - 1] != n_axes) return false;
+  for (int k = 1; k < positions.rank; ++k) {
+    const int64_t d = positions.dims[positions.rank - 1 - k];
+    if (d != 1 && d != x.dims[x.rank - 1 - k]) return false;
+  }
+  return true;
+}
 
 }  // namespace fs
 
@@ -141,6 +153,10 @@ fs_tensor fs_graph_op(fs_graph* g, int32_t opcode, int32_t n_in, const fs_tensor
   const bool is_transpose = opcode == FS_TRANSPOSE;
   for (int i = 0; i < n_in; ++i) {
     const int32_t dt = g->tensors[in[i]].dtype;
+    if (i == 1 && reads_integers(opcode)) {
+      if (dt != FS_I32) return fail(FS_ERR_DTYPE, "fs_graph_op(%s): operand 1 has dtype %s, not i32", opcode_name(opcode), dtype_name(dt));
+      continue;
+    }
     if (!float_dtype(dt) && !is_transpose)
       return fail(FS_ERR_DTYPE, "fs_graph_op(%s): operand %d has dtype %s; only transpose moves integer tensors", opcode_name(opcode), i, dtype_name(dt));
     if (dt == FS_E4M3 && is_transpose) return fail(FS_ERR_DTYPE, "fs_graph_op(transpose): 8-bit tensors are not transposed; convert first");
@@ -198,6 +214,39 @@ fs_tensor fs_graph_op(fs_graph* g, int32_t opcode, int32_t n_in, const fs_tensor
     if (!float_dtype(op.to_dtype)) return fail(FS_ERR_DTYPE, "fs_graph_op(convert): target dtype %d is not a float type", op.to_dtype);
     r.rank = a.rank;
     r.dtype = op.to_dtype;
+    memcpy(r.dims, a.dims, sizeof r.dims);
+  } else if (opcode == FS_DROPOUT) {
+    if (!need_attr(sizeof(fs_attr_dropout))) return fail(FS_ERR_INVALID_ARG, "fs_graph_op(dropout): needs fs_attr_dropout");
+    const fs_attr_dropout* d = static_cast<const fs_attr_dropout*>(attr);
+    const Tensor& state = g->tensors[in[1]];
+    if (state.producer >= 0 || state.rank != 1 || state.dims[0] != 4)
+      return fail(FS_ERR_SHAPE, "fs_graph_op(dropout): the state is a graph input of extents [4]");
+    // (a probability so close to 1 that it rounds to 65536 / 65536 would keep nothing and multiply it by infinity)
+    if (!(d->probability >= 0.0 && d->probability < 65535.5 / 65536.0) || d->reserved != 0)
+      return fail(FS_ERR_INVALID_ARG, "fs_graph_op(dropout): probability %g outside 0 .. 65535 / 65536, or a reserved field that is not 0", d->probability);
+    op.probability = d->probability;
+    op.draw.threshold = (uint32_t)std::nearbyint(d->probability * 65536.0);
+    op.draw.sequence = d->sequence;
+    op.draw.scale = (float)(65536.0 / (65536.0 - (double)op.draw.threshold));
+    r.rank = a.rank;
+    memcpy(r.dims, a.dims, sizeof r.dims);
+  } else if (opcode == FS_ROTARY) {
+    if (!need_attr(sizeof(fs_attr_rotary))) return fail(FS_ERR_INVALID_ARG, "fs_graph_op(rotary): needs fs_attr_rotary");
+    const fs_attr_rotary* d = static_cast<const fs_attr_rotary*>(attr);
+    const auto flag = [](int32_t v) { return v == 0 || v == 1; };
+    if (d->n_axes < 1 || d->n_axes > FS_MAX_RANK || !(d->base >= 1.0 && d->base <= 1e30) || !flag(d->interleaved) || !flag(d->restart) || !flag(d->inverse))
+      return fail(FS_ERR_INVALID_ARG, "fs_graph_op(rotary): n_axes %d, base %g, or a flag that is neither 0 nor 1", d->n_axes, d->base);
+    int64_t pairs = 0;
+    for (int k = 0; k < d->n_axes; ++k) {
+      if (d->pairs[k] < 1) return fail(FS_ERR_INVALID_ARG, "fs_graph_op(rotary): axis %d has %d pairs", k, d->pairs[k]);
+      pairs += d->pairs[k];
+    }
+    if (pairs > 4096 || 2 * pairs > a.dims[a.rank - 1])
+      return fail(FS_ERR_INVALID_ARG, "fs_graph_op(rotary): %lld pairs in a last axis of %lld (4096 at most)", (long long)pairs, (long long)a.dims[a.rank - 1]);
+    if (!positions_stretch(g->tensors[in[1]], a, d->n_axes))
+      return fail(FS_ERR_SHAPE, "fs_graph_op(rotary): positions of these extents do not stretch over the operand's leading axes");
+    op.rotary = *d;
+    r.rank = a.rank;
     memcpy(r.dims, a.dims, sizeof r.dims);
   } else {  // plain unary
     r.rank = a.rank;

@@ -37,6 +37,9 @@ struct Op {
   int32_t axis = 0;                        // reductions
   int32_t perm[FS_MAX_RANK] = {0, 1, 2, 3};
   int32_t to_dtype = FS_F32;               // FS_CONVERT
+  DropoutDraw draw = {};                        // FS_DROPOUT
+  double probability = 0.0;                // ... as it was given
+  fs_attr_rotary rotary = {};              // FS_ROTARY
 };
 
 int dtype_bytes(int32_t dt);
@@ -247,6 +250,7 @@ fs_status check_execute_args(const fs_plan* p, const void* const* inputs, void* 
 size_t launches_issued(const fs_plan* p, size_t n_launches);
 fs_status complete_plan(fs_plan* p);
 int64_t graph_bytes_min(const fs_graph& g);
+RotaryAngles rotary_angles(const fs_attr_rotary& r);
 // Whether a kernel whose inputs are that large reads them past the caches (with the streaming hint) or through them.
 bool streams_inputs(const fs_graph& g);
 // How a launch reads its row inputs: 1 past the caches, 0 through them, -1 where its kernel has one form.

@@ -541,6 +541,9 @@ int64_t fs_plan_describe(const fs_plan* p, char* text, size_t capacity) try {
       s += "  rscal " + buf_name(l.ptr[kSlotRscal + i]) + " sreg " + std::to_string(q.rscal_sreg[i]) + " " + dtype_name(q.rscal_dt[i]) +
            (((q.rscal_bcast >> i) & 1u) ? " rowstrides=" + std::to_string(q.rms[i][0]) + "," + std::to_string(q.rms[i][1]) + "," +
                                               std::to_string(q.rms[i][2]) : std::string()) + "\n";
+    for (int i = 0; i < q.n_drops; ++i)
+      s += "  drop " + std::to_string(i) + " state " + buf_name(l.ptr[kSlotRscal + q.n_rscal + q.drop_state[i]]) + " threshold " +
+           std::to_string(q.drop_threshold[i]) + " sequence " + std::to_string(q.drop_sequence[i]) + "\n";
     for (int i = 0; i < kProgMaxOperands; ++i)
       if (l.ptr[kSlotOut + i].kind != BUF_NONE)
         s += "  output " + std::to_string(i) + " " + buf_name(l.ptr[kSlotOut + i]) +
@@ -558,7 +561,7 @@ int64_t fs_plan_describe(const fs_plan* p, char* text, size_t capacity) try {
            (q.col_kept > 0 ? ", the first " + std::to_string(q.col_kept + q.col_lds) + " kept in registers" : std::string()) +
            (q.col_lds > 0 ? " and LDS (" + std::to_string(q.col_kept) + " + " + std::to_string(q.col_lds) + ")" : std::string()) + "\n";
     static const char* op_names[] = {"add", "sub", "rsub", "mul", "div", "rdiv", "max", "square", "exp", "rsqrt", "tanh", "gelu",
-                                     "gelu_grad", "log", "sigmoid", "relu", "abs", "sqrt", "cvt", "load", "rsum", "rmax", "rsumsq", "store", "store_scal", "colsum"};
+                                     "gelu_grad", "log", "sigmoid", "relu", "abs", "sqrt", "cvt", "load", "rsum", "rmax", "rsumsq", "store", "store_scal", "colsum", "dropout"};
     static const char* kind_names[] = {"acc", "sacc", "reg", "scal", "imm", "col"};
     for (int i = 0; i < q.n_instr; ++i) {
       const ProgInstr& in = q.instr[i];

@@ -43,6 +43,8 @@ struct Compiler {
   uint32_t rows = 0, cols = 0;
   RowProgP p{};
   std::vector<int32_t> full_in, col_in, rscal_in;   // tensor ids by class (a transposed view of an input: the transpose's result)
+  std::vector<int32_t> state_in;                    // states of dropouts: in no class, read only by them
+  std::vector<int> drop_of;                         // per op: its entry among the program's dropouts, else -1
   // Transposes that keep the innermost axis only renumber rows.  One applied to a graph input is folded into
   // that input's addressing (the view is then an input of the row program, read with permuted row strides); one
   // that produces a graph output nobody else reads is folded into the store.
@@ -159,6 +161,7 @@ struct Compiler {
       ++scal_instr;
     } else {
       ++vec_instr;
+      if (ins.op == PO_DROPOUT) vec_instr += 17;   // 20 products (a quarter of the rate) and 40 other instructions for eight elements, 3 for each
       if (ins.op != PO_STORE && (ins.b_kind == PK_REG || ins.b_kind == PK_COL) &&
           (ins.op <= PO_MAX || ins.op == PO_LOAD)) ++reg_reads;
       if (ins.flags & PF_KEEP) ++reg_writes;
@@ -298,6 +301,7 @@ struct Compiler {
           case FS_ABS: ins.op = PO_ABS; break;
           case FS_SQRT: ins.op = PO_SQRT; break;
           case FS_CONVERT: ins.op = PO_CVT; ins.aux = (uint8_t)op.to_dtype; break;
+          case FS_DROPOUT: ins.op = PO_DROPOUT; ins.b = (uint8_t)drop_of[i]; break;
           case FS_REDUCE_SUM: case FS_REDUCE_MEAN: ins.op = square_of[i] >= 0 ? PO_RSUMSQ : PO_RSUM; break;
           case FS_REDUCE_MAX: ins.op = PO_RMAX; break;
           default: return false;
@@ -404,7 +408,7 @@ struct Compiler {
     // anchor = the largest tensor of the row space
     int anchor = -1;
     for (size_t t = 0; t < n_tensors; ++t)
-      if (!skip_for_anchor[t] && (anchor < 0 || g.tensors[t].numel() > g.tensors[anchor].numel())) anchor = (int)t;
+      if (!skip_for_anchor[t] && g.tensors[t].dtype != FS_I32 && (anchor < 0 || g.tensors[t].numel() > g.tensors[anchor].numel())) anchor = (int)t;
     if (anchor < 0) return false;
     const Tensor& a = g.tensors[anchor];
     rank = a.rank;
@@ -420,8 +424,14 @@ struct Compiler {
     // classes of all tensors; inputs by class
     for (size_t t = 0; t < n_tensors; ++t) {
       const Tensor& T = g.tensors[t];
-      if (T.dtype == FS_I32) return false;
       val[t].root = (int)t;
+      if (T.dtype == FS_I32) {   // only the state of dropouts
+        if (T.producer >= 0 || T.consumers.empty()) return false;
+        for (int c : T.consumers)
+          if (g.ops[c].opcode != FS_DROPOUT) return false;
+        state_in.push_back((int32_t)t);
+        continue;
+      }
       if (skip_for_anchor[t]) {   // lives outside the row space: reached only through its view / its permuted store
         if (T.rank != rank) return false;
         val[t].kind = V_FULL;
@@ -440,7 +450,7 @@ struct Compiler {
     bool narrow = false;   // some vector input is 16 bits wide
     std::vector<int32_t> input_like_tensors;
     for (int t : g.inputs)
-      if (!skip_for_anchor[t]) input_like_tensors.push_back(t);
+      if (!skip_for_anchor[t] && g.tensors[t].dtype != FS_I32) input_like_tensors.push_back(t);
     for (size_t t = 0; t < n_tensors; ++t)
       if (view_src[t] >= 0) input_like_tensors.push_back((int32_t)t);
     for (int t : input_like_tensors) {
@@ -490,6 +500,7 @@ struct Compiler {
     is_alias.assign(n_ops, 0);
     view_fold.assign(n_ops, 0);
     is_colsum.assign(n_ops, 0);
+    drop_of.assign(n_ops, -1);
     for (size_t i = 0; i < n_ops; ++i) {
       const Op& op = g.ops[i];
       const Tensor& out = g.tensors[op.out];
@@ -505,6 +516,18 @@ struct Compiler {
         case FS_LOG: case FS_SIGMOID: case FS_RELU: case FS_ABS: case FS_SQRT:
           want = ka;
           break;
+        case FS_DROPOUT: {   // (what is kept goes by the tensor's own rows, which have to be the pattern's)
+          const Tensor& src = g.tensors[op.in[0]];
+          if (ka != V_FULL || classify(src) != V_FULL || stretched_rows(src) || src.dims[src.rank - 1] != dims[rank - 1]) return false;
+          if (p.n_drops >= kProgMaxOperands) return false;
+          drop_of[i] = p.n_drops;
+          p.drop_state[p.n_drops] = (uint8_t)(std::find(state_in.begin(), state_in.end(), op.in[1]) - state_in.begin());
+          p.drop_threshold[p.n_drops] = op.draw.threshold;
+          p.drop_sequence[p.n_drops] = op.draw.sequence;
+          p.drop_scale[p.n_drops++] = op.draw.scale;
+          want = V_FULL;
+          break;
+        }
         case FS_BROADCAST:
           is_alias[i] = 1;
           break;
@@ -567,7 +590,7 @@ struct Compiler {
       } else {
         if (val[op.out].kind != want) return false;
         reads[i].push_back(val[op.in[0]].root);
-        if (op.n_in > 1) reads[i].push_back(val[op.in[1]].root);
+        if (op.n_in > 1 && op.opcode != FS_DROPOUT) reads[i].push_back(val[op.in[1]].root);
       }
     }
     return true;
@@ -630,6 +653,8 @@ struct Compiler {
     p.n_full = (int32_t)full_in.size();
     p.n_col = (int32_t)col_in.size();
     p.n_rscal = (int32_t)rscal_in.size();
+    p.n_states = (int32_t)state_in.size();
+    if (p.n_rscal + p.n_states > kProgMaxOperands) return false;
     for (size_t i = 0; i < col_in.size(); ++i) {
       val[col_in[i]].input_index = (int)i;
       p.col_dt[i] = (uint8_t)g.tensors[col_in[i]].dtype;
@@ -699,7 +724,7 @@ struct Compiler {
     p.col_kept = 0;
     p.col_lds = 0;
     p.stream = streams_inputs(g) ? 1 : 0;
-    if (n_colsum > 0) interpretable = false;
+    if (n_colsum > 0 || p.n_drops > 0) interpretable = false;
     return n_out + n_rout + n_colsum == (int)g.outputs.size();
   }
 };
@@ -886,6 +911,7 @@ void fill_launch(const fs_graph& g, const Compiler& c, int vec, const Shape& s, 
   for (size_t i = 0; i < c.full_in.size(); ++i) l->ptr[kSlotFull + i] = in_ref(c.full_in[i]);
   for (size_t i = 0; i < c.col_in.size(); ++i) l->ptr[kSlotCol + i] = in_ref(c.col_in[i]);
   for (size_t i = 0; i < c.rscal_in.size(); ++i) l->ptr[kSlotRscal + i] = in_ref(c.rscal_in[i]);
+  for (size_t i = 0; i < c.state_in.size(); ++i) l->ptr[kSlotRscal + c.rscal_in.size() + i] = in_ref(c.state_in[i]);
   for (int i = 0; i < c.n_out; ++i) { l->ptr[kSlotOut + i].kind = BUF_OUTPUT; l->ptr[kSlotOut + i].slot = c.out_slot[i]; }
   for (int i = 0; i < c.n_rout; ++i) { l->ptr[kSlotRout + i].kind = BUF_OUTPUT; l->ptr[kSlotRout + i].slot = c.rout_slot[i]; }
   const uint32_t rows_per_block = (s.block ? 1 : 256 / s.L) * s.R;

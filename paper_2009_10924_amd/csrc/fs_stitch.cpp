@@ -34,6 +34,7 @@ std::string build_stitched(const fs_graph& g, std::vector<Candidate>* out, PackF
       {"layernorm_backward", build_layernorm_backward, false, false}, {"transpose", build_transpose, false, false},
       {"group_norm", build_group_norm, true, true}, {"group_norm_backward", build_group_norm_backward, true, true},
       {"checkpoint", build_checkpoint, true, true}, {"checkpoint_backward", build_checkpoint_backward, true, true},
+      {"dropout", build_dropout, false, false}, {"rmsnorm_8bit", build_rmsnorm_8bit, true, true}, {"rotary", build_rotary, false, true},
   };
   const bool has_8bit = holds_8bit(g);
   std::string recognised;

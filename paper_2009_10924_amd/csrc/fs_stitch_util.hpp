@@ -105,6 +105,9 @@ bool build_group_norm(const fs_graph& g, std::vector<Candidate>* out, PackForm* 
 bool build_group_norm_backward(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
 bool build_checkpoint(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
 bool build_checkpoint_backward(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
+bool build_dropout(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
+bool build_rmsnorm_8bit(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
+bool build_rotary(const fs_graph& g, std::vector<Candidate>* out, PackForm* pack);
 // What the checkpoint and group normalisation families match in common (fs_family_checkpoint.cpp): an activation of $Z; $DY times
 // the slope of one at $Z; the 8-bit output that is $V over its scale, and that scale, `maximum` being the pattern of the largest
 // |$V|.  On success the bindings are merged into *st.

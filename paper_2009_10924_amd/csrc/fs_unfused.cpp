@@ -1,6 +1,7 @@
 // Per-op baseline plan: one launch per op in graph order (two for a reduction over
 // a non-innermost axis), float32 intermediates in the caller's workspace.
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 
 #include "fs_internal.hpp"
@@ -63,6 +64,18 @@ uint32_t pow2_at_least(uint32_t v) {
 }
 
 }  // namespace
+
+RotaryAngles rotary_angles(const fs_attr_rotary& r) {
+  RotaryAngles a{};
+  a.log2_base = std::log2(r.base);
+  a.n_axes = (uint32_t)r.n_axes;
+  for (int k = 0; k < r.n_axes; ++k) a.pairs += (uint32_t)r.pairs[k];
+  uint32_t end = 0;
+  for (int k = 0; k < FS_MAX_RANK; ++k) a.end[k] = end = k < r.n_axes ? end + (uint32_t)r.pairs[k] : a.pairs;
+  a.restart = r.restart;
+  a.inverse = r.inverse;
+  return a;
+}
 
 fs_status build_unfused(const fs_graph& g, Candidate* out) {
   const int n_t = (int)g.tensors.size();
@@ -308,6 +321,40 @@ fs_status build_unfused(const fs_graph& g, Candidate* out) {
         l.shape.grid[0] = (uint32_t)((blocks + per_workgroup - 1) / per_workgroup);
       }
       moved += 2 * n_out * p.elem_bytes;
+    } else if (opc == FS_DROPOUT) {
+      Launch& l = add_launch(K_DROPOUT_OP);
+      DropoutP& p = l.args.u.dropout;
+      p = DropoutP{};
+      p.in_dt = dt[op.in[0]]; p.out_dt = dst_dt;
+      p.cols = (uint32_t)a.dims[a.rank - 1];
+      p.rows = (uint32_t)(n_out / p.cols);
+      p.div_groups.d = (p.cols + 7) / 8;
+      p.draw = op.draw;
+      l.ptr[0] = where[op.in[0]]; l.ptr[1] = where[op.in[1]]; l.ptr[2] = dst;
+      grid1d(l, (int64_t)p.rows * p.div_groups.d);
+      moved += n_out * (dtype_bytes(p.in_dt) + dtype_bytes(dst_dt));
+    } else if (opc == FS_ROTARY) {
+      Launch& l = add_launch(K_ROTARY_OP);
+      RotaryP& p = l.args.u.rotary;
+      p = RotaryP{};
+      p.in_dt = dt[op.in[0]]; p.out_dt = dst_dt;
+      p.interleaved = op.rotary.interleaved;
+      p.s.angles = rotary_angles(op.rotary);
+      p.s.dim = (uint32_t)a.dims[a.rank - 1];
+      p.rows = (uint32_t)(n_out / p.s.dim);
+      const Tensor& pos = g.tensors[op.in[1]];
+      uint32_t ext[3] = {1, 1, 1}, step = 1;
+      for (int k = 0; k < a.rank - 1; ++k) ext[3 - (a.rank - 1) + k] = (uint32_t)a.dims[k];
+      for (int k = 1; k < pos.rank; ++k) {
+        const uint32_t d = (uint32_t)pos.dims[pos.rank - 1 - k];
+        p.s.pos_stride[3 - k] = d == 1 ? 0 : step;
+        step *= d;
+      }
+      p.s.pos_div[0].d = ext[2];
+      p.s.pos_div[1].d = ext[1];
+      l.ptr[0] = where[op.in[0]]; l.ptr[1] = where[op.in[1]]; l.ptr[2] = dst;
+      grid1d(l, (int64_t)p.rows * (p.s.dim - p.s.angles.pairs));
+      moved += n_out * (dtype_bytes(p.in_dt) + dtype_bytes(dst_dt)) + pos.numel() * 4;
     } else {
       // unary family, convert included
       Launch& l = add_launch(K_UNARY);

@@ -18,7 +18,8 @@ const char* const kNames[K_COUNT] = {"unary", "binary", "reduce_row", "reduce_mi
                                      "bias_gelu_dbias", "colfold", "tchain_wave", "tchain_lds", "row_wave", "row_block",
                                      "row_program", "layernorm_bwd", "row_generated", "checkpoint_wave", "checkpoint_block",
                                      "checkpoint_long", "checkpoint_grad", "checkpoint_grad_sums",
-                                     "gn_slab", "gn_stats", "gn_join", "gn_apply", "gn_bwd_slab", "gn_bwd_sums", "gn_bwd_join", "gn_bwd_apply"};
+                                     "gn_slab", "gn_stats", "gn_join", "gn_apply", "gn_bwd_slab", "gn_bwd_sums", "gn_bwd_join", "gn_bwd_apply", "dropout_op", "rotary_op", "dropout", "rmsnorm8_wave",
+    "rmsnorm8_block", "rmsnorm8_long", "rotary"};
 long g_launches = 0;
 
 // what any launch must satisfy whatever the kernel: returns a hipError-like code (1 = invalid value)

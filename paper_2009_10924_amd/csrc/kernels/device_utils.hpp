@@ -239,6 +239,82 @@ __device__ __forceinline__ float gelu_grad(float z) {
   return __builtin_fmaf(z * s * (1.0f - s), d, s);
 }
 
+// ---- dropout: what is kept, from a counter ---------------------------------------------------------------------------
+// Philox4x32-10 (Salmon et al., 2011): ten rounds of two 32 x 32 -> 64 bit products whose halves are exchanged and mixed with a key that
+// grows by a constant.  Eight numbers of 16 bits per call, so eight neighbouring columns share one: 20 products and 40 other
+// instructions, which a kernel that streams 16-bit elements hides (16384 x 4096 bf16, x to y: 42.3 us with and without, 40 rounds 63;
+// the products as one 64-bit multiplication each, 72 us with separate high and low words).
+struct DropKey { uint32_t seed0, seed1, offset0, offset1; };
+__device__ __forceinline__ DropKey drop_key(const void* state) {
+  const uint32_t* s = static_cast<const uint32_t*>(state);
+  return DropKey{s[0], s[1], s[2], s[3]};
+}
+__device__ __forceinline__ void drop_words(const DropKey& key, uint32_t sequence, uint32_t group, uint32_t (&w)[4]) {
+  uint32_t c0 = group, c1 = sequence, c2 = key.offset0, c3 = key.offset1, k0 = key.seed0, k1 = key.seed1;
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const unsigned long long a = (unsigned long long)c0 * 0xD2511F53u, b = (unsigned long long)c2 * 0xCD9E8D57u;
+    c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+    c1 = (uint32_t)b;
+    c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+    c3 = (uint32_t)a;
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  w[0] = c0; w[1] = c1; w[2] = c2; w[3] = c3;
+}
+// The 16-bit numbers of VEC columns from column `col` on, two in a word; first_group: the row's first group of eight.
+// WHOLE: col is a multiple of VEC.
+template <int VEC, bool WHOLE>
+__device__ __forceinline__ void drop_numbers(const DropKey& key, uint32_t sequence, uint32_t first_group, uint32_t col, uint32_t (&n)[(VEC + 1) / 2]) {
+  uint32_t a[8];
+  const uint32_t group = first_group + (col >> 3), at = col & 7u;
+  {
+    uint32_t w[4];
+    drop_words(key, sequence, group, w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = w[i], a[4 + i] = 0u;
+  }
+  if constexpr (WHOLE && VEC == 8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n[i] = a[i];
+  } else if constexpr (WHOLE && VEC == 4) {
+    n[0] = at ? a[2] : a[0];
+    n[1] = at ? a[3] : a[1];
+  } else {
+    if (VEC > 1 && at + VEC > 8u) {
+      uint32_t w[4];
+      drop_words(key, sequence, group + 1u, w);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[4 + i] = w[i];
+    }
+    // down by `at` halves of a word, a power of two at a time
+#pragma unroll
+    for (int i = 0; i < 6; ++i) a[i] = (at & 4u) ? a[i + 2] : a[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) a[i] = (at & 2u) ? a[i + 1] : a[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = (at & 1u) ? (a[i] >> 16 | a[i + 1] << 16) : a[i];
+#pragma unroll
+    for (int i = 0; i < (VEC + 1) / 2; ++i) n[i] = a[i];
+  }
+}
+// v where its number is at least `threshold`, scaled, else 0 (whatever v is)
+template <int VEC>
+__device__ __forceinline__ void drop_apply(const uint32_t (&n)[(VEC + 1) / 2], uint32_t threshold, float scale, float (&v)[VEC]) {
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) {
+    const bool keep = (e & 1) ? n[e / 2] >= threshold << 16 : (n[e / 2] & 0xFFFFu) >= threshold;
+    v[e] = keep ? v[e] * scale : 0.0f;
+  }
+}
+template <int VEC, bool WHOLE>
+__device__ __forceinline__ void drop(const DropKey& key, uint32_t sequence, uint32_t threshold, float scale, uint32_t first_group, uint32_t col, float (&v)[VEC]) {
+  uint32_t n[(VEC + 1) / 2];
+  drop_numbers<VEC, WHOLE>(key, sequence, first_group, col, n);
+  drop_apply<VEC>(n, threshold, scale, v);
+}
+
 // ---- wave64 cross-lane all-reduce over aligned groups of L lanes (L power of two) ----
 // Steps inside a 16-lane DPP row use DPP operand modifiers (no LDS traffic); the
 // 32- and 64-lane steps use ds_bpermute.  Every lane of the group ends with the

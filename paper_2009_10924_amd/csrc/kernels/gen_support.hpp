@@ -382,6 +382,26 @@ struct GenRow {
     else return group_allreduce<OP>(r, (int)L);
   }
 
+  // Dropout of the row's values (see drop()).  Rows whose steps slide or lie on the tensor's grid may start them at any column.
+  __device__ __forceinline__ void dropout(float (&v)[KV], const DropKey& key, uint32_t sequence, uint32_t threshold, float scale) const {
+    constexpr uint32_t GROUPS = (ROW_STRIDE + 7u) / 8u;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float part[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) part[e] = v[k * VEC + e];
+      const uint32_t at = (uint32_t)((int)col0 + first_of(k));
+      if constexpr (TAIL == 0 && !ON_GRID) {
+        drop<VEC, true>(key, sequence, threshold, scale, row_c * GROUPS, at, part);
+      } else {
+        if (at % VEC == 0u) drop<VEC, true>(key, sequence, threshold, scale, row_c * GROUPS, at, part);
+        else drop<VEC, false>(key, sequence, threshold, scale, row_c * GROUPS, at, part);
+      }
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) v[k * VEC + e] = part[e];
+    }
+  }
+
   // ---- column sums over all rows (lane-group rows only) ----------------------------------------------------
   // the row's values join the lane's running sums; padding lanes, repeated elements and rows beyond the last add nothing
   __device__ __forceinline__ void colsum_add(const float (&v)[KV], float (&sum)[KV]) const {

@@ -129,10 +129,12 @@ inline GnShape gn_shape(const GroupNormP& p) {
                  p.eps, p.inv_count, p.inv_max, p.tiny};
 }
 
+inline uint32_t rms8_flags(const RmsNorm8P& p) { return (p.wide_gamma ? 1u : 0u) | (p.round_h ? 2u : 0u); }
+
 // ---- the launcher's side -------------------------------------------------------------------------------------------
 // Storage of one launch's arguments and their addresses, which is what hipLaunchKernel wants.
 struct ArgList {
-  alignas(8) char bytes[256];
+  alignas(8) char bytes[384];
   void* address[24];
   size_t n = 0, at = 0;
   template <typename T>
@@ -148,7 +150,7 @@ struct ArgList {
     add(rest...);
   }
 };
-static_assert(sizeof(TransposeP) + 2 * sizeof(void*) <= 256 && sizeof(BinaryP) + 3 * sizeof(void*) <= 256, "ArgList holds every kernel's arguments");
+static_assert(sizeof(TransposeP) + 2 * sizeof(void*) <= 384 && sizeof(BinaryP) + 3 * sizeof(void*) <= 384 && sizeof(RotaryP) + 5 * sizeof(void*) <= 384, "ArgList holds every kernel's arguments");
 // The arguments of `kernel`, as its definition lists them; false: a value that its word cannot hold (or a kernel that is not
 // launched this way).  Inlined into the launcher, where the list's places are constants.
 __attribute__((always_inline)) inline bool list_arguments(int32_t kernel, const KernelArgs& a, uint32_t grid, ArgList* l) {
@@ -243,6 +245,22 @@ __attribute__((always_inline)) inline bool list_arguments(int32_t kernel, const 
     case K_GN_BWD_SUMS: l->add(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], gn_shape(a.u.gn)); return true;
     case K_GN_BWD_JOIN: l->add(p[0], p[1], gn_shape(a.u.gn)); return true;
     case K_GN_BWD_APPLY: l->add(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], gn_shape(a.u.gn)); return true;
+    case K_DROPOUT_OP: case K_ROTARY_OP:
+      if (kernel == K_DROPOUT_OP) l->add(p[0], p[1], p[2], a.u.dropout);
+      else l->add(p[0], p[1], p[2], a.u.rotary);
+      return true;
+    case K_DROPOUT: {
+      const DropoutP& d = a.u.dropout;
+      l->add(p[0], p[1], p[2], p[3], p[4], d.rows, d.cols, d.draw.threshold, d.draw.sequence, d.draw.scale, d.div_groups.d, d.div_groups.m, d.div_groups.s);
+      return true;
+    }
+    case K_RMS8_WAVE: case K_RMS8_BLOCK: case K_RMS8_LONG: {
+      const RmsNorm8P& n = a.u.rms8;
+      l->add(p[0], p[1], p[3], n.rows, n.cols, p[2], p[4], p[5], p[6], p[7], p[8], p[9], n.lanes_log2, rms8_flags(n), n.eps, n.inv_cols, n.inv_max, n.tiny,
+             n.draw.threshold, n.draw.sequence, n.draw.scale);
+      return true;
+    }
+    case K_ROTARY: l->add(p[0], p[1], p[2], p[3], p[4], a.u.rotary.s); return true;
     default: return false;
   }
 }

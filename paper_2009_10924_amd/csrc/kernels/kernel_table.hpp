@@ -13,5 +13,8 @@ const void* rowops_kernel_symbol(int32_t kernel, const KernelArgs& a);
 const void* group_norm_kernel_symbol(int32_t kernel, const KernelArgs& a);
 const void* group_norm_backward_kernel_symbol(int32_t kernel, const KernelArgs& a);
 const void* checkpoint_kernel_symbol(int32_t kernel, const KernelArgs& a);
+const void* dropout_kernel_symbol(int32_t kernel, const KernelArgs& a);
+const void* rmsnorm8_kernel_symbol(int32_t kernel, const KernelArgs& a);
+const void* rotary_kernel_symbol(int32_t kernel, const KernelArgs& a);
 const void* rowprog_kernel_symbol(int32_t kernel, const KernelArgs& a);
 }  // namespace fs

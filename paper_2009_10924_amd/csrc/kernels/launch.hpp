@@ -60,6 +60,13 @@ enum KernelId : int32_t {
   K_GN_BWD_SUMS,       // p0 x or q, p1 mean or scales, p2 rstd, p3 gamma, p4 beta, p5 dy, p6 chunk sums [batch, chunks, 2, pitch], p7 chunk means [batch, chunks, G, 2]
   K_GN_BWD_JOIN,       // p0 chunk means, p1 group means [batch, G, 2]
   K_GN_BWD_APPLY,      // p0 x or q, p1 mean or scales, p2 rstd, p3 gamma, p4 beta, p5 dy, p6 dx, p7 chunk or group means, p8 chunk sums, p9 dbeta, p10 dgamma
+  K_DROPOUT_OP,        // per-op: p0 in, p1 state, p2 out
+  K_ROTARY_OP,         // per-op: p0 in, p1 positions, p2 out
+  K_DROPOUT,           // p0 x, p1 bias (or null), p2 residual or incoming gradient (or null), p3 state, p4 y
+  K_RMS8_WAVE,         // p0 x, p1 residual, p2 bias, p3 gamma, p4 state, p5 h, p6 n, p7 q, p8 scales, p9 reciprocal deviations (p1, p2, p4, p5, p6, p9: or null) : a lane group per row
+  K_RMS8_BLOCK,        // a workgroup per row
+  K_RMS8_LONG,         // a workgroup per row, which it reads twice
+  K_ROTARY,            // p0, p1 x (p1: or null), p2 positions, p3, p4 y
   K_COUNT
 };
 
@@ -67,6 +74,12 @@ enum KernelId : int32_t {
 // q = n (d == 1), else q = mulhi(n, m) >> s with m = floor(2^(32+s) / d) + 1, s = ceil(log2 d) - 1.
 struct FastDiv {
   uint32_t d, m, s;
+};
+
+// What a dropout draws (FS_DROPOUT): kept are elements whose 16-bit number is at least `threshold`.
+struct DropoutDraw {
+  uint32_t threshold, sequence;
+  float scale;
 };
 
 struct LaunchShape {
@@ -211,6 +224,60 @@ struct GroupNormP {
   uint32_t fold_blocks;             // K_GN_BWD_APPLY: workgroups that add up the chunks' sums
   float eps, inv_count, inv_max, tiny;   // inv_count = 1 / (positions * dim)
 };
+struct DropoutP {
+  int32_t in_dt, out_dt;            // K_DROPOUT: x, bias, the third operand and y are all of in_dt
+  int32_t act;                      // activation in front of the dropout, or (slope) the one whose slope the gradient is multiplied by
+  int32_t slope;                    // K_DROPOUT: 1: y = dropout(p2) * act'(x + bias), 0: y = dropout(act(x + bias)) + p2
+  uint32_t rows, cols;
+  FastDiv div_groups;               // groups of eight columns in a row
+  DropoutDraw draw;
+  int32_t has_other;                // p2 is there
+  int32_t stream;
+};
+struct RmsNorm8P {
+  int32_t dt;                       // x, residual, bias, h and n; gamma too unless wide_gamma
+  int32_t wide_gamma;               // 1: gamma is float32 beside a 16-bit dt
+  int32_t round_h;                  // 1: h is rounded to dt before the norm reads it
+  int32_t form;                     // 0: h = x, 1: x (+ bias) + residual, 2: dropout(x (+ bias)) + residual
+  uint32_t rows, cols;
+  float eps, inv_cols, inv_max, tiny;
+  DropoutDraw draw;
+  int32_t vec;                      // elements per access: a whole vector, or 1 for rows shorter than one
+  int32_t lanes_log2, vecs_per_lane;
+  int32_t stream;
+};
+// Which angle a pair is turned by: `end[a]` is the first pair behind axis a's (all pairs, for axes that are not there).
+struct RotaryAngles {
+  double log2_base;
+  uint32_t pairs, n_axes;
+  uint32_t end[4];
+  int32_t restart, inverse;
+};
+// A tensor's rows: (position axes, shared axes) -> element, as strides along the three leading axes.  Its rows at one position are
+// `shared` many, numbered along the axes that the positions stretch over.
+struct RotaryRows {
+  uint32_t shared;
+  FastDiv div[2];                   // by the shared extents of axes 2 and 1
+  uint32_t in_stride[3], out_stride[3];
+};
+struct RotaryShape {
+  RotaryAngles angles;
+  uint32_t dim, positions;          // last extent; rows of positions
+  FastDiv pos_div[2];               // by the positions' extents along axes 2 and 1
+  uint32_t pos_stride[3];           // rows of positions, along the leading axes
+  RotaryRows t[2];
+  uint32_t p_tile, h_tile;          // a workgroup's positions, and rows at each of them
+  FastDiv div_h_tiles, div_inner, div_units;
+  uint32_t p_inner;                 // 1: neighbouring rows of a workgroup are at neighbouring positions, 0: at the same
+  uint32_t rot_units;               // steps of a row that turn pairs; the others (up to div_units.d) copy
+};
+struct RotaryP {
+  int32_t in_dt, out_dt;            // K_ROTARY: the same
+  int32_t interleaved, vec, iter;   // iter: steps that a lane loads at once
+  int32_t stream;
+  uint32_t rows;                    // K_ROTARY_OP
+  RotaryShape s;
+};
 enum RowPattern : int32_t { ROW_SOFTMAX_BWD = 0, ROW_RMSNORM = 1 };
 struct RowP {
   int32_t pattern, dt;              // all row inputs and outputs share dt
@@ -263,9 +330,10 @@ enum ProgOp : uint8_t {
   PO_RSUM, PO_RMAX, PO_RSUMSQ,                            // row reduction of acc (RSUMSQ: of acc squared) -> sacc
   PO_STORE,                                               // acc -> full output `dst`, stored as dtype `aux`
   PO_STORE_SCAL,                                          // sacc -> per-row output `dst`, dtype `aux`
-  PO_COLSUM                                               // acc is added to column sum `dst` (the sum over all rows of the
+  PO_COLSUM,                                              // acc is added to column sum `dst` (the sum over all rows of the
                                                           // pattern; generated kernels only: partial sums per workgroup go
                                                           // to the workspace and a second launch folds them)
+  PO_DROPOUT                                              // acc dropped out by entry `b` of `drops` (generated kernels only)
 };
 // where operand b comes from
 enum ProgKind : uint8_t {
@@ -326,6 +394,10 @@ struct RowProgP {
                                        // pass (the later passes do not read them again)
   int32_t col_lds;                     // ... and the next col_lds of them in LDS
   int32_t stream;                      // generated kernels: 1 = row inputs are read past the caches (see streams_inputs)
+  int32_t n_states, n_drops;           // states of dropouts (their pointers follow the per-row inputs'), dropouts
+  uint8_t drop_state[kProgMaxOperands];
+  uint32_t drop_threshold[kProgMaxOperands], drop_sequence[kProgMaxOperands];
+  float drop_scale[kProgMaxOperands];
   ProgInstr instr[kProgMaxInstr];
 };
 // Floats between two column sums in a row of partial sums: whole quads, which the fold reads (the padding is never
@@ -355,6 +427,9 @@ struct KernelArgs {
     LnBwdP lnbwd;
     CheckpointP checkpoint;
     GroupNormP gn;
+    DropoutP dropout;
+    RmsNorm8P rms8;
+    RotaryP rotary;
     RowProgP prog;
   } u;
   KernelArgs() { u.binary = BinaryP{}; }

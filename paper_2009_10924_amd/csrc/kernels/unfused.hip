@@ -8,6 +8,7 @@
 #include "device_utils.hpp"
 #include "e4m3.hpp"
 #include "kernel_table.hpp"
+#include "rotary.hpp"
 
 namespace fsk {
 using namespace fs;
@@ -369,6 +370,58 @@ __global__ void __launch_bounds__(256) k_transpose_units2(const T* __restrict__ 
   transpose_units<T, UQ, STREAM, UNITS, true>(in, out, p);
 }
 
+// ---- dropout: a thread draws for a group of eight columns -------------------------------------------
+__global__ void __launch_bounds__(256) k_dropout_op(const void* in, const void* state, void* out, DropoutP p) {
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x, groups = p.div_groups.d;
+  const uint32_t row = i / groups, col = (i - row * groups) * 8u;
+  if (row >= p.rows) return;
+  uint32_t n[4];
+  drop_numbers<8, true>(drop_key(state), p.draw.sequence, row * groups, col, n);
+  const uint32_t at = row * p.cols + col, here = min(8u, p.cols - col);
+  float v[8];
+  if (p.cols % 8u == 0u) {
+    load_rt<8>(in, p.in_dt, at, v);
+    drop_apply<8>(n, p.draw.threshold, p.draw.scale, v);
+    store_rt<8>(out, p.out_dt, at, v);
+    return;
+  }
+#pragma unroll
+  for (uint32_t e = 0; e < 8u; ++e) v[e] = e < here ? load_rt1(in, p.in_dt, at + e) : 0.0f;
+  drop_apply<8>(n, p.draw.threshold, p.draw.scale, v);
+#pragma unroll
+  for (uint32_t e = 0; e < 8u; ++e)
+    if (e < here) {
+      const float one[1] = {v[e]};
+      store_rt<1>(out, p.out_dt, at + e, one);
+    }
+}
+
+// ---- rotary positions: a thread per pair, or per element behind the pairs --------------------------------
+__global__ void __launch_bounds__(256) k_rotary_op(const void* in, const int32_t* positions, void* out, RotaryP p) {
+  const RotaryShape& s = p.s;
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x, units = s.angles.pairs + (s.dim - 2u * s.angles.pairs);
+  const uint32_t row = i / units, u = i - row * units;
+  if (row >= p.rows) return;
+  const uint32_t at = row * s.dim;
+  if (u >= s.angles.pairs) {
+    const uint32_t e = at + s.angles.pairs + u;
+    const float one[1] = {load_rt1(in, p.in_dt, e)};
+    store_rt<1>(out, p.out_dt, e, one);
+    return;
+  }
+  // (the extents along the leading axes stand where the family's kernel has its divisors)
+  const uint32_t c2 = row % s.pos_div[0].d, rest = row / s.pos_div[0].d, c1 = rest % s.pos_div[1].d, c0 = rest / s.pos_div[1].d;
+  const uint32_t at_position = c0 * s.pos_stride[0] + c1 * s.pos_stride[1] + c2 * s.pos_stride[2];
+  const uint32_t axis = rotary_axis(s.angles, u);
+  float c, d;
+  rotary_turn(s.angles, u, axis, positions[(size_t)at_position * s.angles.n_axes + axis], c, d);
+  const uint32_t ea = at + (p.interleaved ? 2u * u : u), eb = p.interleaved ? ea + 1u : ea + s.angles.pairs;
+  const float a = load_rt1(in, p.in_dt, ea), b = load_rt1(in, p.in_dt, eb);
+  const float va[1] = {a * c - b * d}, vb[1] = {b * c + a * d};
+  store_rt<1>(out, p.out_dt, ea, va);
+  store_rt<1>(out, p.out_dt, eb, vb);
+}
+
 // ---- streaming copy (the measured HBM ceiling) ------------------------------------
 __global__ void __launch_bounds__(256) k_copy(const u32x4* __restrict__ src, u32x4* __restrict__ dst, UnaryP p) {
   const uint32_t n_vec = p.n;   // 128-bit vectors
@@ -423,6 +476,10 @@ const void* unfused_kernel_symbol(int32_t kernel, const KernelArgs& a) {
       return a.u.transpose.elem_bytes == 4 ? (const void*)k_transpose_tile<uint32_t> : (const void*)k_transpose_tile<uint16_t>;
     case K_COPY:
       return (const void*)k_copy;
+    case K_DROPOUT_OP:
+      return (const void*)k_dropout_op;
+    case K_ROTARY_OP:
+      return (const void*)k_rotary_op;
     default:
       return nullptr;
   }

@@ -1,0 +1,267 @@
+"""Dropout, the 8-bit norm and rotary positions without a GPU: what a graph refuses, which pattern and launches a plan gets, the
+oracle's own pins, and gradients against differences."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+import workloads as W
+from oracle import oracle as O
+from paper_2009_10924_amd import binding as B
+from workloads.graphs import GraphSpec, OpSpec, TensorSpec, _softmax_ops
+
+
+# ---- the oracle ------------------------------------------------------------------------------------------------------
+def test_generator_against_its_published_answers():
+    """Known answers of Philox4x32-10 as its authors publish them, for counters and keys of zeros and of ones."""
+    zeros, ones = O.philox_words(np.zeros((1, 4)), (0, 0)), O.philox_words(np.full((1, 4), 0xFFFFFFFF), (0xFFFFFFFF, 0xFFFFFFFF))
+    assert [int(w) for w in zeros[0]] == [0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8]
+    assert [int(w) for w in ones[0]] == [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]
+    pi = O.philox_words(np.array([[0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344]]), (0xA4093822, 0x299F31D0))
+    assert [int(w) for w in pi[0]] == [0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1]
+
+
+def test_a_dropout_by_hand():
+    """Element (1, 9) of rows of 11: group 1 * 2 + 1, place 1: the high half of the group's first word."""
+    state = np.array([5, -6, 7, -8], np.int32)
+    kept, threshold = O.dropout_kept((3, 11), state, 0.3, sequence=4)
+    word = int(O.philox_words(np.array([[3, 4, 7, (1 << 32) - 8]]), (5, (1 << 32) - 6))[0, 0])
+    assert threshold == 19661 and bool(kept[1, 9]) == (word >> 16 >= threshold) and bool(kept[1, 8]) == (word & 0xFFFF >= threshold)
+    x = np.arange(1.0, 34.0).reshape(3, 11)
+    y = O.op_dropout(x, state, 0.3, 4)
+    assert np.array_equal(y != 0, kept) and np.allclose(y[kept], x[kept] * 65536 / (65536 - 19661), rtol=1e-7)
+
+
+def test_kept_share_and_independence():
+    state = np.array([1, 2, 3, 4], np.int32)
+    n = 512 * 512
+    for p in (0.1, 0.5, 0.9):
+        kept, t = O.dropout_kept((512, 512), state, p)
+        q = t / 65536
+        assert abs(kept.sum() - n * (1 - q)) < 6 * math.sqrt(n * q * (1 - q))
+        for shift in ((1, 0), (0, 1), (0, 8)):   # neighbours are kept independently of each other
+            both = (kept & np.roll(kept, shift, (0, 1))).sum()
+            assert abs(both - n * (1 - q) ** 2) < 8 * math.sqrt(n) * 0.5
+
+
+def test_a_rotation_by_hand():
+    """Position 3 turns pair 0 by 3 and pair 1 by 3 / sqrt(base) radians."""
+    x = np.array([[1.0, 2.0, 3.0, 4.0, 5.0]])
+    y = O.op_rotary(x, np.array([[3]]), 16.0, (2,))
+    c0, s0, c1, s1 = math.cos(3.0), math.sin(3.0), math.cos(0.75), math.sin(0.75)
+    assert np.allclose(y, [[1 * c0 - 3 * s0, 2 * c1 - 4 * s1, 3 * c0 + 1 * s0, 4 * c1 + 2 * s1, 5.0]], rtol=1e-14)
+    y = O.op_rotary(x, np.array([[3]]), 16.0, (2,), interleaved=True)
+    assert np.allclose(y, [[1 * c0 - 2 * s0, 2 * c0 + 1 * s0, 3 * c1 - 4 * s1, 4 * c1 + 3 * s1, 5.0]], rtol=1e-14)
+
+
+def test_axes_and_ladders():
+    """Two axes of one and two pairs: shared exponents 0, 1/3, 2/3; restarted ones 0 | 0, 1/2."""
+    x, pos = np.zeros((1, 6)), np.array([[2, 5]])
+    x[0, :3] = 1.0
+    for restart, powers in ((False, (0.0, 1 / 3, 2 / 3)), (True, (0.0, 0.0, 0.5))):
+        angles = [p * 100.0 ** -e for p, e in zip((2, 5, 5), powers)]
+        y = O.op_rotary(x, pos, 100.0, (1, 2), restart=restart)
+        assert np.allclose(y, [[math.cos(a) for a in angles] + [math.sin(a) for a in angles]], rtol=1e-13)
+        assert np.allclose(O.op_rotary(y, pos, 100.0, (1, 2), restart=restart, inverse=True), x, atol=1e-15)
+
+
+def _loss(spec, inputs, weights):
+    out = O.evaluate(spec, inputs)
+    return sum(float((out[n] * w).sum()) for n, w in weights.items())
+
+
+def _difference(spec, inputs, name, weights, at, step=1e-4):
+    a, b = ({k: v.copy() for k, v in inputs.items()} for _ in range(2))
+    a[name] = a[name].astype(np.float64)
+    b[name] = b[name].astype(np.float64)
+    a[name][at] += step
+    b[name][at] -= step
+    wide = GraphSpec(spec.name, [TensorSpec(t.name, t.dtype, t.dims) for t in spec.inputs], spec.ops, spec.outputs)
+    keep = O.to_f64
+    O.to_f64 = lambda v, dt: v if v.dtype == np.float64 else keep(v, dt)   # (inputs that are no float32 numbers)
+    try:
+        return (_loss(wide, a, weights) - _loss(wide, b, weights)) / (2 * step)
+    finally:
+        O.to_f64 = keep
+
+
+@pytest.mark.parametrize("act", ["none", "gelu", "silu"])
+def test_dropout_gradient_against_differences(act):
+    rows, cols = 6, 21
+    forward = W.dropout_graph(rows, cols, 0.3, dtype="f32", act=act, bias=True, sequence=5)
+    backward = W.dropout_backward_graph(rows, cols, 0.3, dtype="f32", act=act, bias=act != "none", sequence=5)
+    inputs = W.make_inputs(forward, 1)
+    dy = np.random.default_rng(2).standard_normal((rows, cols)).astype(np.float32)
+    given = {"dy": dy, "state": inputs["state"], "x": inputs["x"], "bias": inputs["bias"]}
+    got = O.evaluate(backward, {t.name: given[t.name] for t in backward.inputs})
+    dx, dbias = got[backward.outputs[0][0]], got["dbias"]
+    weights = {"d": dy.astype(np.float64)}
+    for at in ((0, 0), (2, 20), (5, 8), (3, 15), (4, 4)):
+        assert abs(_difference(forward, inputs, "x", weights, at) - dx[at]) < 1e-6
+    for c in (0, 13, 20):
+        assert abs(_difference(forward, inputs, "bias", weights, (c,)) - dbias[0, c]) < 1e-5
+
+
+def test_block_border_gradient_against_differences():
+    rows, cols, p = 3, 24, 0.25
+    forward = W.rmsnorm_8bit_graph(rows, cols, dtype="f32", p=p, keep="stats", normed=True, eps=1e-2)
+    forward = GraphSpec(forward.name, forward.inputs, [o for o in forward.ops if not (o.out.startswith("q") or o.out == "s")],
+                        [("h", "f32"), ("n", "f32"), ("r", "f32")])
+    backward = W.rmsnorm_residual_backward_graph(rows, cols, dtype="f32", p=p)
+    inputs = W.make_inputs(forward, 3)
+    env = O.evaluate(forward, inputs, keep_all=True)
+    g = np.random.default_rng(4)
+    dn, dres = g.standard_normal((rows, cols)), g.standard_normal((rows, cols))
+    keep = O.to_f64
+    O.to_f64 = lambda v, dt: v if v.dtype == np.float64 else keep(v, dt)
+    try:
+        got = O.evaluate(backward, {"dn": dn, "h": env["h"], "r": env["r"], "gamma": inputs["gamma"], "dres": dres, "state": inputs["state"]})
+    finally:
+        O.to_f64 = keep
+    weights = {"n": dn, "h": dres}   # h goes on as the residual stream, its gradient there is dres
+    for at in ((0, 0), (1, 23), (2, 9)):
+        assert abs(_difference(forward, inputs, "res", weights, at) - got["dh"][at]) < 1e-6
+        assert abs(_difference(forward, inputs, "x", weights, at) - got["dx"][at]) < 1e-6
+    for c in (0, 11, 23):
+        assert abs(_difference(forward, inputs, "gamma", weights, (c,)) - got["dgamma"][0, c]) < 1e-6
+
+
+def test_rotary_gradient_against_differences():
+    forward = W.rotary_graph(1, 3, (2,), 12, (2, 3), dtype="f32", interleaved=True, restart=True)
+    backward = W.rotary_graph(1, 3, (2,), 12, (2, 3), dtype="f32", interleaved=True, restart=True, inverse=True)
+    inputs = W.make_inputs(forward, 1)
+    dy = np.random.default_rng(2).standard_normal((1, 3, 2, 12)).astype(np.float32)
+    dx = O.evaluate(backward, {"q": dy, "positions": inputs["positions"]})["qr"]
+    for at in ((0, 0, 0, 0), (0, 1, 1, 5), (0, 2, 0, 9), (0, 2, 1, 11)):
+        assert abs(_difference(forward, inputs, "q", {"qr": dy.astype(np.float64)}, at) - dx[at]) < 1e-7
+
+
+# ---- refusals --------------------------------------------------------------------------------------------------------
+def _code(call):
+    with pytest.raises(B.FsError) as e:
+        call()
+    return e.value.code
+
+
+def test_dropout_refusals():
+    g = B.Graph()
+    x, state, wide, floats = g.input("f32", (4, 8)), g.input("i32", (4,)), g.input("i32", (1, 4)), g.input("f32", (4,))
+    for p in (-0.1, 1.0, 65535.5 / 65536, float("nan"), float("inf"), 2.0):
+        assert _code(lambda: g.op("dropout", (x, state), probability=p)) == -1
+    assert _code(lambda: g.op("dropout", (x, wide), probability=0.1)) == -2
+    assert _code(lambda: g.op("dropout", (x, floats), probability=0.1)) == -3
+    assert _code(lambda: g.op("dropout", (state, state), probability=0.1)) == -3
+    assert _code(lambda: g.op("dropout", (x,), probability=0.1)) == -1
+    assert _code(lambda: g.op("dropout", (x, 99), probability=0.1)) == -4
+    assert _code(lambda: g.op("add", (x, state))) == -3
+    moved = g.op("transpose", (state,), perm=(0,))
+    assert _code(lambda: g.op("dropout", (x, moved), probability=0.1)) == -2   # a state is a graph input
+    lib, ins = B.load(), (C.c_int32 * 2)(x, state)
+    a = B.fs_attr_dropout(0.1, 0, 1)
+    assert lib.fs_graph_op(g.handle, 24, 2, ins, C.cast(C.byref(a), C.c_void_p), C.sizeof(a)) == -1   # the reserved field
+    assert lib.fs_graph_op(g.handle, 24, 2, ins, C.cast(C.byref(a), C.c_void_p), 8) == -1             # half an attribute
+    assert lib.fs_graph_op(g.handle, 24, 2, ins, None, 0) == -1
+    assert lib.fs_graph_op(g.handle, 26, 2, ins, None, 0) == -1                                       # behind the last opcode
+    assert g.op("dropout", (x, state), probability=65535.4 / 65536) >= 0
+
+
+def test_rotary_refusals():
+    g = B.Graph()
+    x, pos = g.input("f32", (2, 3, 4, 16)), g.input("i32", (2, 3, 1, 2))
+    good = dict(base=100.0, pairs=(3, 5))
+    for bad in (dict(base=0.5), dict(base=float("nan")), dict(base=1e31), dict(pairs=(3, 0)), dict(pairs=(4, 5)), dict(pairs=(-1, 5)),
+                dict(interleaved=2), dict(restart=-1), dict(inverse=3)):
+        assert _code(lambda: g.op("rotary", (x, pos), **{**good, **bad})) == -1, bad
+    assert _code(lambda: g.op("rotary", (x, pos), base=100.0, pairs=(8,))) == -2        # two axes in the tensor, one in the attribute
+    for dims in ((2, 3, 4, 3), (3, 3, 1, 2), (2, 2, 1, 2), (3, 2), (1, 2, 3, 4)[:3]):
+        p = g.input("i32", dims)
+        assert _code(lambda: g.op("rotary", (x, p), **good)) == -2, dims
+    assert _code(lambda: g.op("rotary", (x, x), **good)) == -3
+    wide = g.input("f32", (1, 9000))
+    p = g.input("i32", (1, 1))
+    assert _code(lambda: g.op("rotary", (wide, p), base=100.0, pairs=(4097,))) == -1
+    lib, ins = B.load(), (C.c_int32 * 2)(x, pos)
+    a = B.fs_attr_rotary(100.0, 5, (C.c_int32 * 4)(1, 1, 1, 1), 0, 0, 0)
+    assert lib.fs_graph_op(g.handle, 25, 2, ins, C.cast(C.byref(a), C.c_void_p), C.sizeof(a)) == -1
+    for dims in ((2,), (4, 2), (3, 1, 2), (1, 1, 1, 2), (2, 3, 4, 2)):
+        assert g.op("rotary", (x, g.input("i32", dims)), **good) >= 0
+
+
+def test_what_has_no_transpose_or_integer_output():
+    g = B.Graph()
+    x, state = g.input("f32", (4, 8)), g.input("i32", (4,))
+    d = g.op("dropout", (x, state), probability=0.1)
+    assert _code(lambda: g.output(d, "i32")) == -3
+
+
+# ---- plans -----------------------------------------------------------------------------------------------------------
+def _plan(spec, **opts):
+    return B.Plan(B.Graph.from_spec(spec), **opts)
+
+
+def test_patterns_and_their_kernels():
+    for spec, pattern, kernel in (
+            (W.dropout_graph(64, 128), "dropout", "dropout<bf16,none>"),
+            (W.dropout_graph(64, 130, act="silu", bias=True, residual=True), "dropout", "dropout<bf16,silu,ragged>"),
+            (W.dropout_backward_graph(64, 128, act="gelu", bias=True, dbias=False), "dropout", "dropout<bf16,gelu,slope>"),
+            (W.rmsnorm_8bit_graph(64, 1024), "rmsnorm_8bit", "rmsnorm8_wave<bf16,residual"),
+            (W.rmsnorm_8bit_graph(64, 1024, residual=False), "rmsnorm_8bit", "rmsnorm8_wave<bf16,plain"),
+            (W.rmsnorm_8bit_graph(64, 1024, p=0.1, bias=True, rounded=True, normed=True, keep="stats"), "rmsnorm_8bit", "rmsnorm8_wave<bf16,dropout"),
+            (W.rotary_graph(2, 64, (8, 2), 128, (64,)), "rotary", "rotary<bf16,halves,v8"),
+            (W.rotary_graph(2, 64, (8, 2), 128, (16, 24, 24), split=True, interleaved=True), "rotary", "rotary<bf16,interleaved,v8"),
+            (W.rotary_graph(2, 64, (8,), 128, (16, 24, 24), split=True, inverse=True, dtype="f32"), "rotary", "rotary<f32,halves,v4"),
+            (W.rotary_graph(2, 64, (8,), 6, (3,)), "rotary", "rotary<bf16,halves,v1")):
+        info = _plan(spec).info
+        assert info["pattern"] == pattern and info["kernel"].startswith(kernel) and info["n_kernels"] == 1 and info["workspace_bytes"] == 0, info
+
+
+def test_what_is_another_pattern():
+    """A residual that is another tensor's shape, two states, outputs that the family does not hand out: per op or a row program."""
+    spec = W.dropout_graph(64, 128, residual=True)
+    spec.inputs[-1] = TensorSpec("res", "bf16", (128,))
+    assert _plan(spec).info["pattern"] != "dropout"
+    spec = W.rmsnorm_8bit_graph(64, 128)
+    spec.outputs.append(("hr", "f32"))
+    assert _plan(spec).info["pattern"] == "unfused"
+    spec = W.rmsnorm_8bit_graph(64, 128, gain_dtype="f16")
+    assert _plan(spec).info["pattern"] == "unfused"
+    spec = W.rotary_graph(2, 64, (8, 2), 128, (64,))
+    spec.ops[1] = OpSpec("kr", "rotary", spec.ops[1].inputs, {**spec.ops[1].attr, "base": 500.0})
+    assert _plan(spec).info["pattern"] == "unfused"
+    spec = W.rotary_graph(2, 64, (8,), 128, (64,), split=True)
+    spec.ops[-1] = OpSpec("qs", "transpose", spec.ops[-1].inputs, {"perm": (0, 2, 3, 1)})
+    assert _plan(spec).info["pattern"] == "unfused"
+
+
+@pytest.mark.skipif(not B.codegen_available(), reason="needs the run-time compiler")
+def test_a_dropout_joins_row_programs():
+    spec = GraphSpec("pattern_x", [TensorSpec("x", "f16", (6, 64)), TensorSpec("state", "i32", (4,))],
+                     _softmax_ops("x", 1) + [OpSpec("d", "dropout", ("y", "state"), {"probability": 0.1, "sequence": 3})], [("d", "f16")])
+    plan = _plan(spec)
+    assert plan.info["kernel"].startswith("row_generated") and "drop 0 state in1 threshold 6554 sequence 3" in plan.describe()
+    assert "row.dropout(acc, drop0, 3u, 6554u" in plan.source()
+    with B.codegen(False):   # the interpreter has no generator: op by op
+        assert _plan(spec).info["pattern"] == "unfused"
+        assert _plan(W.dropout_graph(64, 128)).info["pattern"] == "dropout"
+
+
+def test_a_program_keeps_the_attributes():
+    """The explorer's sub-graphs draw and turn as the whole graph says."""
+    spec = W.decoder_block_graph(batch=2, seq=16, heads=4, kv_heads=2, dim=32, ffn=64, sections=(4, 6, 6))
+    patterns = B.Program(B.Graph.from_spec(spec)).patterns()
+    covered = sorted(o for p in patterns for o in p["ops"])
+    assert covered == list(range(len(spec.ops)))
+    kinds = [p["info"]["pattern"] for p in patterns]
+    assert kinds.count("rmsnorm_8bit") == 2 and kinds.count("rotary") == 1 and kinds.count("dropout") == 1
+
+
+def test_sizes_up_to_the_largest():
+    """Plans at the borders of 31 bits: launches stay within 32 bits of threads, every form has a plan."""
+    for spec in (W.dropout_graph((1 << 31) - 1, 1, dtype="f32"), W.dropout_graph(1, (1 << 31) - 1, dtype="bf16"), W.dropout_graph(2, (1 << 30) - 1, dtype="f16"),
+                 W.rmsnorm_8bit_graph((1 << 31) - 1, 1, dtype="f32", residual=False), W.rmsnorm_8bit_graph(1, (1 << 31) - 1, residual=False),
+                 W.rotary_graph(1, (1 << 30) - 1, (1,), 2, (1,), dtype="f32"), W.rotary_graph(1, 1, ((1 << 30) - 1,), 2, (1,), dtype="f32"),
+                 W.rotary_graph(1, 1, (1,), (1 << 31) - 1, (4096,), dtype="bf16")):
+        for scheme in ("auto", "unfused"):
+            info = _plan(spec, scheme=scheme).info
+            assert info["grid"][0] * info["block"][0] < 1 << 32, (spec.name, scheme, info)

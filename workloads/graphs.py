@@ -32,6 +32,7 @@ OPCODES = {
     "broadcast": 1,
     "reduce_sum": 1, "reduce_max": 1, "reduce_mean": 1,
     "transpose": 1, "convert": 1,
+    "dropout": 2, "rotary": 2,   # the second operand: a state / positions, in 32-bit integers
 }
 
 
@@ -431,6 +432,171 @@ NEXT_CONFIGS = {
 }
 
 # ---- row-local patterns no hand-written kernel family covers (served by the row-program compiler: generated kernel or interpreter) ----
+# ---- dropout, the norm behind a residual connection, rotary positions -----------------------------------------------------
+RMS_EPS = 1e-6
+
+
+def _state() -> TensorSpec:
+    """Seed and offset of a dropout, 64 bits each, low words first."""
+    return TensorSpec("state", "i32", (4,))
+
+
+def dropout_graph(rows: int, cols: int, p: float = 0.1, dtype: str = "bf16", act: str = "none", bias: bool = False, residual: bool = False,
+                  sequence: int = 0) -> GraphSpec:
+    """y = dropout(act(x + bias)) + res, each of bias, activation and residual where it is asked for."""
+    full, ops, z = (rows, cols), [], "x"
+    inputs = [TensorSpec("x", dtype, full)]
+    if bias:
+        inputs.append(TensorSpec("bias", dtype, (cols,)))
+        ops.append(_op("z", "add", "x", "bias"))
+        z = "z"
+    if act != "none":
+        ops += _act_ops(act, z, "a")
+        z = "a"
+    inputs.append(_state())
+    ops.append(_op("d", "dropout", z, "state", probability=p, sequence=sequence))
+    if residual:
+        inputs.append(TensorSpec("res", dtype, full))
+        ops.append(_op("y", "add", "d", "res"))
+    return GraphSpec(name=f"pattern_dropout_{dtype}_{act}_{int(bias)}{int(residual)}_{rows}x{cols}", inputs=inputs, ops=ops,
+                     outputs=[("y" if residual else "d", dtype)])
+
+
+def dropout_backward_graph(rows: int, cols: int, p: float = 0.1, dtype: str = "bf16", act: str = "gelu", bias: bool = False, dbias: bool = True,
+                           sequence: int = 0) -> GraphSpec:
+    """dx = dropout(dy) * act'(x + bias) and, if asked for, the bias gradient, dx summed over all rows."""
+    full = (rows, cols)
+    inputs, ops = [TensorSpec("dy", dtype, full), _state()], [_op("g", "dropout", "dy", "state", probability=p, sequence=sequence)]
+    dx = "g"
+    if act != "none":
+        z = "x"
+        inputs.append(TensorSpec("x", dtype, full))
+        if bias:
+            inputs.append(TensorSpec("bias", dtype, (cols,)))
+            ops.append(_op("z", "add", "x", "bias"))
+            z = "z"
+        ops += [*_act_grad_ops(act, z, "da"), _op("dx", "mul", "g", "da")]
+        dx = "dx"
+    outputs = [(dx, dtype)]
+    if dbias:
+        ops.append(_op("dbias", "reduce_sum", dx, axis=0))
+        outputs.append(("dbias", "f32"))
+    return GraphSpec(name=f"pattern_dropout_backward_{dtype}_{act}_{int(bias)}{int(dbias)}_{rows}x{cols}", inputs=inputs, ops=ops, outputs=outputs)
+
+
+def _residual_norm_ops(x: str, gamma: str, prefix: str = "", bias: str = "", res: str = "", state: str = "", p: float = 0.0, sequence: int = 0,
+                       eps: float = RMS_EPS, round_to: str = "") -> List[OpSpec]:
+    """h = dropout(x + bias) + res (rounded to `round_to`, if given), r = 1 / rms(h), n = h r gamma, and n in 8 bits (q, s)."""
+    ops, h = [], x
+    if bias:
+        ops.append(_op(prefix + "z", "add", h, bias))
+        h = prefix + "z"
+    if p > 0.0:
+        ops.append(_op(prefix + "d", "dropout", h, state, probability=p, sequence=sequence))
+        h = prefix + "d"
+    if res:
+        ops.append(_op(prefix + ("h0" if round_to else "h"), "add", h, res))
+        h = prefix + "h"
+        if round_to:
+            ops.append(_op(h, "convert", prefix + "h0", dtype=round_to))
+    ops += [_op(prefix + "h2", "square", h), _op(prefix + "ms", "reduce_mean", prefix + "h2", axis=1),
+            _op(prefix + "ve", "add_scalar", prefix + "ms", value=float(eps)), _op(prefix + "r", "rsqrt", prefix + "ve"),
+            _op(prefix + "hr", "mul", h, prefix + "r"), _op(prefix + "n", "mul", prefix + "hr", gamma)]
+    return ops + [OpSpec(prefix + o.out, o.opcode, tuple(i if i == prefix + "n" else prefix + i for i in o.inputs), o.attr)
+                  for o in _store_8bit_ops(prefix + "n", (1,))]
+
+
+def rmsnorm_8bit_graph(rows: int, cols: int, dtype: str = "bf16", bias: bool = False, residual: bool = True, p: float = 0.0, keep: str = "none",
+                       eps: float = RMS_EPS, normed: bool = False, rounded: bool = False, gain_dtype: str = "", sequence: int = 0) -> GraphSpec:
+    """Root-mean-square norm behind a residual connection, its result in 8 bits with a scale per row: h = dropout(x + bias) + res
+    (bias, dropout and residual where they are asked for), n = h / rms(h) * gamma, q * s = n.  keep = "stats": the reciprocal
+    rms as well; normed: n too; rounded: h is rounded to the storage dtype before the norm reads it."""
+    full = (rows, cols)
+    inputs = [TensorSpec("x", dtype, full)]
+    if bias:
+        inputs.append(TensorSpec("bias", dtype, (cols,)))
+    if p > 0.0:
+        inputs.append(_state())
+    if residual:
+        inputs.append(TensorSpec("res", dtype, full))
+    inputs.append(TensorSpec("gamma", gain_dtype or dtype, (cols,)))
+    ops = _residual_norm_ops("x", "gamma", bias="bias" if bias else "", res="res" if residual else "", state="state", p=p, sequence=sequence, eps=eps,
+                             round_to=dtype if rounded and residual else "")
+    outputs = ([("h", dtype)] if residual else []) + [("q", "e4m3"), ("s", "f32")] + ([("r", "f32")] if keep == "stats" else []) + \
+        ([("n", dtype)] if normed else [])
+    return GraphSpec(name=f"pattern_rmsnorm_8bit_{dtype}_{int(bias)}{int(residual)}{int(p > 0)}_{keep}_{rows}x{cols}", inputs=inputs, ops=ops,
+                     outputs=outputs)
+
+
+def rmsnorm_residual_backward_graph(rows: int, cols: int, dtype: str = "bf16", p: float = 0.0, sequence: int = 0) -> GraphSpec:
+    """Backward of a block border: dn is the gradient of the norm's result, dres that of the residual stream behind it.  With the kept
+    h and r: dh = (g - nh mean(g nh)) r + dres, g = dn gamma, nh = h r; dgamma = sum of dn nh; the branch's gradient dx = dropout(dh)."""
+    full = (rows, cols)
+    inputs = [TensorSpec("dn", dtype, full), TensorSpec("h", dtype, full), TensorSpec("r", "f32", (rows, 1)), TensorSpec("gamma", dtype, (cols,)),
+              TensorSpec("dres", dtype, full)]
+    ops = [_op("nh", "mul", "h", "r"), _op("dnh", "mul", "dn", "nh"), _op("dgamma", "reduce_sum", "dnh", axis=0), _op("g", "mul", "dn", "gamma"),
+           _op("gn", "mul", "g", "nh"), _op("m", "reduce_mean", "gn", axis=1), _op("nm", "mul", "nh", "m"), _op("c", "sub", "g", "nm"),
+           _op("cr", "mul", "c", "r"), _op("dh", "add", "cr", "dres")]
+    outputs = [("dh", dtype), ("dgamma", "f32")]
+    if p > 0.0:
+        inputs.append(_state())
+        ops.append(_op("dx", "dropout", "dh", "state", probability=p, sequence=sequence))
+        outputs.append(("dx", dtype))
+    return GraphSpec(name=f"pattern_rmsnorm_residual_backward_{dtype}_{int(p > 0)}_{rows}x{cols}", inputs=inputs, ops=ops, outputs=outputs)
+
+
+def rotary_graph(batch: int, seq: int, heads: Sequence[int], dim: int, sections: Sequence[int], dtype: str = "bf16", base: float = 10000.0,
+                 interleaved: bool = False, restart: bool = False, inverse: bool = False, split: bool = False) -> GraphSpec:
+    """Rotary positions of queries and keys [batch, seq, heads[i], dim] (one tensor if `heads` has one entry), the first sections[0]
+    pairs by axis 0 of the positions, and so on.  split: the heads come out in front of the sequence ([batch, heads, seq, dim]);
+    with inverse, the gradient, they come in that way."""
+    attr = dict(base=float(base), pairs=tuple(sections), interleaved=interleaved, restart=restart, inverse=inverse)
+    inputs, ops, outputs = [], [], []
+    for n, h in zip("qk", heads):
+        src, res = n, n + "r"
+        if split and inverse:
+            inputs.append(TensorSpec(n, dtype, (batch, h, seq, dim)))
+            ops.append(_op(n + "t", "transpose", n, perm=(0, 2, 1, 3)))
+            src = n + "t"
+        else:
+            inputs.append(TensorSpec(n, dtype, (batch, seq, h, dim)))
+        ops.append(_op(res, "rotary", src, "positions", **attr))
+        if split and not inverse:
+            if dtype != "f32":
+                ops.append(_op(n + "c", "convert", res, dtype=dtype))
+                res = n + "c"
+            ops.append(_op(n + "s", "transpose", res, perm=(0, 2, 1, 3)))
+            res = n + "s"
+        outputs.append((res, dtype))
+    inputs.append(TensorSpec("positions", "i32", (batch, seq, 1, len(sections))))
+    return GraphSpec(name=f"pattern_rotary_{dtype}_{batch}x{seq}x{'_'.join(map(str, heads))}x{dim}", inputs=inputs, ops=ops, outputs=outputs)
+
+
+def decoder_block_graph(batch: int = 2, seq: int = 64, heads: int = 4, kv_heads: int = 2, dim: int = 16, ffn: int = 128, dtype: str = "bf16",
+                        p: float = 0.1, sections: Sequence[int] = (2, 3, 3), base: float = 10000.0) -> GraphSpec:
+    """The memory-intensive ops of one decoder block in training, its matrix products and its attention taken out (as in
+    transformer_block_graph): norm of the residual stream in 8 bits, rotary positions of queries and keys with the head split, attention
+    output through bias, dropout and residual into the second norm, gated SiLU with dropout, and the second branch's dropout and residual."""
+    hidden, rows = heads * dim, batch * seq
+    full = (rows, hidden)
+    attr = dict(base=float(base), pairs=tuple(sections))
+    inputs = [TensorSpec("x", dtype, full), TensorSpec("gamma1", dtype, (hidden,)), TensorSpec("q_lin", dtype, (batch, seq, heads, dim)),
+              TensorSpec("k_lin", dtype, (batch, seq, kv_heads, dim)), TensorSpec("positions", "i32", (batch, seq, 1, len(sections))),
+              TensorSpec("attn_out", dtype, full), TensorSpec("bias_o", dtype, (hidden,)), TensorSpec("gamma2", dtype, (hidden,)),
+              TensorSpec("gate", dtype, (rows, ffn)), TensorSpec("up", dtype, (rows, ffn)), TensorSpec("ffn_out", dtype, full), _state()]
+    ops = _residual_norm_ops("x", "gamma1", prefix="a_")
+    for n, h in (("q", heads), ("k", kv_heads)):
+        ops += [_op(n + "r", "rotary", n + "_lin", "positions", **attr), _op(n + "c", "convert", n + "r", dtype=dtype),
+                _op(n + "s", "transpose", n + "c", perm=(0, 2, 1, 3))]
+    ops += _residual_norm_ops("attn_out", "gamma2", prefix="b_", bias="bias_o", res="x", state="state", p=p, sequence=1, round_to=dtype)
+    ops += [*_act_ops("silu", "gate", "ga"), _op("gu", "mul", "ga", "up"), _op("gd", "dropout", "gu", "state", probability=p, sequence=2),
+            _op("fd", "dropout", "ffn_out", "state", probability=p, sequence=3), _op("y", "add", "fd", "b_h")]
+    outputs = [("a_q", "e4m3"), ("a_s", "f32"), ("a_r", "f32"), ("qs", dtype), ("ks", dtype), ("b_h", dtype), ("b_q", "e4m3"), ("b_s", "f32"), ("b_r", "f32"),
+               ("gd", dtype), ("y", dtype)]
+    external = [("a_q", "q_lin"), ("a_q", "k_lin"), ("qs", "attn_out"), ("ks", "attn_out"), ("b_q", "gate"), ("b_q", "up"), ("gd", "ffn_out")]
+    return GraphSpec(name=f"pattern_decoder_block_{dtype}_b{batch}_s{seq}", inputs=inputs, ops=ops, outputs=outputs, external=external)
+
+
 def layernorm_stats_graph(rows: int, cols: int, eps: float = 1e-5, in_dtype: str = "f32", out_dtype: str = "bf16",
                           with_variance: bool = False) -> GraphSpec:
     """Residual add + bias + LayerNorm that also hands out the per-row mean and reciprocal standard

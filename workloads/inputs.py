@@ -89,7 +89,8 @@ def make_inputs(graph: GraphSpec, seed: int = 0) -> Dict[str, np.ndarray]:
                          r ~ U(0.8,1.2); q ~ N(0,112), saturating; s ~ U(0.5,1.5)/112
       pattern (any other pattern or multi-pattern graph) by tensor name (a segment prefix s<k>_ is ignored):
                          g* ~ 1+N(0,0.02); r* ~ U(0.8,1.2); mu* ~ N(0,0.05); bias*, beta* ~ N(0,0.02);
-                         mask* 0 / -10000 from per-batch valid length; everything else ~ N(0,1)
+                         mask* 0 / -10000 from per-batch valid length; state uniform 32-bit words; positions counting up from a
+                         start below 1000 along the second axis, the further ones of several axes from their own; everything else ~ N(0,1)
     """
     kind = _kind(graph)
     cfg = CONFIG_INDEX[kind]
@@ -145,6 +146,14 @@ def make_inputs(graph: GraphSpec, seed: int = 0) -> Dict[str, np.ndarray]:
                 lens = valid_lengths(batch, k_len, seed)
                 a = np.where(np.arange(k_len)[None, :] < lens[:, None], 0.0, -10000.0).reshape(t.dims)
                 out[key] = quantise(a, t.dtype)
+                continue
+            if base == "state":
+                out[key] = g.integers(-(1 << 31), 1 << 31, size=t.dims).astype(np.int32)
+                continue
+            if base == "positions":
+                start = g.integers(0, 1000, size=t.dims[:1] + (1,) * (len(t.dims) - 2) + t.dims[-1:])
+                run = np.arange(t.dims[1]).reshape((1, -1) + (1,) * (len(t.dims) - 2)) if len(t.dims) > 2 else 0
+                out[key] = np.broadcast_to(start + run // np.arange(1, t.dims[-1] + 1), t.dims).astype(np.int32).copy()
                 continue
             n = base
             if n.startswith("g"):
