@@ -263,6 +263,7 @@ __device__ __forceinline__ void drop_words(const DropKey& key, uint32_t sequence
   }
   w[0] = c0; w[1] = c1; w[2] = c2; w[3] = c3;
 }
+__device__ __forceinline__ uint32_t pick(uint32_t condition, uint32_t yes, uint32_t no) { return condition != 0u ? yes : no; }
 // The 16-bit numbers of VEC columns from column `col` on, two in a word; first_group: the row's first group of eight.
 // WHOLE: col is a multiple of VEC.
 template <int VEC, bool WHOLE>
@@ -279,8 +280,8 @@ __device__ __forceinline__ void drop_numbers(const DropKey& key, uint32_t sequen
 #pragma unroll
     for (int i = 0; i < 4; ++i) n[i] = a[i];
   } else if constexpr (WHOLE && VEC == 4) {
-    n[0] = at ? a[2] : a[0];
-    n[1] = at ? a[3] : a[1];
+    n[0] = pick(at, a[2], a[0]);
+    n[1] = pick(at, a[3], a[1]);
   } else {
     if (VEC > 1 && at + VEC > 8u) {
       uint32_t w[4];
@@ -288,13 +289,14 @@ __device__ __forceinline__ void drop_numbers(const DropKey& key, uint32_t sequen
 #pragma unroll
       for (int i = 0; i < 4; ++i) a[4 + i] = w[i];
     }
-    // down by `at` halves of a word, a power of two at a time
+    // down by `at` halves of a word, a power of two at a time (values picked, not places: a conditional between two elements of an
+    // array is one between their addresses, and the array then lives in memory)
 #pragma unroll
-    for (int i = 0; i < 6; ++i) a[i] = (at & 4u) ? a[i + 2] : a[i];
+    for (int i = 0; i < 6; ++i) a[i] = pick(at & 4u, a[i + 2], a[i]);
 #pragma unroll
-    for (int i = 0; i < 5; ++i) a[i] = (at & 2u) ? a[i + 1] : a[i];
+    for (int i = 0; i < 5; ++i) a[i] = pick(at & 2u, a[i + 1], a[i]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a[i] = (at & 1u) ? (a[i] >> 16 | a[i + 1] << 16) : a[i];
+    for (int i = 0; i < 4; ++i) a[i] = pick(at & 1u, a[i] >> 16 | a[i + 1] << 16, a[i]);
 #pragma unroll
     for (int i = 0; i < (VEC + 1) / 2; ++i) n[i] = a[i];
   }

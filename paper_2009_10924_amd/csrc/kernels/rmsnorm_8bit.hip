@@ -45,7 +45,7 @@ struct Rms8Source {
       if (pbias) bias = IO::template load<false>(pbias + col);
     }
   }
-  __device__ __forceinline__ void values(bool has_bias, const DropKey& key, const Rms8Args& a, uint32_t row, uint32_t col, float (&h)[VEC]) const {
+  __device__ __forceinline__ void values(bool has_bias, const uint32_t (&numbers)[(VEC + 1) / 2], const Rms8Args& a, float (&h)[VEC]) const {
     IO::widen(x, h);
     if constexpr (FORM != RMS_PLAIN) {
       float t[VEC];
@@ -54,11 +54,7 @@ struct Rms8Source {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) h[e] += t[e];
       }
-      if constexpr (FORM == RMS_DROPPED) {
-        const uint32_t first = row * ((a.cols + 7u) / 8u);
-        if (col % VEC == 0u) drop<VEC, true>(key, a.sequence, a.threshold, a.scale, first, col, h);
-        else drop<VEC, false>(key, a.sequence, a.threshold, a.scale, first, col, h);
-      }
+      if constexpr (FORM == RMS_DROPPED) drop_apply<VEC>(numbers, a.threshold, a.scale, h);
       IO::widen(res, t);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) h[e] += t[e];
@@ -66,6 +62,22 @@ struct Rms8Source {
     if (a.flags & 2u) round_to_storage<T, VEC>(h, (const T*)nullptr);
   }
 };
+
+// The numbers of the vector that starts at `start` of the row, or early, at `col`: its own group's, but for a row's last vector that
+// starts early (in one wavefront of a row; a vector behind the row's end has none).
+template <int VEC, int FORM, bool WHOLE>
+__device__ __forceinline__ void row_numbers(const void* state, const Rms8Args& a, uint32_t row, uint32_t start, uint32_t col, uint32_t (&n)[(VEC + 1) / 2]) {
+  if constexpr (FORM == RMS_DROPPED) {
+    const DropKey key = drop_key(state);
+    const uint32_t first = row * ((a.cols + 7u) / 8u);
+    if constexpr (WHOLE) {
+      drop_numbers<VEC, true>(key, a.sequence, first, col, n);
+    } else {
+      if (start == col) drop_numbers<VEC, true>(key, a.sequence, first, col, n);
+      else if (start < a.cols) drop_numbers<VEC, false>(key, a.sequence, first, col, n);
+    }
+  }
+}
 
 template <typename T, int VEC>
 __device__ __forceinline__ void load_gains(const void* gamma, uint32_t flags, uint32_t col, float (&g)[VEC]) {
@@ -104,7 +116,8 @@ __device__ __forceinline__ void rms8_join(float& sum, float& most, float (*slot)
 // BLOCK: the whole workgroup on a row, otherwise 1 << lanes_log2 lanes; K vectors per lane.  The last vector of a row whose length is
 // no multiple of VEC starts early, at the row's last VEC elements; what the vector before it holds as well counts once in the sum and
 // is written twice, the same.
-template <typename T, int VEC, int K, int FORM, bool BLOCK, bool STREAM>
+// WHOLE: the length is a multiple of VEC.  A dropout's numbers need nothing of the row, so they are drawn while its loads are on their way.
+template <typename T, int VEC, int K, int FORM, bool BLOCK, bool STREAM, bool WHOLE>
 __global__ void __launch_bounds__(BLOCK ? 1024 : 256) k_rmsnorm8(const T* x, const T* res, const void* gamma, uint32_t rows, uint32_t cols, const T* bias,
                                                                const void* state, T* h_out, T* n_out, e4m3_t* q_out, float* scales, float* deviations,
                                                                int32_t lanes_log2, uint32_t flags, float eps, float inv_cols, float inv_max, float tiny,
@@ -123,19 +136,24 @@ __global__ void __launch_bounds__(BLOCK ? 1024 : 256) k_rmsnorm8(const T* x, con
     col[k] = min((lane + (uint32_t)k * L) * VEC, cols - VEC);
     source[k].load(x, res, bias, base, col[k]);
   }
-  DropKey key = {};
-  if constexpr (FORM == RMS_DROPPED) key = drop_key(state);
+  uint32_t numbers[K][(VEC + 1) / 2] = {};
+#pragma unroll
+  for (int k = 0; k < K; ++k) row_numbers<VEC, FORM, WHOLE>(state, a, r, (lane + (uint32_t)k * L) * VEC, col[k], numbers[k]);
   float h[K][VEC], g[K][VEC];
 #pragma unroll
   for (int k = 0; k < K; ++k) load_gains<T, VEC>(gamma, flags, col[k], g[k]);
   float sum = 0.0f, most = 0.0f;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    source[k].values(bias != nullptr, key, a, r, col[k], h[k]);
+    source[k].values(bias != nullptr, numbers[k], a, h[k]);
     const uint32_t again = (lane + (uint32_t)k * L) * VEC - col[k];   // elements that another vector holds too (VEC and more: all)
+    if (again >= (uint32_t)VEC) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) h[k][e] = 0.0f;
+    }
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-      sum += (uint32_t)e >= again ? h[k][e] * h[k][e] : 0.0f;
+      sum += WHOLE || (uint32_t)e >= again ? h[k][e] * h[k][e] : 0.0f;
       most = fmaxf(most, __builtin_fabsf(h[k][e] * g[k][e]));
     }
   }
@@ -185,19 +203,19 @@ __global__ void __launch_bounds__(1024) k_rmsnorm8_long(const T* x, const T* res
   const Rms8Args a = {rows, cols, flags, eps, inv_cols, inv_max, tiny, threshold, sequence, drop_scale};
   const uint32_t row = blockIdx.x;
   const size_t base = (size_t)row * cols;
-  DropKey key = {};
-  if constexpr (FORM == RMS_DROPPED) key = drop_key(state);
-  auto values = [&](uint32_t col, float (&h)[VEC], float (&g)[VEC]) {
+  auto values = [&](uint32_t start, uint32_t col, float (&h)[VEC], float (&g)[VEC]) {
     Rms8Source<T, VEC, FORM, false> source;
     source.load(x, res, bias, base, col);
+    uint32_t numbers[(VEC + 1) / 2] = {};
+    row_numbers<VEC, FORM, false>(state, a, row, start, col, numbers);
     load_gains<T, VEC>(gamma, flags, col, g);
-    source.values(bias != nullptr, key, a, row, col, h);
+    source.values(bias != nullptr, numbers, a, h);
   };
   float sum = 0.0f, most = 0.0f;
   for (uint32_t c = threadIdx.x * VEC; c < cols; c += 1024u * VEC) {
     float h[VEC], g[VEC];
     const uint32_t col = min(c, cols - VEC);
-    values(col, h, g);
+    values(c, col, h, g);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       sum += col + (uint32_t)e >= c ? h[e] * h[e] : 0.0f;
@@ -212,7 +230,7 @@ __global__ void __launch_bounds__(1024) k_rmsnorm8_long(const T* x, const T* res
     float m = 0.0f, none = 0.0f;
     for (uint32_t c = threadIdx.x * VEC; c < cols; c += 1024u * VEC) {
       float h[VEC], g[VEC];
-      values(min(c, cols - VEC), h, g);
+      values(c, min(c, cols - VEC), h, g);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) m = fmaxf(m, __builtin_fabsf(h[e] * rr * g[e]));
     }
@@ -227,7 +245,7 @@ __global__ void __launch_bounds__(1024) k_rmsnorm8_long(const T* x, const T* res
   for (uint32_t c = threadIdx.x * VEC; c < cols; c += 1024u * VEC) {
     float h[VEC], g[VEC], d[VEC];
     const uint32_t col = min(c, cols - VEC);
-    values(col, h, g);
+    values(c, col, h, g);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       h[e] = h[e] * rr * g[e];
@@ -244,31 +262,35 @@ namespace fs {
 using namespace fsk;
 
 namespace {
-template <typename T, int VEC, int FORM, bool S>
+template <typename T, int VEC, int FORM, bool S, bool WHOLE>
 const void* shape_sym(int32_t kernel, int vecs) {
   if (kernel == K_RMS8_LONG) return VEC > 1 ? (const void*)k_rmsnorm8_long<T, VEC, FORM> : nullptr;
-  if constexpr (VEC == 1) return kernel == K_RMS8_WAVE && vecs == 1 ? (const void*)k_rmsnorm8<T, 1, 1, FORM, false, S> : nullptr;
+  if constexpr (VEC == 1) return kernel == K_RMS8_WAVE && vecs == 1 ? (const void*)k_rmsnorm8<T, 1, 1, FORM, false, S, true> : nullptr;
   else if (kernel == K_RMS8_WAVE) {
     switch (vecs) {
-      case 1: return (const void*)k_rmsnorm8<T, VEC, 1, FORM, false, S>;
-      case 2: return (const void*)k_rmsnorm8<T, VEC, 2, FORM, false, S>;
-      case 4: return (const void*)k_rmsnorm8<T, VEC, 4, FORM, false, S>;
-      case 8: return (const void*)k_rmsnorm8<T, VEC, 8, FORM, false, S>;
+      case 1: return (const void*)k_rmsnorm8<T, VEC, 1, FORM, false, S, WHOLE>;
+      case 2: return (const void*)k_rmsnorm8<T, VEC, 2, FORM, false, S, WHOLE>;
+      case 4: return (const void*)k_rmsnorm8<T, VEC, 4, FORM, false, S, WHOLE>;
+      case 8: return (const void*)k_rmsnorm8<T, VEC, 8, FORM, false, S, WHOLE>;
     }
   } else {
     switch (vecs) {
-      case 1: return (const void*)k_rmsnorm8<T, VEC, 1, FORM, true, S>;
-      case 2: return (const void*)k_rmsnorm8<T, VEC, 2, FORM, true, S>;
-      case 4: return (const void*)k_rmsnorm8<T, VEC, 4, FORM, true, S>;
+      case 1: return (const void*)k_rmsnorm8<T, VEC, 1, FORM, true, S, WHOLE>;
+      case 2: return (const void*)k_rmsnorm8<T, VEC, 2, FORM, true, S, WHOLE>;
+      case 4: return (const void*)k_rmsnorm8<T, VEC, 4, FORM, true, S, WHOLE>;
     }
   }
   return nullptr;
 }
+template <typename T, int VEC, int FORM, bool S>
+const void* whole_sym(int32_t kernel, const RmsNorm8P& p) {
+  return p.cols % VEC == 0 ? shape_sym<T, VEC, FORM, S, true>(kernel, p.vecs_per_lane) : shape_sym<T, VEC, FORM, S, false>(kernel, p.vecs_per_lane);
+}
 template <typename T, int VEC, bool S>
 const void* form_sym(int32_t kernel, const KernelArgs& a) {
   const RmsNorm8P& p = a.u.rms8;
-  if (p.form == RMS_PLAIN) return shape_sym<T, VEC, RMS_PLAIN, S>(kernel, p.vecs_per_lane);
-  return p.form == RMS_DROPPED ? shape_sym<T, VEC, RMS_DROPPED, S>(kernel, p.vecs_per_lane) : shape_sym<T, VEC, RMS_RESIDUAL, S>(kernel, p.vecs_per_lane);
+  if (p.form == RMS_PLAIN) return whole_sym<T, VEC, RMS_PLAIN, S>(kernel, p);
+  return p.form == RMS_DROPPED ? whole_sym<T, VEC, RMS_DROPPED, S>(kernel, p) : whole_sym<T, VEC, RMS_RESIDUAL, S>(kernel, p);
 }
 template <typename T>
 const void* type_sym(int32_t kernel, const KernelArgs& a) {
