@@ -111,6 +111,7 @@ bool build_rotary(const fs_graph& g, std::vector<Candidate>* out, PackForm*) {
   s.pos_div[0] = make_fastdiv(pos_ext[2]);
   s.pos_div[1] = make_fastdiv(pos_ext[1]);
   uint32_t shared = 0;
+  s.lines = 1;
   for (size_t i = 0; i < 2; ++i) {
     RotaryRows& t = s.t[i];
     uint32_t ext[3] = {1, 1, 1};
@@ -124,6 +125,14 @@ bool build_rotary(const fs_graph& g, std::vector<Candidate>* out, PackForm*) {
         t.shared *= ext[at];
       }
       for (int k = 0; k < 3; ++k) t.in_stride[k] = r[i].in_stride[k], t.out_stride[k] = r[i].out_stride[k];
+      int longer = 0;
+      for (int k = 0; k < 3; ++k)
+        if (ext[k] > 1) {
+          ++longer;
+          t.line_in = t.in_stride[k];
+          t.line_out = t.out_stride[k];
+        }
+      if (longer > 1) s.lines = 0;
     }
     t.div[0] = make_fastdiv(ext[2]);
     t.div[1] = make_fastdiv(ext[1]);
@@ -135,57 +144,79 @@ bool build_rotary(const fs_graph& g, std::vector<Candidate>* out, PackForm*) {
   const uint32_t rest = s.dim - 2 * s.angles.pairs;
   const uint32_t V = (uint32_t)vec_of(p.in_dt);
   const uint32_t turned = p.interleaved ? 2 * s.angles.pairs : s.angles.pairs;   // elements that the accesses of turning steps start in
-  p.vec = turned >= V && (rest == 0 || rest >= V) ? (int32_t)V : 1;
+  p.vec = turned >= V ? (int32_t)V : turned >= 4 ? 4 : 1;
   const uint32_t vec = (uint32_t)p.vec;
   s.rot_units = vec == 1 ? s.angles.pairs : (turned + vec - 1) / vec;
-  const uint32_t units = s.rot_units + (rest + vec - 1) / vec;
-  s.div_units = make_fastdiv(units);
-  if (s.pos_div[0].d == 0 || s.pos_div[1].d == 0 || s.div_units.d == 0) return true;
+  s.units = s.rot_units + (rest + vec - 1) / vec;
+  s.short_rest = rest < vec ? rest : 0;
+  s.lanes = std::min<uint32_t>(s.units, 256);
+  s.div_lanes = make_fastdiv(s.lanes);
+  s.div_pairs = make_fastdiv(s.angles.pairs);
+  if (s.pos_div[0].d == 0 || s.pos_div[1].d == 0 || s.div_lanes.d == 0 || s.div_pairs.d == 0) return true;
 
   const int esz = dtype_bytes(p.in_dt);
   double n = 0;
   for (size_t i = 0; i < tensors; ++i) n += (double)g.tensors[r[i].out].numel();
-  for (int U : {1, 2, 4}) {
-    // rows of one workgroup: what U steps of 256 threads cover, at least one; all rows of a position where they fit
-    const uint32_t rows = std::max<uint32_t>(1, 256u * U / units);
-    const uint32_t tiles_h = (shared + rows - 1) / rows;
-    s.h_tile = (shared + tiles_h - 1) / tiles_h;
-    s.p_tile = std::max<uint32_t>(1, std::min(s.positions, rows / s.h_tile));
-    while (s.p_tile > 1 && s.p_tile * s.angles.pairs > 4096) --s.p_tile;
-    const uint32_t h_tiles = (shared + s.h_tile - 1) / s.h_tile, p_tiles = (s.positions + s.p_tile - 1) / s.p_tile;
-    s.div_h_tiles = make_fastdiv(h_tiles);
-    s.div_inner = make_fastdiv(s.p_inner ? s.p_tile : s.h_tile);
-    if (s.div_h_tiles.d == 0 || s.div_inner.d == 0 || (uint64_t)h_tiles * p_tiles >= (1ull << 24)) continue;
-    p.iter = U;
-    Candidate c = make_candidate(g, "rotary", FS_SCHEME_LDS, K_ROTARY);
-    Launch& l = c.launches.front();
-    l.args.u.rotary = p;
-    l.ptr[0] = in_ref(g, r[0].in);
-    if (tensors == 2) l.ptr[1] = in_ref(g, r[1].in);
-    l.ptr[2] = in_ref(g, t_pos);
-    l.ptr[3] = out_ref(g.tensors[r[0].out].output_slot);
-    if (tensors == 2) l.ptr[4] = out_ref(g.tensors[r[1].out].output_slot);
-    l.shape.block[0] = 256;
-    l.shape.grid[0] = h_tiles * p_tiles;
-    l.shape.lds_bytes = s.p_tile * s.angles.pairs * 8;
-    c.info.lanes_per_row = (int32_t)std::min<uint32_t>(units, 256);
-    c.info.vecs_per_lane = U;
-    c.info.rows_per_block = (int32_t)(s.p_tile * s.h_tile);
-    c.info.lds_bytes = (int32_t)l.shape.lds_bytes;
-    KernelCost kc;
-    kc.waves_per_block = 4;
-    kc.waves = (double)l.shape.grid[0] * 4;
-    kc.lds_bytes_per_block = c.info.lds_bytes;
-    kc.vgpr_estimate = 40 + 16 * U;
-    const double groups = (double)l.shape.grid[0];
-    const double used = n / vec / (p.interleaved && vec > 1 ? 1.0 : 2.0) / (groups * 256.0 * U);   // of the lanes' steps
-    const double angles = std::max(1.0, std::ceil(s.p_tile * s.angles.pairs / 256.0));
-    kc.own_estimate_s = (3.2 + 0.1 * U + std::max(2.0 * n * esz / 6.2e6 * (1.0 + 0.15 * (1.0 / std::max(0.05, std::min(1.0, used)) - 1.0)),
-                                                  groups / 2048.0 * (0.6 * angles + 0.3 * U))) * 1e-6;
-    char var[48];
-    snprintf(var, sizeof var, "<%s,%s,v%d,U%d,P%u,H%u>", dtype_name(p.in_dt), p.interleaved ? "interleaved" : "halves", p.vec, U, s.p_tile, s.h_tile);
-    finish_candidate(&c, var, kc);
-    out->push_back(c);
+  const uint32_t slots = 256 / s.lanes;
+  for (uint32_t P = 1; P <= slots; P *= 2) {
+    if (P > 1 && P / 2 >= s.positions) break;
+    s.p_slots = std::min(P, s.positions);
+    if (s.p_slots * s.angles.pairs > (P > 1 ? 4096u : 8192u)) break;   // its angles in LDS, 64 KB at most
+    s.h_slots = std::min(shared, slots / s.p_slots);
+    const uint32_t p_tiles = (s.positions + s.p_slots - 1) / s.p_slots;
+    for (int U : {1, 2, 3, 5}) {
+      if (U > 1 && s.h_slots * (U == 5 ? 3 : U - 1) >= shared) break;
+      const uint32_t most = s.h_slots * U;   // a thread's rows are all loaded at once
+      uint32_t h_tiles = (shared + most - 1) / most;
+      s.h_tile = (shared + h_tiles - 1) / h_tiles;
+      h_tiles = (shared + s.h_tile - 1) / s.h_tile;
+      s.div_h_tiles = make_fastdiv(h_tiles);
+      s.div_inner = make_fastdiv(s.p_inner ? s.p_slots : s.h_slots);
+      if (s.div_h_tiles.d == 0 || s.div_inner.d == 0 || (uint64_t)h_tiles * p_tiles >= (1ull << 24)) continue;
+      p.iter = U;
+      Candidate c = make_candidate(g, "rotary", FS_SCHEME_LDS, K_ROTARY);
+      Launch& l = c.launches.front();
+      l.args.u.rotary = p;
+      l.ptr[0] = in_ref(g, r[0].in);
+      if (tensors == 2) l.ptr[1] = in_ref(g, r[1].in);
+      l.ptr[2] = in_ref(g, t_pos);
+      l.ptr[3] = out_ref(g.tensors[r[0].out].output_slot);
+      if (tensors == 2) l.ptr[4] = out_ref(g.tensors[r[1].out].output_slot);
+      l.shape.block[0] = 256;
+      l.shape.grid[0] = h_tiles * p_tiles;
+      l.shape.lds_bytes = s.p_slots * s.angles.pairs * 8;
+      c.info.lanes_per_row = (int32_t)s.lanes;
+      c.info.vecs_per_lane = U;
+      c.info.rows_per_block = (int32_t)(s.p_slots * s.h_tile);
+      c.info.lds_bytes = (int32_t)l.shape.lds_bytes;
+      KernelCost kc;
+      kc.waves_per_block = 4;
+      kc.waves = (double)l.shape.grid[0] * 4;
+      kc.lds_bytes_per_block = c.info.lds_bytes;
+      // The estimate (us), fitted to every candidate of 880 drawn shapes of 1 to 2^26 elements in three dtypes, positions of one to three
+      // axes: the one chosen is 3.2 % behind the fastest (geometric mean; 3.7 % from 50 MB on).  Rows that are no whole lines cost by the
+      // runs in which a workgroup reads and writes them, most of all written ones.
+      const double row_bytes = (double)s.dim * esz, steps = std::ceil((double)s.h_tile / s.h_slots);
+      const double per = p.interleaved && vec > 1 ? vec : 2.0 * vec;   // elements of a step
+      const double used = std::min(1.0, n / per / ((double)l.shape.grid[0] * 256.0 * steps));   // of the threads' steps
+      const double at_once = s.angles.pairs < 256 ? 256 / s.angles.pairs : 1, angles = std::ceil(s.p_slots / at_once) * std::ceil(s.angles.pairs / 256.0);
+      auto run = [&](const uint32_t (&stride)[3]) {   // bytes that neighbouring slots cover without a gap
+        const bool along_h = s.t[0].shared > 1 && stride[s.p_inner ? 1 : 2] == s.dim;
+        return row_bytes * (along_h ? std::min(s.h_slots, s.t[0].shared) : s.p_slots);
+      };
+      const double cuts = (int64_t)row_bytes % 128 != 0 ? 13.9 : 1.0;
+      kc.vgpr_estimate = 46 + (vec == 8 ? 6 : 0) + (p.interleaved && vec > 1 ? 5 : 10) * U;
+      const double resident = std::min(8, 512 / ((kc.vgpr_estimate + 7) / 8 * 8));
+      const double memory = 2.0 * n * esz / 5.18e6 * (1.0 + 0.0058 * (1.0 / std::max(0.05, used) - 1.0)) * (1.0 + 0.083 * (8.0 / resident - 1.0)) *
+                            (1.0 + cuts * (0.017 * 128.0 / run(r[0].in_stride) + 0.186 * 128.0 / run(r[0].out_stride)));
+      const double issue = kc.waves / 1024.0 * (218.0 + 16.0 * angles + 245.0 * steps * (per / 16.0 * 0.8 + 0.4)) / 2400.0;
+      const double both = std::pow(std::pow(memory, 0.73) + std::pow(issue, 0.73), 1.0 / 0.73);
+      kc.own_estimate_s = (2.9 + 0.55 * (both + 0.176 * angles + 0.188 * steps)) * 1e-6;
+      char var[48];
+      snprintf(var, sizeof var, "<%s,%s,v%d,U%d,P%u,H%ux%u>", dtype_name(p.in_dt), p.interleaved ? "interleaved" : "halves", p.vec, U, s.p_slots, s.h_slots, (s.h_tile + s.h_slots - 1) / s.h_slots);
+      finish_candidate(&c, var, kc);
+      out->push_back(c);
+    }
   }
   return true;
 }

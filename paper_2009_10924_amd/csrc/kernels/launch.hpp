@@ -253,12 +253,12 @@ struct RotaryAngles {
   uint32_t end[4];
   int32_t restart, inverse;
 };
-// A tensor's rows: (position axes, shared axes) -> element, as strides along the three leading axes.  Its rows at one position are
-// `shared` many, numbered along the axes that the positions stretch over.
+// A tensor's rows at one position are `shared` many, numbered along the axes that the positions stretch over.
 struct RotaryRows {
   uint32_t shared;
+  uint32_t line_in, line_out;       // the strides of the only one of those axes that is longer than 1 (RotaryShape::lines)
   FastDiv div[2];                   // by the shared extents of axes 2 and 1
-  uint32_t in_stride[3], out_stride[3];
+  uint32_t in_stride[3], out_stride[3];   // elements, along the three leading axes
 };
 struct RotaryShape {
   RotaryAngles angles;
@@ -266,10 +266,13 @@ struct RotaryShape {
   FastDiv pos_div[2];               // by the positions' extents along axes 2 and 1
   uint32_t pos_stride[3];           // rows of positions, along the leading axes
   RotaryRows t[2];
-  uint32_t p_tile, h_tile;          // a workgroup's positions, and rows at each of them
-  FastDiv div_h_tiles, div_inner, div_units;
-  uint32_t p_inner;                 // 1: neighbouring rows of a workgroup are at neighbouring positions, 0: at the same
-  uint32_t rot_units;               // steps of a row that turn pairs; the others (up to div_units.d) copy
+  // A workgroup: 256 threads as p_slots positions x h_slots rows of each x `lanes` steps of a row; h_tile rows at a position
+  uint32_t lanes, p_slots, h_slots, h_tile;
+  FastDiv div_h_tiles, div_lanes, div_pairs, div_inner;
+  uint32_t p_inner;                 // 1: neighbouring groups of lanes are at neighbouring positions, 0: at the same
+  uint32_t lines;                   // 1: neither tensor's rows at a position lie along more than one axis
+  uint32_t short_rest;              // elements behind the pairs where they are fewer than an access, else 0
+  uint32_t units, rot_units;        // steps of a row; those that turn pairs (the others copy)
 };
 struct RotaryP {
   int32_t in_dt, out_dt;            // K_ROTARY: the same

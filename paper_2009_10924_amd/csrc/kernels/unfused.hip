@@ -414,7 +414,7 @@ __global__ void __launch_bounds__(256) k_rotary_op(const void* in, const int32_t
   const uint32_t at_position = c0 * s.pos_stride[0] + c1 * s.pos_stride[1] + c2 * s.pos_stride[2];
   const uint32_t axis = rotary_axis(s.angles, u);
   float c, d;
-  rotary_turn(s.angles, u, axis, positions[(size_t)at_position * s.angles.n_axes + axis], c, d);
+  rotary_turn((double)positions[(size_t)at_position * s.angles.n_axes + axis] * rotary_speed(s.angles, u, axis), s.angles.inverse != 0, c, d);
   const uint32_t ea = at + (p.interleaved ? 2u * u : u), eb = p.interleaved ? ea + 1u : ea + s.angles.pairs;
   const float a = load_rt1(in, p.in_dt, ea), b = load_rt1(in, p.in_dt, eb);
   const float va[1] = {a * c - b * d}, vb[1] = {b * c + a * d};

@@ -45,6 +45,26 @@ template <typename T> struct VecIo<T, 1> {
   template <typename U> __device__ __forceinline__ static void put1(U* p, float v) { store1(p, v); }
   __device__ __forceinline__ static void put1(e4m3_t* p, float v) { store1_in_range(p, v); }
 };
+// half a vector of a 16-bit type
+template <typename T> struct HalfVecIo {
+  typedef u32x2 Raw;
+  typedef typename AtAlignment<u32x2, 2>::type Place;
+  template <bool STREAM> __device__ __forceinline__ static Raw load(const T* p) {
+    const Place* q = reinterpret_cast<const Place*>(p);
+    return STREAM ? __builtin_nontemporal_load(q) : *q;
+  }
+  __device__ __forceinline__ static void widen(Raw r, float (&v)[4]) {
+    float w[8];
+    unpack(u32x4{r.x, r.y, 0u, 0u}, w, (const T*)nullptr);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = w[e];
+  }
+  template <bool STREAM = true> __device__ __forceinline__ static void store(T* p, const float (&v)[4]) {
+    put<STREAM, 2>(u32x2{pack2(v[0], v[1], (const T*)nullptr), pack2(v[2], v[3], (const T*)nullptr)}, p);
+  }
+};
+template <> struct VecIo<f16_t, 4> : HalfVecIo<f16_t> {};
+template <> struct VecIo<bf16_t, 4> : HalfVecIo<bf16_t> {};
 template <> struct VecIo<e4m3_t, 8> {
   typedef u32x2 Raw;
   typedef AtAlignment<u32x2, 1>::type Place;
