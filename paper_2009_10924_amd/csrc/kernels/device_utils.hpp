@@ -263,7 +263,7 @@ __device__ __forceinline__ void drop_words(const DropKey& key, uint32_t sequence
   }
   w[0] = c0; w[1] = c1; w[2] = c2; w[3] = c3;
 }
-__device__ __forceinline__ uint32_t pick(uint32_t condition, uint32_t yes, uint32_t no) { return condition != 0u ? yes : no; }
+template <typename V> __device__ __forceinline__ V pick(uint32_t condition, V yes, V no) { return condition != 0u ? yes : no; }
 // The 16-bit numbers of VEC columns from column `col` on, two in a word; first_group: the row's first group of eight.
 // WHOLE: col is a multiple of VEC.
 template <int VEC, bool WHOLE>

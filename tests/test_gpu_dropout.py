@@ -61,6 +61,14 @@ def test_forms(act, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("cols", [1, 2, 5, 7, 9, 10, 11, 12, 13, 14, 15, 17, 23, 63])
+def test_ends_of_rows(cols, dtype):
+    """A row's last group holds 1 to 7 elements of its own."""
+    _forward_case(300, cols, 0.3, dtype, "none", True, True, "auto")
+    _forward_case(300, cols, 0.5, dtype, "none", False, False, "auto")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("act", ["none", "gelu", "silu"])
 @pytest.mark.parametrize("dbias", [False, True])
 def test_backward(act, dtype, dbias):
@@ -174,6 +182,23 @@ def test_norm_backward_with_dropout_every_shape():
         assert _candidates(spec, inputs, compare) >= 2
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sums_over_one_row(dtype):
+    """Sums, means and maxima over leading axes of extent 1 are the row's own values, whatever reads them."""
+    spec = GraphSpec("pattern_one_row", [TensorSpec("x", dtype, (1, 1, 300)), TensorSpec("state", "i32", (4,)), TensorSpec("g", dtype, (300,))],
+                     [OpSpec("d", "dropout", ("x", "state"), {"probability": 0.5}), OpSpec("a", "reduce_sum", ("d",), {"axis": 0}),
+                      OpSpec("b", "reduce_mean", ("a",), {"axis": 0}), OpSpec("m", "reduce_max", ("d",), {"axis": 1}),
+                      OpSpec("y", "mul", ("b", "g"))], [("d", dtype), ("b", "f32"), ("m", "f32"), ("y", dtype)])
+    inputs = W.make_inputs(spec, 8)
+    ref = O.evaluate(spec, inputs, keep_all=True)
+
+    def compare(got, raw, info, plan):
+        for name, dt in spec.outputs:
+            E.close(got[name], ref[name].reshape(got[name].shape), dt, 2 * E.U32 * np.abs(ref[name]).reshape(got[name].shape), f"{info['kernel']} {name}")
+
+    assert _candidates(spec, inputs, compare) >= 2
+
+
 def test_transposed_and_stretched_neighbours():
     """A dropout behind a folded transpose goes by its own rows; one of a value that stretches later is drawn once."""
     dims = (2, 5, 3, 16)
@@ -196,7 +221,7 @@ def test_transposed_and_stretched_neighbours():
 def test_in_place():
     """The element-wise kernel may write over its input or residual."""
     import torch
-    for cols in (64, 67):
+    for cols in (64, 67, 7, 9, 15, 654):
         spec = W.dropout_graph(50, cols, 0.3, dtype="bf16", residual=True, bias=True)
         inputs = W.make_inputs(spec, 2)
         want = run_spec(spec, inputs)[1]["y"]
