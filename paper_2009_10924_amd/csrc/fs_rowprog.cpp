@@ -538,6 +538,10 @@ struct Compiler {
             val[op.out].kind = V_FULL;
             break;
           }
+          if (rows == 1 && op.axis != src.rank - 1) {   // over the one row there is: its values
+            is_alias[i] = 1;
+            break;
+          }
           if (op.opcode == FS_REDUCE_SUM && op.axis == 0 && src.rank == rank && ka == V_FULL && !stretched_rows(src) &&
               sum_chain[i] == 0) {
             const int end = column_sum_chain_end(i);

@@ -246,6 +246,13 @@ def test_a_dropout_joins_row_programs():
         assert _plan(W.dropout_graph(64, 128)).info["pattern"] == "dropout"
 
 
+@pytest.mark.skipif(not B.codegen_available(), reason="needs the run-time compiler")
+def test_sums_over_one_row_take_no_launch_of_their_own():
+    for spec in (W.dropout_backward_graph(1, 2048, act="gelu", bias=True, dbias=True), W.rmsnorm_residual_backward_graph(1, 1024, p=0.1)):
+        info = _plan(spec).info
+        assert info["pattern"] == "row_generated" and info["n_kernels"] == 1, info
+
+
 def test_a_program_keeps_the_attributes():
     """The explorer's sub-graphs draw and turn as the whole graph says."""
     spec = W.decoder_block_graph(batch=2, seq=16, heads=4, kv_heads=2, dim=32, ffn=64, sections=(4, 6, 6))
