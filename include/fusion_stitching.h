@@ -341,6 +341,35 @@ int64_t fs_plan_source(const fs_plan *p, char *text, size_t capacity);
  * per-op plan, and so does the normalisation of so many short groups that a workgroup for each
  * would be 2^32 threads or take longer than the ops one by one.                             */
 
+/* ---- dropout, norms with an 8-bit result, rotary positions ----------------------
+ * Patterns that have kernels of their own; T is FS_F32, FS_F16 or FS_BF16.
+ *
+ * "dropout": y = FS_DROPOUT(act(x + bias)), or that + residual; and dx = FS_DROPOUT(dy) * act'(x + bias)
+ *   (bias [columns], act and its slope as for checkpoints, each where there is one; all of T and but for the
+ *   bias of one shape).  y may be x's, dy's or the residual's own memory.
+ *   With column sums beside it (a bias gradient), or in front of or behind row reductions (attention
+ *   probabilities, a norm of the dropped branch), a dropout is part of a generated row kernel; where
+ *   kernels are not generated (FS_CODEGEN=0) those run op by op.  An element that is not kept is 0 even
+ *   where it held NaN or an infinity.
+ *
+ * "rmsnorm_8bit": h = x, or x + residual, x + bias + residual, or FS_DROPOUT(x, or x + bias) + residual,
+ *   read as it is or rounded to T (FS_CONVERT);
+ *     r = FS_RSQRT(mean of h^2 along the last axis + eps), n = h * r * gamma
+ *   and n in 8 bits with a scale per row, spelled like a checkpoint: s = max |n| * inv_max + tiny, q = n / s.
+ *   Outputs: q (FS_E4M3), s (FS_F32, last extent 1); if wanted h (T), n (T), r (FS_F32, last extent 1).
+ *   gamma [columns], T or FS_F32.  A row may have any length; one of more than 4096 16-byte vectors is
+ *   read twice.  A NaN in h makes r, s and the row's n and q NaN; an infinity makes r 0, its own n and q
+ *   NaN, the row's others 0 and s = tiny.  Rows beside it do not change.
+ *
+ * "rotary": FS_ROTARY of one tensor, or of two (queries and keys) with the same positions and attributes,
+ *   each with an FS_TRANSPOSE of leading axes in front (heads that come in split, for the gradient) or
+ *   behind (head split; the result is first rounded with FS_CONVERT to what is stored, or is a graph
+ *   output's rounding).  One launch reads and writes every element once.
+ *
+ * The outputs of the last two may share no memory with an input or with another output (see the
+ * rules of group normalisation: the ops run one by one where no tensor is FS_E4M3 and the workspace
+ * holds them, else FS_ERR_INVALID_ARG).  State and positions are read when the kernels run.            */
+
 /* ---- execution (the run-time hot path) --------------------------------------- */
 
 /* Enqueues the plan's kernel(s) on `hip_stream` (a hipStream_t; null = the
@@ -358,7 +387,8 @@ int64_t fs_plan_source(const fs_plan *p, char *text, size_t capacity);
  * in different orders, so their last bits may differ; and where rows of an odd number of
  * 16-bit elements lie on the tensor's 16-byte grid, which lane adds which elements depends
  * on the row's index, so that equal rows of a tensor may round differently.
- * Group normalisation and 8-bit checkpoints have rules of their own for outputs that share memory (above).
+ * Group normalisation, 8-bit checkpoints and norms, and rotary positions have rules of their own for outputs that share
+ * memory (above).
  * Two calls that share a workspace must be ordered on one stream.
  * Errors: FS_ERR_INVALID_ARG, FS_ERR_WORKSPACE, FS_ERR_ALIGN, FS_ERR_HIP.         */
 fs_status fs_execute(const fs_plan *p, const void *const *inputs, void *const *outputs,

@@ -161,7 +161,7 @@ bool build_rotary(const fs_graph& g, std::vector<Candidate>* out, PackForm*) {
   for (uint32_t P = 1; P <= slots; P *= 2) {
     if (P > 1 && P / 2 >= s.positions) break;
     s.p_slots = std::min(P, s.positions);
-    if (s.p_slots * s.angles.pairs > (P > 1 ? 4096u : 8192u)) break;   // its angles in LDS, 64 KB at most
+    if (s.p_slots * s.angles.pairs > 4096) break;   // 32 KB of angles (one position has no more)
     s.h_slots = std::min(shared, slots / s.p_slots);
     const uint32_t p_tiles = (s.positions + s.p_slots - 1) / s.p_slots;
     for (int U : {1, 2, 3, 5}) {

@@ -454,6 +454,9 @@ int fs::streamed_loads(const Launch& l) {
     case K_ROW_GENERATED: return a.u.prog.stream;
     case K_CHECKPOINT_WAVE: case K_CHECKPOINT_BLOCK: case K_CHECKPOINT_GRAD: case K_CHECKPOINT_GRAD_SUMS:
       return a.u.checkpoint.vec > 1 ? a.u.checkpoint.stream : -1;
+    case K_DROPOUT: return a.u.dropout.stream;
+    case K_RMS8_WAVE: case K_RMS8_BLOCK: return a.u.rms8.vec > 1 ? a.u.rms8.stream : -1;
+    case K_ROTARY: return a.u.rotary.vec * dtype_bytes(a.u.rotary.in_dt) == 16 ? a.u.rotary.stream : -1;
     default: return -1;
   }
 }
