@@ -120,20 +120,21 @@ bool build_rmsnorm_8bit(const fs_graph& g, std::vector<Candidate>* out, PackForm
     if (out_r >= 0) l.ptr[9] = out_ref(g.tensors[out_r].output_slot);
     return c;
   };
-  // The estimate (us), fitted to every candidate of 900 drawn shapes of 1 to 2^25 elements, three dtypes and all forms: the one chosen is
-  // 2.7 % behind the fastest (geometric mean).  Many values a lane leave too few wavefronts to keep the memory busy (bf16 [8192,4096], 64 a
-  // lane 47.2, 32 43.4, 16 39.7, 8 39.6).  A workgroup's exchange shows with every round of resident workgroups.
+  // The estimate (us), fitted to every candidate of 18,000 drawn shapes of 1 to 2^25 elements, three dtypes and all forms: on 9,000 others the
+  // one chosen is 2.0 % behind the fastest (geometric mean; 1.4 % from 50 MB on).  Many values a lane leave too few wavefronts to keep the
+  // memory busy (bf16 [8192,4096], 64 a lane 47.2, 32 43.4, 16 39.7, 8 39.6).  A workgroup's exchange shows with every round of resident
+  // workgroups, and rows that are no whole vectors take a fifth more instructions and straddle lines.
   auto estimate = [&](KernelCost* kc, double lanes, int K, bool workgroup) {
-    const double bytes = n * esz * wide + n + 4.0 * p.rows * (out_r >= 0 ? 2 : 1);
-    const double ops = (14.0 + (p.form == 2 ? 18.0 : 0.0) + (tb >= 0 ? 2.0 : 0.0)) * K * p.vec;
+    const double bytes = n * esz * wide + n + 4.0 * p.rows * (out_r >= 0 ? 2 : 1), whole = p.cols % p.vec == 0 ? 1.0 : 0.0;
+    const double ops = (14.0 + (p.form == 2 ? 18.0 : 0.0) + (tb >= 0 ? 2.0 : 0.0)) * K * p.vec * (1.0 + 0.21 * (1.0 - whole));
     kc->vgpr_estimate = 24 + K * p.vec * (tres >= 0 ? 2 : 1) + K * p.vec;
-    const double issue = std::max(1.0, kc->waves / 1024.0) * 6.28 * ops / 2400.0;
+    const double issue = std::max(1.0, kc->waves / 1024.0) * (31.1 + 3.54 * ops) / 2400.0;
     const double run = std::min<double>(lanes * p.vec, p.cols) * esz;
     const double per_simd = std::max(1, std::min(8, 512 / ((kc->vgpr_estimate + 7) / 8 * 8)));   // wavefronts
-    const double memory = bytes / 6.77e6 * (1.0 + 0.046 * (1.0 / kc->lane_utilisation - 1.0)) * (1.0 + 0.07 * (8.0 / per_simd - 1.0)) *
-                          (1.0 + 0.284 * std::max(0.0, 128.0 / run - (p.cols % p.vec == 0 ? 1.0 : 0.0)));
-    const double rounds = std::max(1.0, kc->waves / (1024.0 * per_simd)), exchange = workgroup ? rounds * (0.057 + 0.0197 * kc->waves_per_block) : 0.0;
-    kc->own_estimate_s = (3.08 + std::pow(std::pow(memory, 2.62) + std::pow(issue, 2.62) + std::pow(exchange, 2.62), 1.0 / 2.62)) * 1e-6;
+    const double memory = bytes / 7.75e6 * (1.0 + 0.017 * (1.0 / kc->lane_utilisation - 1.0)) * (1.0 + 0.367 * (8.0 / per_simd - 1.0)) *
+                          (1.0 + 0.42 * std::max(0.0, 128.0 / run - whole));
+    const double rounds = std::max(1.0, kc->waves / (1024.0 * per_simd)), exchange = workgroup ? rounds * (0.291 + 0.0287 * kc->waves_per_block) : 0.0;
+    kc->own_estimate_s = (3.14 + std::pow(std::pow(memory, 1.49) + std::pow(issue, 1.49) + std::pow(exchange, 1.49), 1.0 / 1.49)) * 1e-6;
   };
   const char* form = p.form == 0 ? "plain" : p.form == 1 ? "residual" : "dropout";
   for (int K : {1, 2, 4, 8}) {

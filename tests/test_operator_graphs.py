@@ -205,7 +205,7 @@ def test_patterns_and_their_kernels():
             (W.dropout_graph(64, 128), "dropout", "dropout<bf16,none>"),
             (W.dropout_graph(64, 130, act="silu", bias=True, residual=True), "dropout", "dropout<bf16,silu,ragged>"),
             (W.dropout_backward_graph(64, 128, act="gelu", bias=True, dbias=False), "dropout", "dropout<bf16,gelu,slope>"),
-            (W.rmsnorm_8bit_graph(64, 1024), "rmsnorm_8bit", "rmsnorm8_block<bf16,residual"),
+            (W.rmsnorm_8bit_graph(64, 1024), "rmsnorm_8bit", "rmsnorm8_"),
             (W.rmsnorm_8bit_graph(64, 1024, residual=False), "rmsnorm_8bit", "rmsnorm8_"),
             (W.rmsnorm_8bit_graph(64, 1024, p=0.1, bias=True, rounded=True, normed=True, keep="stats"), "rmsnorm_8bit", "rmsnorm8_"),
             (W.rotary_graph(2, 64, (8, 2), 128, (64,)), "rotary", "rotary<bf16,halves,v8"),
