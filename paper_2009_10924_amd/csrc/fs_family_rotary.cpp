@@ -194,8 +194,8 @@ bool build_rotary(const fs_graph& g, std::vector<Candidate>* out, PackForm*) {
       kc.waves = (double)l.shape.grid[0] * 4;
       kc.lds_bytes_per_block = c.info.lds_bytes;
       // The estimate (us), fitted to every candidate of 880 drawn shapes of 1 to 2^26 elements in three dtypes, positions of one to three
-      // axes: on 6,700 others the one chosen is 3.8 % behind the fastest (geometric mean; 4.5 % from 30 MB on; fitted to those, 3.7 and 4.2).  Rows that are no whole lines cost by the
-      // runs in which a workgroup reads and writes them, most of all written ones.
+      // axes: on 6,700 others the one chosen is 3.8 % behind the fastest (geometric mean; 4.5 % from 30 MB on; fitted to those, 3.7 and
+      // 4.2).  Rows that are no whole lines cost by the runs in which a workgroup reads and writes them, most of all written ones.
       const double row_bytes = (double)s.dim * esz, steps = std::ceil((double)s.h_tile / s.h_slots);
       const double per = p.interleaved && vec > 1 ? vec : 2.0 * vec;   // elements of a step
       const double used = std::min(1.0, n / per / ((double)l.shape.grid[0] * 256.0 * steps));   // of the threads' steps
