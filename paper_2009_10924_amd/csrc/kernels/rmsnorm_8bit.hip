@@ -102,6 +102,9 @@ __device__ __forceinline__ void load_gains(const void* gamma, uint32_t flags, ui
 // The row's sum of squares and largest magnitude from the lanes': over a lane group, or over the workgroup through LDS.
 template <bool BLOCK>
 __device__ __forceinline__ void rms8_join(float& sum, float& most, float (*slot)[2], uint32_t lanes) {
+  // A lane's only square, fused into the first addition, would go in unrounded there and rounded into its neighbours' sums: the lanes of a
+  // row would normalise by different r.  (No instruction.)
+  asm volatile("" : "+v"(sum));
   if constexpr (BLOCK) {
     sum = group_allreduce<OpSum>(sum, kWave);
     most = group_allreduce<OpMax>(most, kWave);
