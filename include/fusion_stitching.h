@@ -359,7 +359,8 @@ int64_t fs_plan_source(const fs_plan *p, char *text, size_t capacity);
  *   Outputs: q (FS_E4M3), s (FS_F32, last extent 1); if wanted h (T), n (T), r (FS_F32, last extent 1).
  *   gamma [columns], T or FS_F32.  A row may have any length; one of more than 4096 16-byte vectors is
  *   read twice.  A NaN in h makes r, s and the row's n and q NaN; an infinity makes r 0, its own n and q
- *   NaN, the row's others 0 and s = tiny.  Rows beside it do not change.
+ *   NaN, the row's others 0 and s = tiny; a row of zeros with eps 0 has r infinite, n and q NaN and
+ *   s = tiny.  Rows beside it do not change.
  *
  * "rotary": FS_ROTARY of one tensor, or of two (queries and keys) with the same positions and attributes,
  *   each with an FS_TRANSPOSE of leading axes in front (heads that come in split, for the gradient) or

@@ -2,7 +2,10 @@
 //   h = x,  x + bias + residual,  or  dropout(x + bias) + residual
 //   r = 1 / sqrt(mean h^2 + eps),  n = h r gamma,  s = max |n| / 448 + tiny,  q = e4m3(n / s)
 // A lane group or a workgroup holds the row between its sum and its quotients: what is read is read once.  The largest |n| is r times
-// the largest |h gamma|, so one pass over the registers and one exchange between lanes give both the sum and the maximum.
+// the largest |h gamma|, so one pass over the registers and one exchange between lanes give both the sum and the maximum.  (Taken of n itself,
+// in an exchange of its own behind the sum's, the maximum would be rounded as n is, not once otherwise; that took 40.2 instead of 39.0 us at
+// bf16 [8192,4096], 46.5 instead of 42.5 at [2048,16384], and r's last bit, from the order of the sum, moves as many quotients over a rounding
+// border of the 8-bit format as the maximum's.)
 // Memory bounds it: x and the residual read, h and q written, 7 bytes an element of 16 bits.  bf16 [8192,4096] 38.9 us, 6.0 TB/s; f16
 // [8192,2048] 22.0, with bias and dropout 22.8 (5.2 TB/s; the launch's ramp is 3 of it); [8191,2050] 22 to 26, rows straddle lines.  Four
 // rows of 4096: 2.5 us, the chain of load, sum, exchange, quotient.
@@ -99,6 +102,10 @@ __device__ __forceinline__ void load_gains(const void* gamma, uint32_t flags, ui
   }
 }
 
+// Whether max |h gamma| has lost what n = h r gamma keeps: beyond the range, or below the normal one, where a product has fewer bits
+// than n or none (and where all are 0, r may be infinite).  A NaN has not come through.
+__device__ __forceinline__ bool left_range(float most) { return !(most < __builtin_inff() && most >= 1.17549435e-38f); }
+
 // The row's sum of squares and largest magnitude from the lanes': over a lane group, or over the workgroup through LDS.
 template <bool BLOCK>
 __device__ __forceinline__ void rms8_join(float& sum, float& most, float (*slot)[2], uint32_t lanes) {
@@ -166,16 +173,16 @@ __global__ void __launch_bounds__(BLOCK ? 1024 : 256) k_rmsnorm8(const T* x, con
   rms8_join<BLOCK>(sum, most, slot[0], L);
   const float rr = fast_rsqrt(sum * inv_cols + eps);
   float largest = most * rr;
-  // Where a product with the gain has left the range, or the row holds an infinity, the maximum is taken of n itself, as it is
+  // Where the products with the gains have left the range, or the row holds an infinity, the maximum is taken of n itself, as it is
   // defined.  (All lanes of a wavefront take part in the exchange, whosever row it is for.)
-  if (__any(!(most < __builtin_inff()))) {
+  if (__any(left_range(most))) {
     float m = 0.0f, none = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) m = fmaxf(m, __builtin_fabsf(h[k][e] * rr * g[k][e]));
     rms8_join<BLOCK>(none, m, slot[1], L);
-    if (!(most < __builtin_inff())) largest = rr == rr ? m : rr;
+    if (left_range(most)) largest = rr == rr ? m : rr;
   }
   const Divisor s(scale_of(largest, inv_max, tiny));
   if (row >= rows) return;
@@ -232,7 +239,7 @@ __global__ void __launch_bounds__(1024) k_rmsnorm8_long(const T* x, const T* res
   rms8_join<true>(sum, most, slot[0], 1024u);
   const float rr = fast_rsqrt(sum * inv_cols + eps);
   float largest = most * rr;
-  if (!(most < __builtin_inff())) {   // (the whole workgroup's: see k_rmsnorm8)
+  if (left_range(most)) {   // (the whole workgroup's: see k_rmsnorm8)
     float m = 0.0f, none = 0.0f;
     for (uint32_t c = threadIdx.x * VEC; c < cols; c += 1024u * VEC) {
       float h[VEC], g[VEC];
