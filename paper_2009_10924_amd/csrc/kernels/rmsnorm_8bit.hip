@@ -206,7 +206,9 @@ __global__ void __launch_bounds__(BLOCK ? 1024 : 256) k_rmsnorm8(const T* x, con
   }
 }
 
-// Rows that no workgroup can hold: read twice, once for the sum and the maximum and once for the quotients.
+// Rows that no workgroup can hold: read twice, once for the sum and the maximum and once for the quotients.  A lane adds the sums of its
+// vectors up in 64 bits: one float32 for 2^14 squares and more, a lane's share of 2^24 columns, was off by 1e-4 of itself (and the lanes
+// by the same where values are alike).
 template <typename T, int VEC, int FORM>
 __global__ void __launch_bounds__(1024) k_rmsnorm8_long(const T* x, const T* res, const void* gamma, uint32_t rows, uint32_t cols, const T* bias,
                                                         const void* state, T* h_out, T* n_out, e4m3_t* q_out, float* scales, float* deviations, int32_t,
@@ -224,18 +226,21 @@ __global__ void __launch_bounds__(1024) k_rmsnorm8_long(const T* x, const T* res
     load_gains<T, VEC>(gamma, flags, col, g);
     source.values(bias != nullptr, numbers, a, h);
   };
-  float sum = 0.0f, most = 0.0f;
+  double squares = 0.0;
+  float most = 0.0f;
   for (uint32_t c = threadIdx.x * VEC; c < cols; c += 1024u * VEC) {
-    float h[VEC], g[VEC];
+    float h[VEC], g[VEC], part = 0.0f;
     const uint32_t col = min(c, cols - VEC);
     values(c, col, h, g);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-      sum += col + (uint32_t)e >= c ? h[e] * h[e] : 0.0f;
+      part += col + (uint32_t)e >= c ? h[e] * h[e] : 0.0f;
       most = fmaxf(most, __builtin_fabsf(h[e] * g[e]));
     }
+    squares += (double)part;
     if (h_out) VecIo<T, VEC>::store(h_out + base + col, h);
   }
+  float sum = (float)squares;
   rms8_join<true>(sum, most, slot[0], 1024u);
   const float rr = fast_rsqrt(sum * inv_cols + eps);
   float largest = most * rr;

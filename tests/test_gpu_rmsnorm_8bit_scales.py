@@ -6,8 +6,11 @@ import pytest
 import workloads as W
 from oracle import oracle as O
 from paper_2009_10924_amd import binding as B
+from tests import operator_bounds as E
 from tests.gpu_util import note, run_spec
 from tests.test_gpu_rmsnorm_8bit import _case
+from workloads.graphs import RMS_EPS
+from workloads.inputs import quantise
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +52,20 @@ def test_rows_of_zeros_without_eps(cols):
     for k in (0, 2, 3):
         for name in ("h", "q", "s", "r", "n"):
             assert np.array_equal(raw[name][k], plain[name][k]), (k, name)
+
+
+@pytest.mark.parametrize("cols", [1 << 20, (1 << 22) + 8, (1 << 24) - 3])
+def test_very_long_rows(cols):
+    """The deviation's bound is that of any row (half of what the sum of squares is off by): equal values, whose roundings all go one way,
+    and positive ones."""
+    rng = np.random.default_rng(11)
+    for x in (np.full((1, cols), 1.7), rng.uniform(0.5, 1.5, (1, cols))):
+        spec = W.rmsnorm_8bit_graph(1, cols, dtype="bf16", residual=False, keep="stats")
+        inputs = W.make_inputs(spec, 3)
+        inputs["x"] = quantise(x, "bf16")
+        note(f"  case {spec.name}")
+        got, _, info, _ = run_spec(spec, inputs)
+        assert info["kernel"].startswith("rmsnorm8_long")
+        h = O.to_f64(inputs["x"], "bf16")
+        r = 1.0 / np.sqrt((h * h).mean(1, keepdims=True) + RMS_EPS)
+        E.close(got["r"], r, "f32", r * 48.0 * E.U32, "r")
