@@ -43,6 +43,7 @@ struct Compiler {
   uint32_t rows = 0, cols = 0;
   RowProgP p{};
   std::vector<int32_t> full_in, col_in, rscal_in;   // tensor ids by class (a transposed view of an input: the transpose's result)
+  bool sums_of_one_row = false;                     // a reduction over leading axes stands for the pattern's only row
   std::vector<int32_t> state_in;                    // states of dropouts: in no class, read only by them
   std::vector<int> drop_of;                         // per op: its entry among the program's dropouts, else -1
   // Transposes that keep the innermost axis only renumber rows.  One applied to a graph input is folded into
@@ -540,6 +541,7 @@ struct Compiler {
           }
           if (rows == 1 && op.axis != src.rank - 1) {   // over the one row there is: its values
             is_alias[i] = 1;
+            sums_of_one_row = true;
             break;
           }
           if (op.opcode == FS_REDUCE_SUM && op.axis == 0 && src.rank == rank && ka == V_FULL && !stretched_rows(src) &&
@@ -1163,11 +1165,27 @@ bool make_candidate(const fs_graph& g, const Compiler& c, int vec, const Shape& 
 
 }  // namespace
 
+// Whether a pattern of a single row with sums over it is a row program.  That is one workgroup, whose compute unit moves 0.11 MB a us; the
+// ops one by one have all of them, but for a reduction along the row, which then is one workgroup's as well.  So patterns with such a
+// reduction are (us, row program / op by op: RMS norm backward bf16 [1,2^17] 27 / 116, [1,2^24] 4540 / 12420, with dropout behind a residual
+// [1,2^24] 6290 / 12450), and the others go by an estimate of both sides, within a third of ten patterns' times from 2^13 to 2^22 columns: square
+// and sum f32 [1,2^15] 3.3 / 5.8, [1,2^16] 5.2 / 5.7, [1,2^17] 9.2 / 5.7, [1,2^22] 304 / 15.7; backward of dropout and gelu bf16 [1,2^15] 8.1 / 18.1,
+// [1,2^16] 15.6 / 18.1, [1,2^17] 30.5 / 18.6, [1,2^22] 951 / 46.
+static bool one_workgroup_pays(const fs_graph& g, const Compiler& c, int64_t bytes_min) {
+  if (!c.sums_of_one_row || c.n_reductions > 0) return true;
+  Candidate ops;
+  if (build_unfused(g, &ops) != FS_OK) return true;
+  predict(&ops);
+  const double memory = 9e-6 * (double)bytes_min, vector_units = (5.5e-6 * c.vec_instr + 3.2e-5 * c.trans) * c.p.cols;
+  return 2.0 + std::max(memory, vector_units) <= 1.3 * ops.info.predicted_us;
+}
+
 bool build_row_program(const fs_graph& g, std::vector<Candidate>* out) {
   if (holds_8bit(g)) return false;   // neither form reads or writes 8-bit values
   Compiler c(g);
   if (!c.run()) return false;
   const int64_t bytes_min = graph_bytes_min(g);
+  if (!one_workgroup_pays(g, c, bytes_min)) return false;
   for (int vec : step_widths(c.p)) {
     const bool interpretable = c.interpretable && vec == c.p.vec;
     for (const Shape& s : enumerate_shapes(c, vec, interpretable)) {
