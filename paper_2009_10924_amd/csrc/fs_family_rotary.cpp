@@ -164,9 +164,12 @@ bool build_rotary(const fs_graph& g, std::vector<Candidate>* out, PackForm*) {
     if (s.p_slots * s.angles.pairs > 4096) break;   // 32 KB of angles (one position has no more)
     s.h_slots = std::min(shared, slots / s.p_slots);
     const uint32_t p_tiles = (s.positions + s.p_slots - 1) / s.p_slots;
+    // A thread's rows, a kernel for each number: one is for single tokens (us for 1 / 2 / 3 / 5 rows: bf16 [16,1,32+8,128] 3.4 / 3.7 / 4.0 / 4.8),
+    // several keep more loads on their way ([2,8192,32+8,128] with 8 slots 62.3 / 59.2 / 57.2 / 63.5, pairs side by side 74.2 / 59.2 / 56.4 / 57.5;
+    // [4,4096,16+4,64] with 4 slots 18.4 / 17.7 / 17.5 / 17.4).
     for (int U : {1, 2, 3, 5}) {
       if (U > 1 && s.h_slots * (U == 5 ? 3 : U - 1) >= shared) break;
-      const uint32_t most = s.h_slots * U;   // a thread's rows are all loaded at once
+      const uint32_t most = s.h_slots * U;   // a thread's rows are all loaded at once: h_tile <= U * h_slots, which the kernel relies on
       uint32_t h_tiles = (shared + most - 1) / most;
       s.h_tile = (shared + h_tiles - 1) / h_tiles;
       h_tiles = (shared + s.h_tile - 1) / s.h_tile;

@@ -1,7 +1,7 @@
 // Rotary positions of one or two tensors (queries and keys) that share their positions.
 // A workgroup takes p_slots positions and h_tile of the rows at each.  Its angles depend on the positions alone, so each is formed once, by
-// one thread, and handed round through LDS, the loads of a thread's first rows on their way meanwhile; a thread takes the same step of
-// rows at one position, whose angles it keeps in registers.
+// one thread, and handed round through LDS, the loads of a thread's rows on their way meanwhile; a thread takes the same step of 1, 2, 3 or
+// 5 rows at one position, whose angles it keeps in registers.
 // Memory bounds it (n elements read, n written), as long as angles are few beside elements: an angle is about 60 operations, 20 of them in
 // 64 bits.  bf16 queries and keys [2,8192,32+8,128] with three axes and the head split: 59 us, 5.7 TB/s (a plain copy of as much 53); every
 // thread forming its own angles 65.  Pairs that stand side by side 56.  One token of 16 sequences: 3.4 us, the chain of one workgroup.
@@ -70,17 +70,18 @@ __global__ void __launch_bounds__(256) k_rotary(const T* x0, const T* x1, const 
   uint32_t unit = tid - slot * s.lanes;
   RotaryStep at = rotary_step<VEC, INTERLEAVED>(s, unit);
   typename IO::Raw ra[U], rb[U];
-  auto load = [&](uint32_t h, uint32_t a, uint32_t b) {
+  // a thread's U rows, all that it has: the tile holds at most U * h_slots of them
+  auto load = [&](uint32_t a, uint32_t b) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const uint32_t row = min(h + (uint32_t)u * s.h_slots, h_end - 1u);
+      const uint32_t row = min(h0 + own_h + (uint32_t)u * s.h_slots, h_end - 1u);
       const bool second = row >= s.t[0].shared;
       const T* const x = (second ? x1 : x0) + ((second ? in_p[1] : in_p[0]) + shared_row<LINES>(s, second, second ? row - s.t[0].shared : row, false));
       ra[u] = IO::template load<STREAM>(x + a);
       if constexpr (PAIRED) rb[u] = IO::template load<STREAM>(x + b);
     }
   };
-  load(h0 + own_h, at.a, at.b);
+  load(at.a, at.b);
   {
     // the workgroup's angles, a thread for one pair at one or more positions (a position is on its way while a speed is formed)
     const uint32_t first = fast_div(tid, s.div_pairs), at_once = pairs < 256u ? fast_div(256u, s.div_pairs) : 1u;
@@ -114,50 +115,45 @@ __global__ void __launch_bounds__(256) k_rotary(const T* x0, const T* x1, const 
       c[e] = w.x;
       d[e] = w.y;
     }
-    for (uint32_t h = h0 + own_h;;) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        uint32_t row = h + (uint32_t)u * s.h_slots;
-        if (!works || row >= h_end) continue;
-        const bool second = row >= s.t[0].shared;
-        T* const y = (second ? y1 : y0) + ((second ? out_p[1] : out_p[0]) + shared_row<LINES>(s, second, second ? row - s.t[0].shared : row, true));
-        float va[VEC], vb[VEC];
-        IO::widen(ra[u], va);
-        if constexpr (PAIRED) {
-          IO::widen(rb[u], vb);
-          if (pair != kCopies) {
+    for (int u = 0; u < U; ++u) {
+      const uint32_t row = h0 + own_h + (uint32_t)u * s.h_slots;
+      if (!works || row >= h_end) continue;
+      const bool second = row >= s.t[0].shared;
+      T* const y = (second ? y1 : y0) + ((second ? out_p[1] : out_p[0]) + shared_row<LINES>(s, second, second ? row - s.t[0].shared : row, true));
+      float va[VEC], vb[VEC];
+      IO::widen(ra[u], va);
+      if constexpr (PAIRED) {
+        IO::widen(rb[u], vb);
+        if (pair != kCopies) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-              const float v = va[e], w = vb[e];
-              va[e] = v * c[e] - w * d[e];
-              vb[e] = w * c[e] + v * d[e];
-            }
-            IO::store(y + at.b, vb);
+          for (int e = 0; e < VEC; ++e) {
+            const float v = va[e], w = vb[e];
+            va[e] = v * c[e] - w * d[e];
+            vb[e] = w * c[e] + v * d[e];
           }
-        } else if (pair != kCopies) {
-#pragma unroll
-          for (int e = 0; e < VEC; e += 2) {
-            const float v = va[e], w = va[e + 1];
-            va[e] = v * c[e / 2] - w * d[e / 2];
-            va[e + 1] = w * c[e / 2] + v * d[e / 2];
-          }
+          IO::store(y + at.b, vb);
         }
-        if (VEC > 1 && pair == kCopies && s.short_rest) {   // fewer elements than an access: one by one
+      } else if (pair != kCopies) {
 #pragma unroll
-          for (int e = 0; e < VEC; ++e)
-            if (e + (int)s.short_rest >= VEC) store1(y + at.a + e, va[e]);
-        } else {
-          IO::store(y + at.a, va);
+        for (int e = 0; e < VEC; e += 2) {
+          const float v = va[e], w = va[e + 1];
+          va[e] = v * c[e / 2] - w * d[e / 2];
+          va[e + 1] = w * c[e / 2] + v * d[e / 2];
         }
       }
-      h += U * s.h_slots;
-      if (h >= h_end) break;
-      load(h, at.a, at.b);
+      if (VEC > 1 && pair == kCopies && s.short_rest) {   // fewer elements than an access: one by one
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (e + (int)s.short_rest >= VEC) store1(y + at.a + e, va[e]);
+      } else {
+        IO::store(y + at.a, va);
+      }
     }
     unit += s.lanes;
     if (unit >= s.units) break;
     at = rotary_step<VEC, INTERLEAVED>(s, unit);
-    load(h0 + own_h, at.a, at.b);
+    load(at.a, at.b);
   }
 }
 
