@@ -1222,7 +1222,8 @@ static bool sums_need_no_reduction(const RowProgP& p) {
 // backward): bf16 [64,768] 6.2 / 3.3, 5.7 / 3.2, 6.1 / 3.7; [512,768] 6.3 / 3.6, 5.9 / 3.1, 6.5 / 3.8; [1024,768], beyond it, 6.2 / 7.0, 6.2 / 6.4,
 // 6.1 / 5.6; [256,3072] 6.1 / 4.2, 6.8 / 3.9, 6.1 / 3.6; [512,3072], beyond it, 6.3 / 7.6, 8.1 / 5.5, 7.0 / 4.7; f32 [512,768] 6.6 / 3.7, 6.3 / 4.4,
 // 6.3 / 3.8; [256,3072] 6.1 / 3.7, 7.0 / 4.0, 6.1 / 3.7.  The arithmetic is done twice as well: patterns of more than these three have are
-// left out.
+// left out.  A dropout, whose numbers both kinds of workgroup draw, leaves room for little else: alone with its sums, f32 and 16-bit [2,64],
+// [16,256], [512,768], [128,2048], [16,4096] 5.3 to 5.9 / 3.3 to 3.6.
 bool sums_beside_rows(const fs_graph& g, SumsBesideRows* out) {
   if (holds_8bit(g)) return false;
   Compiler c(g);
