@@ -349,8 +349,9 @@ int64_t fs_plan_source(const fs_plan *p, char *text, size_t capacity);
  *   bias of one shape).  y may be x's, dy's or the residual's own memory.
  *   With column sums beside it (a bias gradient), or in front of or behind row reductions (attention
  *   probabilities, a norm of the dropped branch), a dropout is part of a generated row kernel; where
- *   kernels are not generated (FS_CODEGEN=0) those run op by op.  An element that is not kept is 0 even
- *   where it held NaN or an infinity.
+ *   kernels are not generated (FS_CODEGEN=0) those run op by op.  A generated kernel has the probability
+ *   and the sequence as constants: patterns that differ in them are compiled apart.  An element that is
+ *   not kept is 0 even where it held NaN or an infinity.
  *
  * "rmsnorm_8bit": h = x, or x + residual, x + bias + residual, or FS_DROPOUT(x, or x + bias) + residual,
  *   read as it is or rounded to T (FS_CONVERT);

@@ -6,7 +6,7 @@
 // in an exchange of its own behind the sum's, the maximum would be rounded as n is, not once otherwise; that took 40.2 instead of 39.0 us at
 // bf16 [8192,4096], 46.5 instead of 42.5 at [2048,16384], and r's last bit, from the order of the sum, moves as many quotients over a rounding
 // border of the 8-bit format as the maximum's.)
-// Memory bounds it: x and the residual read, h and q written, 7 bytes an element of 16 bits.  bf16 [8192,4096] 38.9 us, 6.0 TB/s; f16
+// Memory bounds it: x and the residual read, h and q written, 7 bytes an element of 16 bits.  bf16 [8192,4096] 39.0 us, 6.0 TB/s; f16
 // [8192,2048] 22.0, with bias and dropout 22.8 (5.2 TB/s; the launch's ramp is 3 of it); [8191,2050] 22 to 26, rows straddle lines.  Four
 // rows of 4096: 2.5 us, the chain of load, sum, exchange, quotient.
 #include <hip/hip_runtime.h>

@@ -4,7 +4,7 @@
 // 5 rows at one position, whose angles it keeps in registers.
 // Memory bounds it (n elements read, n written), as long as angles are few beside elements: an angle is about 60 operations, 20 of them in
 // 64 bits.  bf16 queries and keys [2,8192,32+8,128] with three axes and the head split: 59 us, 5.7 TB/s (a plain copy of as much 53); every
-// thread forming its own angles 65.  Pairs that stand side by side 56.  One token of 16 sequences: 3.4 us, the chain of one workgroup.
+// thread forming its own angles 65.  Pairs that stand side by side 56.  One token of 16 sequences: 3.2 to 3.8 us, the chain of one workgroup.
 #include <hip/hip_runtime.h>
 
 #include "kernel_table.hpp"
