@@ -258,6 +258,10 @@ struct Explorer {
         }
         s.valid = true;
         s.t_fused = best;
+        // (a long row's sums, which its plan runs op by op: one step all the same, no slower than single ops, and the only one where results
+        // are stored rounded and read unrounded)
+        const OneRow row = one_row_times(*sub.g);
+        if (row.by_ops()) s.t_fused = std::min({best, row.ops_us * 1e-6, 0.999 * s.t_unfused});
         s.f = (s.t_unfused - s.t_fused) * 1e6;
       }
     }

@@ -199,6 +199,13 @@ std::string build_stitched(const fs_graph& g, std::vector<Candidate>* out, PackF
 // Candidates that run `g` as an interpreted row program (fs_rowprog.cpp); false if `g` is not a
 // pattern of element-wise ops and last-axis reductions over one row space.
 bool build_row_program(const fs_graph& g, std::vector<Candidate>* out);
+// A row program with sums over the only row there is: what its one workgroup takes at least, and what its ops one by one take (us; 0 and 0:
+// the graph is no such pattern).  Plans that are left to choose take the ops where they are faster.
+struct OneRow {
+  double workgroup_us = 0, ops_us = 0;
+  bool by_ops() const { return workgroup_us > ops_us; }
+};
+OneRow one_row_times(const fs_graph& g);
 // The graph's column sums and rows as one launch, where that is the faster form (fs_rowprog.cpp); false: it is not, or has none.
 bool sums_beside_rows(const fs_graph& g, SumsBesideRows* out);
 // Generated row kernels (fs_codegen.cpp): HIP source of the kernel specialised to the program `p` and its

@@ -345,10 +345,19 @@ fs_status fs::create_plan(const fs_graph* g, int32_t scheme, const fs_plan_opts*
 
   std::vector<Candidate> all;
   std::string pattern;
+  bool by_ops = false;
   PackForm pack_form;
   if (scheme != FS_SCHEME_UNFUSED) {
     pattern = build_stitched(*g, &all, &pack_form);
     for (Candidate& c : all) predict(&c);
+    // (the ops one by one join the list behind the others, and are the choice where no shape is asked for)
+    const bool any_shape = o.block_threads <= 0 && o.lanes_per_row <= 0 && o.vecs_per_lane <= 0;
+    Candidate u;
+    if (scheme == FS_SCHEME_AUTO && any_shape && pattern == "row_program" && one_row_times(*g).by_ops() && build_unfused(*g, &u) == FS_OK) {
+      predict(&u);
+      all.push_back(u);
+      by_ops = true;
+    }
   }
   if (scheme == FS_SCHEME_UNFUSED || (scheme == FS_SCHEME_AUTO && all.empty())) {
     Candidate u;
@@ -387,7 +396,7 @@ fs_status fs::create_plan(const fs_graph* g, int32_t scheme, const fs_plan_opts*
       return fail(FS_ERR_INVALID_ARG, "fs_plan_create: candidate %d outside 0..%zu", o.candidate, kept.size() - 1);
     best = o.candidate;
   } else {
-    best = choose(kept, o);
+    best = by_ops && kept.back().info.scheme == FS_SCHEME_UNFUSED ? (int)kept.size() - 1 : choose(kept, o);
     if (best < 0)
       return fail(FS_ERR_LOCALITY, "fs_plan_create: no %s candidate of pattern '%s' has the requested launch shape",
                   scheme_name(scheme), pattern.c_str());

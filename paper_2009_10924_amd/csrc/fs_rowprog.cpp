@@ -1167,27 +1167,11 @@ bool make_candidate(const fs_graph& g, const Compiler& c, int vec, const Shape& 
 
 }  // namespace
 
-// Whether a pattern of a single row with sums over it is a row program.  That is one workgroup, whose compute unit moves 0.11 MB a us; the
-// ops one by one have all of them, but for a reduction along the row, which then is one workgroup's as well.  So patterns with such a
-// reduction are (us, row program / op by op: RMS norm backward bf16 [1,2^17] 27 / 116, [1,2^24] 4540 / 12420, with dropout behind a residual
-// [1,2^24] 6290 / 12450), and the others go by an estimate of both sides, within a third of ten patterns' times from 2^13 to 2^22 columns: square
-// and sum f32 [1,2^15] 3.3 / 5.8, [1,2^16] 5.2 / 5.7, [1,2^17] 9.2 / 5.7, [1,2^22] 304 / 15.7; backward of dropout and gelu bf16 [1,2^15] 8.1 / 18.1,
-// [1,2^16] 15.6 / 18.1, [1,2^17] 30.5 / 18.6, [1,2^22] 951 / 46.
-static bool one_workgroup_pays(const fs_graph& g, const Compiler& c, int64_t bytes_min) {
-  if (!c.sums_of_one_row || c.n_reductions > 0) return true;
-  Candidate ops;
-  if (build_unfused(g, &ops) != FS_OK) return true;
-  predict(&ops);
-  const double memory = 9e-6 * (double)bytes_min, vector_units = (5.5e-6 * c.vec_instr + 3.2e-5 * c.trans) * c.p.cols;
-  return 2.0 + std::max(memory, vector_units) <= 1.3 * ops.info.predicted_us;
-}
-
 bool build_row_program(const fs_graph& g, std::vector<Candidate>* out) {
   if (holds_8bit(g)) return false;   // neither form reads or writes 8-bit values
   Compiler c(g);
   if (!c.run()) return false;
   const int64_t bytes_min = graph_bytes_min(g);
-  if (!one_workgroup_pays(g, c, bytes_min)) return false;
   for (int vec : step_widths(c.p)) {
     const bool interpretable = c.interpretable && vec == c.p.vec;
     for (const Shape& s : enumerate_shapes(c, vec, interpretable)) {
@@ -1196,6 +1180,25 @@ bool build_row_program(const fs_graph& g, std::vector<Candidate>* out) {
     }
   }
   return !out->empty();
+}
+
+// A row program over a single row is one workgroup, whose compute unit moves 0.11 MB a us; the ops one by one have all of them, but for a
+// reduction along the row, which then is one workgroup's as well.  So patterns with such a reduction are taken whatever the row's length (us, row
+// program / op by op: RMS norm backward bf16 [1,2^17] 27 / 116, [1,2^24] 4540 / 12420, with dropout behind a residual [1,2^24] 6290 / 12450), and
+// those that have only sums over the row there is go by an estimate of both sides, within a third of ten patterns' times from 2^13 to
+// 2^22 columns: square and sum f32 [1,2^15] 3.3 / 5.8, [1,2^16] 5.2 / 5.7, [1,2^17] 9.2 / 5.7, [1,2^22] 304 / 15.7; backward of dropout and gelu bf16
+// [1,2^15] 8.1 / 18.1, [1,2^16] 15.6 / 18.1, [1,2^17] 30.5 / 18.6, [1,2^22] 951 / 46.
+OneRow one_row_times(const fs_graph& g) {
+  OneRow t;
+  if (holds_8bit(g)) return t;
+  Compiler c(g);
+  Candidate ops;
+  if (!c.run() || !c.sums_of_one_row || c.n_reductions > 0 || build_unfused(g, &ops) != FS_OK) return t;
+  predict(&ops);
+  const double memory = 9e-6 * (double)graph_bytes_min(g), vector_units = (5.5e-6 * c.vec_instr + 3.2e-5 * c.trans) * c.p.cols;
+  t.workgroup_us = 2.0 + std::max(memory, vector_units);
+  t.ops_us = 1.3 * ops.info.predicted_us;
+  return t;
 }
 
 // No column sum depends on a row reduction.

@@ -43,3 +43,24 @@ def test_a_reduction_along_the_row(cols):
 def test_two_rows_are_not_one():
     info = B.Plan(B.Graph.from_spec(W.dropout_backward_graph(2, 1 << 20, act="gelu", bias=True, dbias=True))).info
     assert info["pattern"] == "row_generated", info
+
+
+def test_asked_for_by_scheme_or_shape():
+    """What is left to choose goes op by op; what is asked for is there at any length."""
+    graph = B.Graph.from_spec(_dropout(1 << 20))
+    assert B.Plan(graph).info["pattern"] == "unfused"
+    assert B.Plan(graph, "lds").info["pattern"] == "row_generated"
+    assert B.Plan(graph, block_threads=1024).info["block"][0] == 1024
+    chosen = B.Plan(graph).info
+    assert chosen["candidate"] == chosen["n_candidates"] - 1 and B.Plan(graph, candidate=chosen["candidate"]).info["pattern"] == "unfused"
+    assert B.Plan(graph, candidate=0).info["pattern"] == "row_generated"
+
+
+@pytest.mark.parametrize("cols", [2048, 1 << 15, 1 << 17, 1 << 18, 1 << 20, 1 << 24])
+@pytest.mark.parametrize("act", ["none", "gelu"])
+def test_explored(act, cols):
+    """The 16-bit gradient is stored rounded and summed unrounded, so its ops have to stay in one step, whichever way that runs."""
+    patterns = B.Program(B.Graph.from_spec(W.dropout_backward_graph(1, cols, act=act, bias=act != "none", dbias=True))).patterns()
+    info = patterns[-1]["info"]
+    assert info["pattern"] == ("row_generated" if cols <= 1 << 15 else "unfused"), [p["info"]["kernel"] for p in patterns]
+    assert cols > 1 << 15 or len(patterns) == 1
