@@ -134,7 +134,9 @@ typedef struct fs_attr_rotary {
  * workgroups, which the paper leaves out (Section 4.1, last paragraph) and which
  * the column-reduction pattern needs; UNFUSED = one kernel per op; AUTO = the
  * cost model chooses among the stitched candidates and falls back to UNFUSED
- * when no stitched kernel matches.                                              */
+ * when no stitched kernel matches, or takes the ops one by one (then the last entry
+ * of its candidates) for sums over the only row of a pattern where that row is so
+ * long that one workgroup would take longer.                                     */
 enum fs_scheme {
   FS_SCHEME_AUTO = 0, FS_SCHEME_UNFUSED = 1, FS_SCHEME_LOCAL = 2,
   FS_SCHEME_WAVE = 3, FS_SCHEME_LDS = 4, FS_SCHEME_GLOBAL = 5
